@@ -253,6 +253,67 @@ int cq_encode_losses(const float *W, const int8_t *k, int B, int G, int64_t N, i
 int cq_encode(const float *W, int B, int G, int64_t N, int64_t K, int objective, int effort, int8_t *k, float *scale,
               uint16_t *a, uint16_t *b, void *stream);
 
+/* ---- 4-bit floating point with block scales (no counterpart in the paper) --------------------------------
+ * A second stored format, for checkpoints that are published in it, and the operators that a linear layer, an MLP and routed
+ * experts need of it.  A value is an e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) times the scale of its block of
+ * consecutive k; weights AND activations are in it, and the tensor cores multiply them as they are.
+ *   CQ_MXFP4  blocks of 32, scale byte b: 2^(b - 127), 255 is NaN.  Quantiser: b - 127 = floor(log2 max|x|) - 2, at least -127; the codes
+ *             are x / scale to the nearest, ties to the even code, at most 6.
+ *   CQ_NVFP4  blocks of 16, scale byte in e4m3 (127 is NaN), and one fp32 factor g > 0 for the whole matrix, given as
+ *             `tensor_scale`: a DEVICE pointer to it (NULL: 1), read when the kernel runs.  Quantiser, in fp32 with IEEE roundings:
+ *             r = 1 / g; scale = (max|x| r) / 6, at least 2^-9 and at most 448, to the nearest e4m3; i = r / scale; codes x i as above.
+ *             (g = max|x| / 2688 over the matrix uses the whole range.)  The value of a code is code * (scale * g).
+ *   A block that holds an infinity or a NaN gets the scale NaN and codes 0; the products it enters are NaN.
+ * Canonical form: codes uint8 [M][K/2], the even k in the low half of a byte; scales uint8 [M][K/32] or [M][K/16].
+ * K is a multiple of the block.  The device layout is private (cq_fp4_pack, cq_fp4_unpack; quantisers write it directly);
+ * rows behind the last of a matrix or of a group are never written and reach no result.
+ * E matrices of one shape (experts) lie one after another in one layout; their tensor scales are E floats.
+ * dtype: CQ_BF16, CQ_F16, CQ_F32.  Rows of x are `ldx` elements apart, 16-byte aligned.
+ * Errors as above; CQ_ERR_UNSUPPORTED: K not a multiple of the block, more than 512 groups, sizes above 2^30. */
+enum { CQ_MXFP4 = 0, CQ_NVFP4 = 1 };
+enum { CQ_BF16 = 0, CQ_F16 = 1, CQ_F32 = 2 };
+
+/* Bytes of the layout of E matrices of M x K, and of R routed rows in E groups; 0 for unsupported arguments. */
+size_t cq_fp4_layout_bytes(int fmt, int64_t E, int64_t M, int64_t K);
+size_t cq_fp4_routed_layout_bytes(int fmt, int64_t E, int64_t R, int64_t K);
+/* Bytes of the workspace of cq_fp4_linear and cq_fp4_linear_routed (the products of quantised rows need 512).  Zero it once with
+ * cq_workspace_init; cq_gemm_status reports a bounded wait that gave up in any call since then. */
+size_t cq_fp4_workspace_bytes(int fmt, int64_t M, int64_t K);
+size_t cq_fp4_routed_workspace_bytes(int fmt, int64_t E, int64_t R, int64_t K);
+
+/* Canonical form to layout, and back (a bijection). */
+int cq_fp4_pack(const uint8_t *codes, const uint8_t *scales, int fmt, int64_t E, int64_t M, int64_t K, void *layout, void *stream);
+int cq_fp4_unpack(const void *layout, int fmt, int64_t E, int64_t M, int64_t K, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* The quantiser: E matrices of M rows, row m of matrix e at x + (e M + m) ldx. */
+int cq_fp4_quantize(const void *x, int dtype, int64_t ldx, int fmt, int64_t E, int64_t M, int64_t K, const float *tensor_scale, void *layout, void *stream);
+/* Routed rows: row r of the layout is row route_token[r] of x [T][K] (zeros for a token outside [0, T)), and belongs to the group e
+ * with expert_offset[e] <= r < expert_offset[e + 1].  Both arrays are int32 on the DEVICE, R and E + 1 of them: no host
+ * needs to know the loads, and a captured call follows them.  Offsets start at 0 and ascend, the last at most R; what does not is taken as
+ * the largest offset so far, at most R.  Rows from the last offset on belong to nobody and are left alone.  tensor_scale: one factor. */
+int cq_fp4_quantize_routed(const void *x, int dtype, int64_t ldx, int64_t T, const int32_t *route_token, const int32_t *expert_offset, int64_t E, int64_t R, int fmt,
+                           int64_t K, const float *tensor_scale, void *layout, void *stream);
+/* h [M][2 I] (gate | up) -> silu(gate) * up, correctly rounded to the model dtype (from fp32), and at once quantised: what stands between
+ * the two products of an MLP block, without the activation reaching memory.  expert_offset: NULL, or the groups of routed rows. */
+int cq_fp4_swiglu_quantize(const void *h, int dtype, int64_t ldh, int fmt, int64_t M, int64_t I, const int32_t *expert_offset, int64_t E, const float *tensor_scale,
+                           void *layout, void *stream);
+/* The values that a layout stands for, y [E M][K] (routed: [M][K], rows of no group left alone), rounded once to `dtype`. */
+int cq_fp4_dequantize(const void *layout, int fmt, int64_t E, int64_t M, int64_t K, const int32_t *expert_offset, const float *tensor_scale, void *y, int dtype, void *stream);
+
+/* y[M][N] = x W^T; w: layout of the N x K matrix, x: layout of M rows (cq_fp4_quantize, cq_fp4_swiglu_quantize), both of one format.
+ * fp32 accumulation, (w_scale * x_scale) applied to the sum, one rounding to bfloat16 or (act_f16) binary16. */
+int cq_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, int fmt, uint16_t *y, int act_f16, int64_t M, int64_t N, int64_t K,
+                void *workspace, size_t workspace_bytes, void *stream);
+/* The same from rows in the model dtype (that of y), quantised on the way. */
+int cq_fp4_linear(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, const float *x_scale, int fmt, uint16_t *y, int act_f16, int64_t M, int64_t N,
+                  int64_t K, void *workspace, size_t workspace_bytes, void *stream);
+/* Routed: w holds E matrices; rows of group e of x, y[R][N] meet matrix e.  Rows of y of no group are left as they were. */
+int cq_fp4_gemm_routed(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *expert_offset, int64_t E, int fmt, uint16_t *y, int act_f16,
+                       int64_t R, int64_t N, int64_t K, void *workspace, size_t workspace_bytes, void *stream);
+int cq_fp4_linear_routed(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, int64_t T, const int32_t *route_token, const float *x_scale,
+                         const int32_t *expert_offset, int64_t E, int fmt, uint16_t *y, int act_f16, int64_t R, int64_t N, int64_t K, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

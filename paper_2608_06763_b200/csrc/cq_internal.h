@@ -147,4 +147,17 @@ cudaError_t launch_gemm_tc(const void *layout, const Dims &d, const uint16_t *x,
 cudaError_t launch_gemm_a8_tc(const void *layout, const Dims &d, const uint16_t *x, uint16_t *y, int64_t M, bool act_f16,
                               uint8_t *ws, const Workspace &plan, cudaStream_t st, bool prequantized = false);
 
+// 4-bit floating point with block scales (cq_fp4_quant.cu, cq_fp4_gemm.cu).  Which rows a quantiser takes and where they go:
+// dense (E matrices of `per` rows), or routed (row r is row route_token[r] of x where that is given, groups by `offset` on the device).
+struct Fp4Rows { const int32_t *route_token, *offset; int E; int64_t per, rows, T; };
+cudaError_t launch_fp4_quantize(const void *x, int dtype, int64_t ldx, const Fp4Rows &rows, int fmt, int64_t K, const float *tensor_scale, void *layout, cudaStream_t st);
+cudaError_t launch_fp4_swiglu_quantize(const void *h, int dtype, int64_t ldh, const Fp4Rows &rows, int fmt, int64_t I, const float *tensor_scale, void *layout,
+                                       cudaStream_t st);
+cudaError_t launch_fp4_dequantize(const void *layout, const Fp4Rows &rows, int fmt, int64_t K, const float *tensor_scale, void *y, int dtype, cudaStream_t st);
+// in: checkpoint form to layout; else back
+cudaError_t launch_fp4_exchange(uint8_t *codes, uint8_t *scales, const Fp4Rows &rows, int fmt, int64_t K, void *layout, bool in, cudaStream_t st);
+// y[M][N] = x W^T of two layouts; offset != null: E groups of rows, group e times matrix e
+cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, int fmt, uint16_t *y, int64_t M,
+                            int64_t N, int64_t K, bool f16, int *status, cudaStream_t st);
+
 }  // namespace cq

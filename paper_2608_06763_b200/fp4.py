@@ -1,0 +1,288 @@
+"""Binding of the 4-bit floating point operators (include/cubicquant.h, last section).  Argument marshalling only."""
+from __future__ import annotations
+
+import ctypes as C
+from dataclasses import dataclass
+
+import torch
+
+from . import binding
+from .binding import CubicQuantError, _check, _stream
+
+CQ_MXFP4, CQ_NVFP4 = 0, 1
+_BLOCK = (32, 16)
+_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+_L = None
+
+
+def _lib():
+    global _L
+    if _L is None:
+        L = binding.lib()
+        vp, i, i64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
+        for name, args in (("layout_bytes", [i, i64, i64, i64]), ("routed_layout_bytes", [i, i64, i64, i64]),
+                           ("workspace_bytes", [i, i64, i64]), ("routed_workspace_bytes", [i, i64, i64, i64])):
+            fn = getattr(L, "cq_fp4_" + name)
+            fn.restype, fn.argtypes = sz, args
+        for name, args in (("pack", [vp, vp, i, i64, i64, i64, vp, vp]), ("unpack", [vp, i, i64, i64, i64, vp, vp, vp]),
+                           ("quantize", [vp, i, i64, i, i64, i64, i64, vp, vp, vp]),
+                           ("quantize_routed", [vp, i, i64, i64, vp, vp, i64, i64, i, i64, vp, vp, vp]),
+                           ("swiglu_quantize", [vp, i, i64, i, i64, i64, vp, i64, vp, vp, vp]),
+                           ("dequantize", [vp, i, i64, i64, i64, vp, vp, vp, i, vp]),
+                           ("gemm", [vp, vp, vp, vp, i, vp, i, i64, i64, i64, vp, sz, vp]),
+                           ("linear", [vp, vp, vp, i64, vp, i, vp, i, i64, i64, i64, vp, sz, vp]),
+                           ("gemm_routed", [vp, vp, vp, vp, vp, i64, i, vp, i, i64, i64, i64, vp, sz, vp]),
+                           ("linear_routed", [vp, vp, vp, i64, i64, vp, vp, vp, i64, i, vp, i, i64, i64, i64, vp, sz, vp])):
+            fn = getattr(L, "cq_fp4_" + name)
+            fn.restype, fn.argtypes = i, args
+        _L = L
+    return _L
+
+
+def _need(ok, what: str):
+    if not ok:
+        raise CubicQuantError(what)
+
+
+def _here(*tensors):
+    """Every tensor on the current device: the call goes to that device's current stream."""
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.device.index == dev):
+            raise CubicQuantError(f"a tensor on {t.device}, with device {dev} current: switch with torch.cuda.device")
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+@dataclass
+class Fp4Tensor:
+    """Rows in the 4-bit device layout: `matrices` of M x K one after another, or (groups) M routed rows of K."""
+    layout: torch.Tensor
+    fmt: int
+    matrices: int
+    M: int
+    K: int
+    tensor_scale: torch.Tensor | None = None     # NVFP4: fp32 on the device, one value or one for each matrix
+    groups: int = 0                              # routed rows: how many groups
+    expert_offset: torch.Tensor | None = None    # routed rows: int32 [groups + 1] on the device
+
+
+def _check_format(fmt: int, K: int):
+    _need(fmt in (CQ_MXFP4, CQ_NVFP4), "fmt is CQ_MXFP4 or CQ_NVFP4")
+    _need(K > 0 and K % _BLOCK[fmt] == 0, f"K = {K} is not a multiple of the block of {_BLOCK[fmt]}")
+
+
+def _check_scale(scale, fmt: int, matrices: int = 1):
+    if scale is None:
+        return
+    _need(fmt == CQ_NVFP4, "MXFP4 has no tensor scale")
+    _need(scale.dtype == torch.float32 and scale.numel() == matrices and scale.is_contiguous(),
+          f"tensor_scale is {matrices} fp32 value(s) on the device")
+
+
+def _check_offset(offset, groups=None):
+    _need(isinstance(offset, torch.Tensor) and offset.dtype == torch.int32 and offset.dim() == 1 and offset.is_contiguous() and
+          (offset.numel() >= 2 if groups is None else offset.numel() == groups + 1),
+          "expert_offset is an int32 tensor of one more value than there are matrices")
+
+
+def _check_rows(x, name="x"):
+    """Rows of contiguous values, any distance of whole 16 bytes apart; a row by itself, any."""
+    _need(x.dtype in _DTYPE, f"{name} is bfloat16, float16 or float32")
+    _need(x.dim() == 2 and (x.shape[1] == 1 or x.stride(1) == 1), f"{name} is a matrix whose rows are contiguous")
+    ld = x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    _need(ld >= x.shape[1] and x.data_ptr() % 16 == 0 and ld * x.element_size() % 16 == 0, f"rows of {name} start on 16-byte boundaries and do not overlap")
+    return ld
+
+
+def cq_fp4_empty(fmt: int, M: int, K: int, matrices: int = 1, groups: int | None = None, device=None) -> Fp4Tensor:
+    """Room for `matrices` of M x K, or for M routed rows of K in `groups` groups."""
+    _check_format(fmt, K)
+    if groups is None:
+        n = _lib().cq_fp4_layout_bytes(fmt, matrices, M, K)
+    else:
+        _need(matrices == 1, "routed rows are one matrix")
+        n = _lib().cq_fp4_routed_layout_bytes(fmt, groups, M, K)
+    _need(n > 0 or M == 0, f"no layout for {matrices} x {M} x {K}, {groups} groups")
+    return Fp4Tensor(torch.empty(n, dtype=torch.uint8, device=device or "cuda"), fmt, matrices, M, K, None, groups or 0)
+
+
+def _into(out, fmt, M, K, matrices=1, groups=None, device=None) -> Fp4Tensor:
+    if out is None:
+        return cq_fp4_empty(fmt, M, K, matrices, groups, device)
+    _need((out.fmt, out.matrices, out.M, out.K, out.groups) == (fmt, matrices, M, K, groups or 0), "out is of another format or shape")
+    return out
+
+
+def cq_fp4_pack(codes: torch.Tensor, scales: torch.Tensor, fmt: int, tensor_scale: torch.Tensor | None = None) -> Fp4Tensor:
+    """A checkpoint's codes uint8 [.., M, K / 2] and scales uint8 [.., M, K / block] (the first axis, if there are three: matrices)."""
+    _need(codes.dim() in (2, 3) and codes.dtype == torch.uint8 and scales.dtype == torch.uint8, "codes and scales are uint8, [M, K / 2] or [E, M, K / 2]")
+    E, M, K = (codes.shape[0] if codes.dim() == 3 else 1), codes.shape[-2], codes.shape[-1] * 2
+    _check_format(fmt, K)
+    _need(tuple(scales.shape) == tuple(codes.shape[:-1]) + (K // _BLOCK[fmt],) and codes.is_contiguous() and scales.is_contiguous(), "scales are [.., M, K / block], both contiguous")
+    _check_scale(tensor_scale, fmt, E)
+    _here(codes, scales, tensor_scale)
+    q = cq_fp4_empty(fmt, M, K, E, device=codes.device)
+    q.tensor_scale = tensor_scale
+    _check(_lib().cq_fp4_pack(codes.data_ptr(), scales.data_ptr(), fmt, E, M, K, q.layout.data_ptr(), _stream()), "cq_fp4_pack")
+    return q
+
+
+def cq_fp4_unpack(q: Fp4Tensor):
+    """(codes, scales) as cq_fp4_pack takes them."""
+    _need(not q.groups, "routed rows have no checkpoint form")
+    _here(q.layout)
+    lead = (q.matrices, q.M) if q.matrices > 1 else (q.M,)
+    codes = torch.empty(lead + (q.K // 2,), dtype=torch.uint8, device=q.layout.device)
+    scales = torch.empty(lead + (q.K // _BLOCK[q.fmt],), dtype=torch.uint8, device=q.layout.device)
+    _check(_lib().cq_fp4_unpack(q.layout.data_ptr(), q.fmt, q.matrices, q.M, q.K, codes.data_ptr(), scales.data_ptr(), _stream()), "cq_fp4_unpack")
+    return codes, scales
+
+
+def cq_fp4_quantize(x: torch.Tensor, fmt: int, tensor_scale: torch.Tensor | None = None, route_token: torch.Tensor | None = None,
+                    expert_offset: torch.Tensor | None = None, out: Fp4Tensor | None = None) -> Fp4Tensor:
+    """x [M, K] or [E, M, K] (bfloat16, float16, float32) -> codes and block scales.  With route_token and expert_offset (int32 on the
+    device): rows route_token of x, grouped by matrix, for cq_fp4_gemm_routed."""
+    E = 1
+    if x.dim() == 3:
+        _need(x.is_contiguous() and route_token is None, "several matrices are one contiguous tensor")
+        E, x = x.shape[0], x.flatten(0, 1)
+    ld = _check_rows(x)
+    K = x.shape[1]
+    _check_format(fmt, K)
+    _check_scale(tensor_scale, fmt, E)
+    _need((route_token is None) == (expert_offset is None), "route_token and expert_offset come together")
+    _here(x, tensor_scale, route_token, expert_offset, out.layout if out is not None else None)
+    if route_token is None:
+        q = _into(out, fmt, x.shape[0] // E if E else 0, K, E, device=x.device)
+        if x.shape[0]:
+            _check(_lib().cq_fp4_quantize(x.data_ptr(), _DTYPE[x.dtype], ld, fmt, E, q.M, K, _at(tensor_scale), q.layout.data_ptr(), _stream()), "cq_fp4_quantize")
+    else:
+        _check_offset(expert_offset)
+        _need(route_token.dtype == torch.int32 and route_token.dim() == 1 and route_token.is_contiguous(), "route_token is an int32 tensor")
+        R, groups = route_token.numel(), expert_offset.numel() - 1
+        q = _into(out, fmt, R, K, 1, groups, device=x.device)
+        q.expert_offset = expert_offset
+        if R:
+            _check(_lib().cq_fp4_quantize_routed(x.data_ptr(), _DTYPE[x.dtype], ld, x.shape[0], route_token.data_ptr(), expert_offset.data_ptr(), groups, R, fmt, K,
+                                                 _at(tensor_scale), q.layout.data_ptr(), _stream()), "cq_fp4_quantize")
+    q.tensor_scale = tensor_scale
+    return q
+
+
+def cq_fp4_swiglu_quantize(h: torch.Tensor, fmt: int, tensor_scale: torch.Tensor | None = None, expert_offset: torch.Tensor | None = None,
+                           out: Fp4Tensor | None = None) -> Fp4Tensor:
+    """h [M, 2 I] (gate | up; bfloat16 or float16) -> silu(gate) * up, rounded to h's dtype, quantised.  expert_offset: the rows are routed."""
+    ld = _check_rows(h, "h")
+    _need(h.dtype != torch.float32 and h.shape[1] % 2 == 0, "h is [M, 2 I] in bfloat16 or float16")
+    M, K = h.shape[0], h.shape[1] // 2
+    _check_format(fmt, K)
+    _check_scale(tensor_scale, fmt)
+    if expert_offset is not None:
+        _check_offset(expert_offset)
+    _here(h, tensor_scale, expert_offset, out.layout if out is not None else None)
+    groups = expert_offset.numel() - 1 if expert_offset is not None else None
+    q = _into(out, fmt, M, K, 1, groups, device=h.device)
+    q.tensor_scale, q.expert_offset = tensor_scale, expert_offset
+    if M:
+        _check(_lib().cq_fp4_swiglu_quantize(h.data_ptr(), _DTYPE[h.dtype], ld, fmt, M, K, _at(expert_offset), groups or 0, _at(tensor_scale), q.layout.data_ptr(), _stream()),
+               "cq_fp4_swiglu_quantize")
+    return q
+
+
+def cq_fp4_dequantize(q: Fp4Tensor, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values that q stands for, [M, K] or [E, M, K]; rows of no group are left as they were (new ones: zeros)."""
+    shape = (q.matrices, q.M, q.K) if q.matrices > 1 else (q.M, q.K)
+    if out is None:
+        out = (torch.zeros if q.groups else torch.empty)(shape, dtype=dtype, device=q.layout.device)
+    _need(out.dtype in _DTYPE and tuple(out.shape) == shape and out.is_contiguous() and out.data_ptr() % 16 == 0, f"out is a contiguous tensor of shape {shape}")
+    _here(q.layout, q.tensor_scale, q.expert_offset, out)
+    if q.M:
+        _check(_lib().cq_fp4_dequantize(q.layout.data_ptr(), q.fmt, q.groups or q.matrices, q.M, q.K, _at(q.expert_offset), _at(q.tensor_scale), out.data_ptr(),
+                                        _DTYPE[out.dtype], _stream()), "cq_fp4_dequantize")
+    return out
+
+
+def cq_fp4_workspace(w: Fp4Tensor, M: int) -> torch.Tensor:
+    """A zeroed workspace for products of up to M rows (routes) with w."""
+    n = _lib().cq_fp4_routed_workspace_bytes(w.fmt, w.matrices, max(M, 1), w.K)
+    return torch.zeros(max(n, 512), dtype=torch.uint8, device=w.layout.device)
+
+
+def _product_args(w, x, M, tensor_scale, workspace, out):
+    """What the dense and the routed product check alike; returns (workspace, out, 16-bit output is binary16)."""
+    _need(isinstance(w, Fp4Tensor) and not w.groups, "w is a matrix of cq_fp4_pack or cq_fp4_quantize")
+    quantised = isinstance(x, Fp4Tensor)
+    if quantised:
+        _need(x.fmt == w.fmt and x.matrices == 1 and x.K == w.K, "x and w differ in format or K")
+        _need(tensor_scale is None, "x carries its own tensor scale")
+        dtype = out.dtype if out is not None else torch.bfloat16
+    else:
+        _need(x.dtype != torch.float32 and x.shape[1] == w.K, f"x is [M, {w.K}] in bfloat16 or float16")
+        _check_scale(tensor_scale, w.fmt)
+        dtype = x.dtype
+    dev = w.layout.device
+    if out is None:
+        out = torch.empty((M, w.M), dtype=dtype, device=dev)
+    _need(out.dtype == dtype and dtype in (torch.bfloat16, torch.float16) and tuple(out.shape) == (M, w.M) and out.is_contiguous() and out.data_ptr() % 16 == 0,
+          f"out is a contiguous [{M}, {w.M}] tensor in the dtype of x")
+    if workspace is None:
+        workspace = torch.zeros(512, dtype=torch.uint8, device=dev) if quantised else cq_fp4_workspace(w, M)
+    _need(workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace is a contiguous uint8 tensor")
+    return workspace, out, 1 if dtype == torch.float16 else 0
+
+
+def cq_fp4_gemm(w: Fp4Tensor, x, tensor_scale: torch.Tensor | None = None, workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y[M, N] = x W^T.  x: [M, K] in the model dtype (quantised on the way, NVFP4 with tensor_scale) or an Fp4Tensor; y has the dtype of x
+    (of out, or bfloat16)."""
+    M = x.M if isinstance(x, Fp4Tensor) else x.shape[0]
+    _need(w.matrices == 1, "several matrices: cq_fp4_gemm_routed")
+    if isinstance(x, Fp4Tensor):
+        _need(not x.groups, "routed rows: cq_fp4_gemm_routed")
+        workspace, out, f16 = _product_args(w, x, M, tensor_scale, workspace, out)
+        _here(w.layout, w.tensor_scale, x.layout, x.tensor_scale, workspace, out)
+        if M:
+            status = _lib().cq_fp4_gemm(w.layout.data_ptr(), _at(w.tensor_scale), x.layout.data_ptr(), _at(x.tensor_scale), w.fmt, out.data_ptr(), f16, M, w.M, w.K,
+                                        workspace.data_ptr(), workspace.numel(), _stream())
+            if status != 0:
+                _check(status, "cq_fp4_gemm")
+        return out
+    ld = _check_rows(x)
+    workspace, out, f16 = _product_args(w, x, M, tensor_scale, workspace, out)
+    _here(w.layout, w.tensor_scale, x, tensor_scale, workspace, out)
+    if M:
+        status = _lib().cq_fp4_linear(w.layout.data_ptr(), _at(w.tensor_scale), x.data_ptr(), ld, _at(tensor_scale), w.fmt, out.data_ptr(), f16, M, w.M, w.K,
+                                      workspace.data_ptr(), workspace.numel(), _stream())
+        if status != 0:
+            _check(status, "cq_fp4_gemm")
+    return out
+
+
+def cq_fp4_gemm_routed(w: Fp4Tensor, x, route_token: torch.Tensor | None, expert_offset: torch.Tensor, tensor_scale: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Route-major y[R, N]: rows [expert_offset[e], expert_offset[e + 1]) meet matrix e of w.  x: [T, K] in the model dtype with route_token
+    (int32 [R] on the device), or an Fp4Tensor of R routed rows with route_token None.  expert_offset: int32 on the device; rows from
+    its last value on are left as they were (in a new tensor: undefined)."""
+    _check_offset(expert_offset, w.matrices)
+    if isinstance(x, Fp4Tensor):
+        _need(route_token is None and x.groups == w.matrices, "x holds the routed rows of as many groups as w has matrices")
+        R = x.M
+        workspace, out, f16 = _product_args(w, x, R, tensor_scale, workspace, out)
+        _here(w.layout, w.tensor_scale, x.layout, x.tensor_scale, expert_offset, workspace, out)
+        if R:
+            _check(_lib().cq_fp4_gemm_routed(w.layout.data_ptr(), _at(w.tensor_scale), x.layout.data_ptr(), _at(x.tensor_scale), expert_offset.data_ptr(), w.matrices, w.fmt,
+                                             out.data_ptr(), f16, R, w.M, w.K, workspace.data_ptr(), workspace.numel(), _stream()), "cq_fp4_gemm_routed")
+        return out
+    ld = _check_rows(x)
+    _need(route_token is not None and route_token.dtype == torch.int32 and route_token.dim() == 1 and route_token.is_contiguous(), "route_token is an int32 tensor")
+    R = route_token.numel()
+    workspace, out, f16 = _product_args(w, x, R, tensor_scale, workspace, out)
+    _here(w.layout, w.tensor_scale, x, tensor_scale, route_token, expert_offset, workspace, out)
+    if R:
+        _check(_lib().cq_fp4_linear_routed(w.layout.data_ptr(), _at(w.tensor_scale), x.data_ptr(), ld, x.shape[0], route_token.data_ptr(), _at(tensor_scale),
+                                           expert_offset.data_ptr(), w.matrices, w.fmt, out.data_ptr(), f16, R, w.M, w.K, workspace.data_ptr(), workspace.numel(), _stream()),
+               "cq_fp4_gemm_routed")
+    return out
