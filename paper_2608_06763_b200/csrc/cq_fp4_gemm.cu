@@ -16,57 +16,105 @@ struct GemmArgs {
     uint16_t *y;
     int *status;
     int E, NB, KT, steps;    // matrices; row blocks of W; k tiles; 64-wide steps of the tensor core that K has
-    int token_tiles, band;   // dense: tiles along the rows of x; how many of them are swept together
+    int bt, token_tiles, band;   // rows of x to a tile; dense: tiles along the rows of x; how many of them are swept together
     int M;                   // rows of x
     int64_t N;
-    bool f16;
+    bool f16, wide;          // wide: rows of y start on 16-byte boundaries
 };
 
-// D[tmem] (+)= A B, codes by shared-memory descriptors, scales in tensor memory
-template <int FMT>
+// D[tmem] (+)= A B, codes by shared-memory descriptors, scales in tensor memory.  PAIR: by the tensor cores of two SMs, each with 128 of
+// the 256 rows of A and half of the columns of B in its shared memory.
+template <int FMT, bool PAIR>
 __device__ __forceinline__ void umma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
-    if (FMT == MX)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+#define CQ_UMMA_FP4(group, kind)                                                                          \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                        \
+                 "tcgen05.mma.cta_group::" group ".kind::" kind " [%0], %1, %2, %3, [%4], [%5], p;\n\t}"  \
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory")
+    if (FMT == MX) {
+        if (PAIR) CQ_UMMA_FP4("2", "mxf4.block_scale.scale_vec::2X"); else CQ_UMMA_FP4("1", "mxf4.block_scale.scale_vec::2X");
+    } else {
+        if (PAIR) CQ_UMMA_FP4("2", "mxf4nvf4.block_scale.scale_vec::4X"); else CQ_UMMA_FP4("1", "mxf4nvf4.block_scale.scale_vec::4X");
+    }
+#undef CQ_UMMA_FP4
 }
-// 512 bytes of scales (32 rows of 16 bytes) to four columns of tensor memory, in all four groups of 32 lanes
+// 512 bytes of scales (32 rows of 16 bytes) to four columns of tensor memory, in all four groups of 32 lanes.  PAIR: in both SMs, each
+// from its own shared memory.
+template <bool PAIR>
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 // descriptor of such a piece: eight-row groups of 128 contiguous bytes, no swizzle
 __device__ __forceinline__ uint64_t smem_desc_plain(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)8 << 16) | ((uint64_t)8 << 32) | ((uint64_t)1 << 46);
 }
-// Instruction descriptor: e2m1 both, scale type (bit 23: e8m0), M = 128, N by the tile.  sf: which scales of a 32-bit column an
+// Instruction descriptor: e2m1 both, scale type (bit 23: e8m0), M = 128 (a pair 256), N by the tile.  sf: which scales of a 32-bit column an
 // MXFP4 step takes (0: the first two, 2: the last two).
-template <int FMT>
+template <int FMT, bool PAIR>
 __device__ __forceinline__ uint32_t idesc_fp4(uint32_t n, uint32_t sf) {
-    return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (FMT == MX ? 1u << 23 : 0u) | (1u << 27) | (sf << 4) | (sf << 29);
+    return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (FMT == MX ? 1u << 23 : 0u) | ((PAIR ? 2u : 1u) << 27) | (sf << 4) | (sf << 29);
 }
 
-template <int FMT, int BN>
+// accumulators to registers in the order of 8x8 matrices: lane l has row l / 4 (+ 8), columns 8 i + 2 (l % 4) and the next
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                   "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_out(uint32_t lo, uint32_t hi, float alpha, bool f16) {
+    const float a = __uint_as_float(lo) * alpha, b = __uint_as_float(hi) * alpha;
+    if (f16) { const __half2 p = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t *>(&p); }
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+__device__ __forceinline__ uint16_t round_out(float v, bool f16) { return f16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+
+// PAIR: two CTAs compute 256 channels x up to 256 rows of x; else one CTA 128 x up to 128.
+template <int FMT, bool PAIR, bool SPLIT>
 struct Shape {
-    static constexpr int SB = scale_bytes(FMT), HALVES = BN / 128;
-    static constexpr int STAGE = CODE_BYTES + SB + HALVES * (CODE_BYTES + SB);
-    static constexpr int STAGES = BN == 256 ? 4 : 6;
-    static constexpr int ACCS = BN == 256 ? 1 : 2;             // accumulators: while one is read the next tile fills the other
-    static constexpr int ATOMS = SB / 512;                     // scale pieces of a row block and stage
-    static constexpr int SF_COLS = ATOMS * 4 * (1 + HALVES);   // scale columns of a stage; each stage has its own
+    static constexpr int BN = PAIR ? 256 : 128, CTAS = PAIR ? 2 : 1;
+    static constexpr int SB = scale_bytes(FMT), BLOCKS = PAIR ? 2 : 1;   // row blocks of x that a tile may touch
+    static constexpr int A_BYTES = CODE_BYTES + SB, B_BYTES = CODE_BYTES;   // codes of x in this CTA: half of a pair's
+    static constexpr int STAGE = A_BYTES + B_BYTES + BLOCKS * SB;
+    static constexpr int STAGES = !PAIR && SPLIT ? 6 : 5;
+    static constexpr int ACCS = PAIR ? 1 : 2;                    // accumulators: while one is read the next tile fills the other
+    static constexpr int ATOMS = SB / 512;                       // scale pieces of a row block and stage
+    static constexpr int SF_COLS = ATOMS * 4 * (1 + BLOCKS);     // scale columns of a stage; each stage has its own
     static constexpr int SF0 = ACCS * BN;
+    static constexpr int PITCH = 272;                            // bytes of a row of the staged output: 128 channels and a gap against bank conflicts
+    static constexpr int OUT_ROWS = 64, OUT_BYTES = SPLIT ? 0 : OUT_ROWS * PITCH;
     static_assert(SF0 + STAGES * SF_COLS <= 512, "tensor memory");
-    static constexpr size_t smem(int E, bool routed) { return 1024 + (size_t)STAGES * STAGE + 256 + (routed ? 3 * (size_t)(E + 1) * 4 : 0); }
+    static constexpr size_t smem(int E, bool routed) { return (size_t)STAGES * STAGE + OUT_BYTES + 256 + (routed ? 3 * (size_t)(E + 1) * 4 : 0); }
+    static_assert(STAGES * STAGE + OUT_BYTES + 256 + 12 * (MAX_EXPERTS + 1) <= 232448, "shared memory");
 };
 
-struct Item { int e, nb, row0, rows, xblk; int64_t yrow; };   // matrix, row block, first row inside the group, rows, row block of x, row of y
+// the MMAs issued so far arrive on this barrier in both CTAs of the pair (cluster ranks r & ~1 and the next) when they have completed
+__device__ __forceinline__ void commit_to_pair(uint64_t *bar, int cluster_rank) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(tc::smem_u32(bar)), "h"((uint16_t)(3 << (cluster_rank & ~1))) : "memory");
+}
+// a bounded wait of a whole warp, whose answer all lanes share
+__device__ __forceinline__ bool uniform_wait(uint64_t *bar, uint32_t parity, int *status, int code, volatile int *dead) {
+    if (__all_sync(~0u, tc::mbar_try_wait(bar, parity))) return true;
+    return __all_sync(~0u, tc::mbar_wait(bar, parity, status, code, tc::WAIT_LIMIT_CYCLES, dead));
+}
+// the eight warps that write y: a barrier, and whether any thread brings a true (what one of them decides alone would leave the others waiting)
+__device__ __forceinline__ bool epilogue_any(bool v) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)v) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+struct Item { int e, nb, row0, rows, xblk, off; int64_t yrow; };   // matrix; row block (pair of them); rows of the tile; first row block of x and row in it; row of y
 
 // The idx-th output tile.  Token tiles run fastest within a band of them, so that the CTAs that work at the same time share the
 // weights of few row blocks and the activations of one band; both then come from L2.
-template <int BN>
+template <bool PAIR>
 __device__ __forceinline__ Item item_of(const GemmArgs &p, int idx, const int *s_off, const int *s_blk, const int *s_item) {
     Item t;
     int rows = p.M, tiles = p.token_tiles, first_blk = 0;
@@ -78,56 +126,64 @@ __device__ __forceinline__ Item item_of(const GemmArgs &p, int idx, const int *s
         first_row = s_off[t.e];
         rows = s_off[t.e + 1] - s_off[t.e];
         first_blk = s_blk[t.e];
-        tiles = (rows + BN - 1) / BN;
+        tiles = (rows + p.bt - 1) / p.bt;
     }
-    const int per_band = p.NB * p.band, g = idx / per_band, rem = idx - g * per_band;
+    const int nbu = PAIR ? (p.NB + 1) >> 1 : p.NB;
+    const int per_band = nbu * p.band, g = idx / per_band, rem = idx - g * per_band;
     const int wide = min(p.band, tiles - g * p.band);
     t.nb = rem / wide;
     const int tt = g * p.band + rem - t.nb * wide;
-    t.row0 = tt * BN;
-    t.rows = min(BN, rows - t.row0);
-    t.xblk = first_blk + tt * (BN / 128);
+    t.row0 = tt * p.bt;
+    t.rows = min(p.bt, rows - t.row0);
+    t.xblk = first_blk + t.row0 / ROWS;
+    t.off = t.row0 % ROWS;
     t.yrow = first_row + t.row0;
     return t;
 }
+template <bool PAIR> __device__ __forceinline__ int columns_of(int rows) { return PAIR ? (rows + 31) & ~31 : (rows + 15) & ~15; }
 
-// Warp 0 brings tiles (bulk copies), warp 1 issues the MMAs, warps 2 to 5 write y.
-// SPLIT: the CTAs of a cluster share one output tile, each a run of its k tiles; the partial sums meet in the shared memory of the
-// cluster, where rank r adds the channels 128 / S r .. in the order of the ranks.  One tile a CTA then; else CTAs take tiles in turn.
-template <int FMT, int BN, bool SPLIT>
-__global__ void __launch_bounds__(192, 1) fp4_gemm_kernel(const GemmArgs p, int S, int64_t n_items) {
-    using SH = Shape<FMT, BN>;
-    constexpr int ST = SH::STAGES, SB = SH::SB, ACCS = SH::ACCS;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t *full = reinterpret_cast<uint64_t *>(ring + ST * SH::STAGE), *empty = full + ST, *acc_full = empty + ST, *acc_empty = acc_full + ACCS;
+// Warps 0 and 2 bring tiles (bulk copies: 0 those of W, 2 those of x), warp 1 issues the MMAs (in the second CTA of a pair it tells the first
+// that its tiles are there), warp 3 reads the offsets of routed rows, warps 4 to 11 write y.
+// SPLIT: S CTAs (pairs) of a cluster share one output tile, each a run of its k tiles; the partial sums meet in the shared memory of the
+// cluster, where each of the S CTAs that hold the same 128 channels adds 128 / S of them in the order of the runs.  One tile a CTA
+// then; else CTAs (pairs) take tiles in turn.
+template <int FMT, bool PAIR, bool SPLIT>
+__global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int S, int64_t n_items) {
+    using SH = Shape<FMT, PAIR, SPLIT>;
+    constexpr int ST = SH::STAGES, SB = SH::SB, ACCS = SH::ACCS, BN = SH::BN, CTAS = SH::CTAS;
+    constexpr uint32_t TMEM = 0;   // a CTA takes all of tensor memory: its first column is column 0
+    extern __shared__ __align__(1024) uint8_t ring[];   // the swizzle counts address bits from 1024 on
+    uint8_t *staged = ring + ST * SH::STAGE;
+    uint64_t *full = reinterpret_cast<uint64_t *>(staged + SH::OUT_BYTES), *empty = full + ST, *acc_full = empty + ST, *acc_empty = acc_full + ACCS;
     uint64_t *drained = acc_empty + ACCS;
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(drained + 1);
     volatile int *dead = reinterpret_cast<volatile int *>(s_tmem + 1);
-    int *s_off = reinterpret_cast<int *>(ring + ST * SH::STAGE + 256), *s_blk = s_off + p.E + 1, *s_item = s_blk + p.E + 1;
+    int *s_off = reinterpret_cast<int *>(staged + SH::OUT_BYTES + 256), *s_blk = s_off + p.E + 1, *s_item = s_blk + p.E + 1;
     static_assert((2 * ST + 2 * ACCS + 1) * 8 + 8 <= 256, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = SPLIT ? (int)tc::cluster_rank() : 0;
+    const int cluster_rank = PAIR || SPLIT ? (int)tc::cluster_rank() : 0;
+    const int half = PAIR ? cluster_rank & 1 : 0, run = cluster_rank / CTAS;   // which 128 channels of the pair; which run of k
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < ST; ++i) { tc::mbar_init(&full[i], 1); tc::mbar_init(&empty[i], 1); }
-        for (int i = 0; i < ACCS; ++i) { tc::mbar_init(&acc_full[i], 1); tc::mbar_init(&acc_empty[i], 4); }
+        for (int i = 0; i < ST; ++i) { tc::mbar_init(&full[i], PAIR && half == 0 ? 3 : 2); tc::mbar_init(&empty[i], 1); }   // a pair's first CTA also waits for the other's tiles
+        for (int i = 0; i < ACCS; ++i) { tc::mbar_init(&acc_full[i], 1); tc::mbar_init(&acc_empty[i], 8 * CTAS); }
         tc::mbar_init(drained, 1);
         *dead = 0;
         tc::fence_barrier_init();
     }
     if (warp == 1) {
-        tc::tmem_alloc(s_tmem, 512);
-        tc::tmem_relinquish();
+        if (PAIR) tc::tmem_alloc_pair(s_tmem, 512);
+        else { tc::tmem_alloc(s_tmem, 512); tc::tmem_relinquish(); }
     }
     tc::wait_for_previous_kernel();
-    if (p.offset && warp == 2) {
+    if (p.offset && warp == 3) {
         scan_groups(p.offset, p.E, p.M, s_off, s_blk);
         __syncwarp();
+        const int nbu = PAIR ? (p.NB + 1) >> 1 : p.NB;
         int sum = 0;   // tiles in front of each group
         for (int e0 = 0; e0 <= p.E; e0 += 32) {
             const int e = e0 + lane;
-            int v = e > 0 && e <= p.E ? p.NB * ((s_off[e] - s_off[e - 1] + BN - 1) / BN) : 0;
+            int v = e > 0 && e <= p.E ? nbu * ((s_off[e] - s_off[e - 1] + p.bt - 1) / p.bt) : 0;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int u = __shfl_up_sync(~0u, v, d);
@@ -140,168 +196,235 @@ __global__ void __launch_bounds__(192, 1) fp4_gemm_kernel(const GemmArgs p, int 
     }
     tc::tc_fence_before();
     __syncthreads();
+    if (PAIR) tc::cluster_sync();   // the partner's barriers exist before anything arrives on them
     tc::tc_fence_after();
-    const uint32_t tmem = *s_tmem;
     const int items = p.offset ? s_item[p.E] : (int)n_items;
-    const int first = SPLIT ? (int)(blockIdx.x / S) : (int)blockIdx.x, stride = SPLIT ? items : (int)gridDim.x;   // split: one tile
-    // this CTA's k tiles
-    const int k0 = SPLIT ? (int)((int64_t)p.KT * rank / S) : 0, k1 = SPLIT ? (int)((int64_t)p.KT * (rank + 1) / S) : p.KT;
+    const int unit = (int)(blockIdx.x / (CTAS * (SPLIT ? S : 1))), units = (int)(gridDim.x / (CTAS * (SPLIT ? S : 1)));
+    const int stride = SPLIT ? items : units;   // split: one tile
+    const int k0 = SPLIT ? (int)((int64_t)p.KT * run / S) : 0, k1 = SPLIT ? (int)((int64_t)p.KT * (run + 1) / S) : p.KT;   // this CTA's k tiles
 
-    int it = 0;   // stages filled (warp 0) or used (warp 1) so far
-    if (warp == 0) {
-        if (lane == 0) {
-            for (int idx = first; idx < items && !*dead; idx += stride) {
-                const Item t = item_of<BN>(p, idx, s_off, s_blk, s_item);
-                const int n = (t.rows + 15) & ~15;
-                const uint8_t *wt = p.w + ((int64_t)(t.e * (int64_t)p.NB + t.nb) * p.KT + k0) * tile_bytes(FMT);
-                const uint8_t *xt = p.x + ((int64_t)t.xblk * p.KT + k0) * tile_bytes(FMT);
-                const int64_t next_block = (int64_t)p.KT * tile_bytes(FMT);
-                const int n0 = n < 128 ? n : 128, n1 = n - n0;
-                const uint32_t bytes = tile_bytes(FMT) + (uint32_t)n * 128 + SB + (n1 ? SB : 0);
-                for (int kt = k0; kt < k1; ++kt, ++it, wt += tile_bytes(FMT), xt += tile_bytes(FMT)) {
-                    const int s = it % ST;
-                    if (it >= ST && !tc::mbar_wait(&empty[s], (it / ST - 1) & 1, p.status, 51, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead)) { *dead = 1; break; }
-                    uint8_t *a = ring + s * SH::STAGE, *b = a + CODE_BYTES + SB, *bs = b + SH::HALVES * CODE_BYTES;
-                    tc::mbar_arrive_expect_tx(&full[s], bytes);
-                    tc::bulk_load(a, wt, tile_bytes(FMT), &full[s]);
-                    tc::bulk_load(b, xt, (uint32_t)n0 * 128, &full[s]);
-                    tc::bulk_load(bs, xt + CODE_BYTES, SB, &full[s]);
-                    if (n1) {
-                        tc::bulk_load(b + CODE_BYTES, xt + next_block, (uint32_t)n1 * 128, &full[s]);
-                        tc::bulk_load(bs + SB, xt + next_block + CODE_BYTES, SB, &full[s]);
-                    }
-                }
+    int it = 0;   // stages filled (warps 0 and 2) or used (warp 1) so far
+    if (warp == 0 || warp == 2) {
+        // A lane for each piece of a stage: warp 0 the weights, warp 2 its rows of codes (from one row block or two) and the scales of all
+        // rows of the tile.  One lane issuing all of them took 530 cycles a stage, more than the tensor core; five lanes of one warp 290.
+        const int64_t block = (int64_t)p.KT * tile_bytes(FMT);   // from a row block to the next
+        uint32_t s = 0, phase = 1;
+        bool ok = true;
+        for (int idx = unit; idx < items && ok; idx += stride) {
+            const Item t = item_of<PAIR>(p, idx, s_off, s_blk, s_item);
+            const int n = columns_of<PAIR>(t.rows), mine = n / CTAS, nb = min(t.nb * CTAS + half, p.NB - 1);   // an odd last pair reads a block twice
+            const int r0 = t.off + half * mine, b0 = r0 / ROWS, in0 = r0 % ROWS, n0 = min(mine, ROWS - in0), n1 = mine - n0;
+            const bool two = t.off + n > ROWS;
+            const uint8_t *xt = p.x + ((int64_t)t.xblk * p.KT + k0) * tile_bytes(FMT), *src = xt;
+            uint32_t to = 0, bytes = 0, all = SH::A_BYTES;
+            if (warp == 0) {
+                if (lane == 0) { src = p.w + (((int64_t)t.e * p.NB + nb) * p.KT + k0) * tile_bytes(FMT); bytes = SH::A_BYTES; }
+            } else {
+                all = (uint32_t)mine * 128 + (two ? 2 * SB : SB);
+                if (lane == 0) { src = xt + b0 * block + in0 * 128; to = SH::A_BYTES; bytes = (uint32_t)n0 * 128; }
+                else if (lane == 1) { src = xt + CODE_BYTES; to = SH::A_BYTES + SH::B_BYTES; bytes = SB; }
+                else if (lane == 2) { src = xt + block + CODE_BYTES; to = SH::A_BYTES + SH::B_BYTES + SB; bytes = two ? SB : 0; }
+                else if (lane == 3) { src = xt + (b0 + 1) * block; to = SH::A_BYTES + n0 * 128; bytes = (uint32_t)n1 * 128; }
+            }
+            for (int kt = k0; kt < k1; ++kt, ++it, src += tile_bytes(FMT)) {
+                ok = uniform_wait(&empty[s], phase, p.status, 51, dead);   // the first round passes at once
+                if (!ok) break;
+                if (lane == 0) tc::mbar_arrive_expect_tx(&full[s], all);
+                __syncwarp();
+                if (bytes) tc::bulk_load(ring + s * SH::STAGE + to, src, bytes, &full[s]);
+                if (++s == ST) { s = 0; phase ^= 1; }
             }
         }
+        if (!ok && lane == 0) *dead = 1;
         __syncwarp();
     } else if (warp == 1) {
+        // The whole warp walks the loops and one lane issues: what the instructions take stays in uniform registers.
         int local = 0;
+        uint32_t s = 0, phase = 0;
         bool ok = true;
-        for (int idx = first; idx < items && ok; idx += stride, ++local) {
-            const Item t = item_of<BN>(p, idx, s_off, s_blk, s_item);
-            const int n = (t.rows + 15) & ~15, acc = local % ACCS;
-            const uint32_t d = tmem + acc * BN;
-            if (local >= ACCS) ok = tc::mbar_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 53, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
+        for (int idx = unit; idx < items && ok; idx += stride, ++local) {
+            const Item t = item_of<PAIR>(p, idx, s_off, s_blk, s_item);
+            const uint32_t n = __shfl_sync(~0u, columns_of<PAIR>(t.rows), 0), sf_row = __shfl_sync(~0u, t.off / 32, 0);
+            const int acc = local % ACCS;
+            const uint32_t d = TMEM + acc * BN, desc = idesc_fp4<FMT, PAIR>(n, 0);
+            if (half == 0 && local >= ACCS) ok = uniform_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 53, dead);
             tc::tc_fence_after();
             for (int kt = k0; kt < k1 && ok; ++kt, ++it) {
-                const int s = it % ST;
-                ok = tc::mbar_wait(&full[s], (it / ST) & 1, p.status, 54, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
+                ok = uniform_wait(&full[s], phase, p.status, 54, dead);
                 if (!ok) break;
-                tc::tc_fence_after();
-                const uint32_t a = tc::smem_u32(ring + s * SH::STAGE), b = a + CODE_BYTES + SB, bs = b + SH::HALVES * CODE_BYTES;
-                const uint32_t sfa = tmem + SH::SF0 + s * SH::SF_COLS, sfb = sfa + SH::ATOMS * 4;
-                const int steps = min(4, p.steps - 4 * kt);
-                if (tc::elect_one()) {
-                    const uint64_t da = tc::smem_desc_sw128(a), db = tc::smem_desc_sw128(b);
-                    const uint64_t dsa = smem_desc_plain(a + CODE_BYTES), dsb = smem_desc_plain(bs);
+                if (PAIR && half == 1) {
+                    if (lane == 0) tc::mbar_arrive_cluster(tc::map_to_rank(&full[s], cluster_rank & ~1));
+                } else {
+                    tc::tc_fence_after();
+                    const uint32_t a = tc::smem_u32(ring) + s * SH::STAGE, sfa = TMEM + SH::SF0 + s * SH::SF_COLS, sfb = sfa + SH::ATOMS * 4, sfn = sfb + sf_row;
+                    const uint64_t da = tc::smem_desc_sw128(a), db = da + SH::A_BYTES / 16, dsa = smem_desc_plain(a + CODE_BYTES), dsb = dsa + (SB + SH::B_BYTES) / 16;
+                    const int steps = p.steps - 4 * kt;
+                    if (tc::elect_one()) {
 #pragma unroll
-                    for (int j = 0; j < SH::ATOMS; ++j) {
-                        copy_scales(sfa + j * 4, dsa + j * 32);
+                        for (int j = 0; j < SH::ATOMS; ++j) {
+                            copy_scales<PAIR>(sfa + j * 4, dsa + j * 32);
 #pragma unroll
-                        for (int h = 0; h < SH::HALVES; ++h) copy_scales(sfb + (j * SH::HALVES + h) * 4, dsb + j * 32 + h * (SB / 16));
+                            for (int h = 0; h < SH::BLOCKS; ++h) copy_scales<PAIR>(sfb + (j * SH::BLOCKS + h) * 4, dsb + j * 32 + h * (SB / 16));
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int atom = FMT == MX ? j / 2 : j;
+                            const uint32_t sf = FMT == MX ? (j & 1) * 2 : 0;
+                            if (j == 0 || j < steps)
+                                umma_fp4<FMT, PAIR>(d, da + 2 * j, db + 2 * j, desc | sf << 4 | sf << 29, sfa + atom * 4, sfn + atom * 4 * SH::BLOCKS, j > 0 || kt > k0);
+                        }
+                        if (PAIR) commit_to_pair(&empty[s], cluster_rank);
+                        else tc::umma_commit(&empty[s]);
+                        if (kt == k1 - 1) {
+                            if (PAIR) commit_to_pair(&acc_full[acc], cluster_rank);
+                            else tc::umma_commit(&acc_full[acc]);
+                        }
                     }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (j >= steps) break;
-                        const int atom = FMT == MX ? j / 2 : j;
-                        umma_fp4<FMT>(d, da + 2 * j, db + 2 * j, idesc_fp4<FMT>(n, FMT == MX ? (j & 1) * 2 : 0), sfa + atom * 4, sfb + atom * 4 * SH::HALVES, kt > k0 || j > 0);
-                    }
-                    tc::umma_commit(&empty[s]);
-                    if (kt == k1 - 1) tc::umma_commit(&acc_full[acc]);
+                    __syncwarp();
                 }
-                __syncwarp();
+                if (++s == ST) { s = 0; phase ^= 1; }
             }
         }
-        if (!ok) {   // what was issued completes before tensor memory is given back
-            if (lane == 0) *dead = 1;
-            if (tc::elect_one()) tc::umma_commit(drained);
+        if (!ok && lane == 0) *dead = 1;
+        if (!ok && half == 0) {   // what was issued completes before tensor memory is given back
+            if (tc::elect_one()) {
+                if (PAIR) commit_to_pair(drained, cluster_rank);
+                else tc::umma_commit(drained);
+            }
             __syncwarp();
             tc::mbar_wait(drained, 0, p.status, 55);
         }
-    } else {
-        const int quad = warp & 3;   // the 32 lanes of tensor memory that a warp may read
+        __syncwarp();
+    } else if (warp >= 4) {
+        // Tensor memory is emptied into registers first, already in the type of y, so that the next tile's MMAs wait for no store;
+        // then 64 rows of y at a time go through shared memory, where the 8x8 matrices are turned round, and out as whole rows.
+        const int quad = warp & 3, part = (warp - 4) >> 2;   // the 32 lanes of tensor memory that a warp may read; its half of 64 columns
         int local = 0;
-        for (int idx = first; idx < items; idx += stride, ++local) {
-            const Item t = item_of<BN>(p, idx, s_off, s_blk, s_item);
+        for (int idx = unit; idx < items; idx += stride, ++local) {
+            const Item t = item_of<PAIR>(p, idx, s_off, s_blk, s_item);
             const int acc = local % ACCS;
             const bool ok = tc::mbar_wait(&acc_full[acc], (local / ACCS) & 1, p.status, 56, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
-            if (!__all_sync(~0u, ok)) { *dead = 1; break; }
+            if (epilogue_any(!ok)) { *dead = 1; break; }
+            if constexpr (SPLIT) break;
             tc::tc_fence_after();
-            if constexpr (!SPLIT) {
-                const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
-                const int64_t ch = (int64_t)t.nb * 128 + quad * 32 + lane;
-                uint16_t *out = p.y + t.yrow * p.N + ch;
-                for (int c0 = 0; c0 < t.rows; c0 += 32) {
-                    uint32_t v[32];
-                    tc::tmem_ld32(tmem + acc * BN + c0 + ((uint32_t)(quad * 32) << 16), v);
-                    tc::tmem_ld_wait();
-                    if (ch < p.N) {
+            const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
+            const int nb = t.nb * CTAS + half;
+            uint32_t out16[BN / 64][16];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (c0 + i >= t.rows) break;
-                            const float f = __uint_as_float(v[i]) * alpha;
-                            out[(int64_t)(c0 + i) * p.N] = p.f16 ? __half_as_ushort(__float2half_rn(f)) : __bfloat16_as_ushort(__float2bfloat16_rn(f));
-                        }
+            for (int g = 0; g < BN / 64; ++g) {
+                if (g * 64 + part * 32 < t.rows) {
+                    uint32_t lo[16], hi[16];
+                    const uint32_t from = TMEM + acc * BN + g * 64 + part * 32 + ((uint32_t)(quad * 32) << 16);
+                    tmem_ld_16x32(from, lo);
+                    tmem_ld_16x32(from + (16u << 16), hi);
+                    tc::tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        out16[g][4 * i] = pack_out(lo[4 * i], lo[4 * i + 1], alpha, p.f16);
+                        out16[g][4 * i + 1] = pack_out(lo[4 * i + 2], lo[4 * i + 3], alpha, p.f16);
+                        out16[g][4 * i + 2] = pack_out(hi[4 * i], hi[4 * i + 1], alpha, p.f16);
+                        out16[g][4 * i + 3] = pack_out(hi[4 * i + 2], hi[4 * i + 3], alpha, p.f16);
                     }
                 }
-                tc::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&acc_empty[acc]);
+            }
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR && half == 1) tc::mbar_arrive_cluster(tc::map_to_rank(&acc_empty[acc], cluster_rank & ~1));
+                else tc::mbar_arrive(&acc_empty[acc]);
+            }
+            const int chans = (int)min((int64_t)128, p.N - (int64_t)nb * 128);   // none or fewer in a last block without a partner
+            const int tid = threadIdx.x - 128;
+            const uint32_t at = tc::smem_u32(staged) + (part * 32 + (lane & 7)) * SH::PITCH + quad * 64 + (lane >> 3) * 16;
+#pragma unroll
+            for (int g = 0; g < BN / 64; ++g) {
+                if (g * 64 >= t.rows) break;
+                if (g * 64 + part * 32 < t.rows) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) stmatrix_trans(at + 8 * i * SH::PITCH, out16[g][4 * i], out16[g][4 * i + 1], out16[g][4 * i + 2], out16[g][4 * i + 3]);
+                }
+                epilogue_sync();
+                const int count = min(64, t.rows - g * 64);
+                uint16_t *out = p.y + (t.yrow + g * 64) * p.N + (int64_t)nb * 128;
+                if (p.wide) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {   // sixteen threads a row
+                        const int r = i * 16 + (tid >> 4), c = (tid & 15) * 8;
+                        if (r < count && c < chans) *reinterpret_cast<uint4 *>(out + (int64_t)r * p.N + c) = *reinterpret_cast<const uint4 *>(staged + r * SH::PITCH + c * 2);
+                    }
+                } else {
+                    for (int r = warp - 4; r < count; r += 8)
+                        for (int c = lane; c < chans; c += 32) out[(int64_t)r * p.N + c] = *reinterpret_cast<const uint16_t *>(staged + r * SH::PITCH + c * 2);
+                }
+                epilogue_sync();   // read before it is written again
             }
         }
     }
 
     if constexpr (SPLIT) {
         // every CTA's MMAs are done (the warps that read tensor memory waited for them), so the rings are free for partial sums
-        const Item t = item_of<BN>(p, first, s_off, s_blk, s_item);
-        const int CW = 128 / S, n = (t.rows + 15) & ~15;
+        const Item t = item_of<PAIR>(p, unit, s_off, s_blk, s_item);
+        const int CW = 128 / S, pitch = columns_of<PAIR>(t.rows) + 4;
         __syncthreads();
         tc::cluster_sync();
         const bool alive = !*dead;
-        float *part = reinterpret_cast<float *>(ring);   // [rank that sent it][token][channel of mine]
-        if (warp >= 2 && alive) {
+        float *part = reinterpret_cast<float *>(ring);   // [run that sent it][channel of mine][row of x]
+        if (warp >= 4 && alive) {
+            tc::tc_fence_after();
             const int quad = warp & 3, c = quad * 32 + lane, owner = c / CW;
-            const uint32_t to = tc::map_to_rank(part, owner) + (uint32_t)((rank * n) * CW + c % CW) * 4;
-            for (int c0 = 0; c0 < t.rows; c0 += 32) {
+            const uint32_t to = tc::map_to_rank(part, owner * CTAS + half) + (uint32_t)(run * CW + c - owner * CW) * pitch * 4;
+            for (int c0 = (warp - 4) / 4 * 32; c0 < t.rows; c0 += 64) {
                 uint32_t v[32];
-                tc::tmem_ld32(tmem + c0 + ((uint32_t)(quad * 32) << 16), v);
+                tc::tmem_ld32(TMEM + c0 + ((uint32_t)(quad * 32) << 16), v);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (c0 + i < t.rows) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + (uint32_t)((c0 + i) * CW) * 4), "r"(v[i]) : "memory");
+                for (int i = 0; i < 32; i += 4)
+                    if (c0 + i < t.rows)
+                        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(c0 + i) * 4), "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]) : "memory");
             }
         }
         __syncwarp();
         tc::cluster_sync();
         if (alive) {
             const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
-            for (int i = threadIdx.x; i < t.rows * CW; i += 192) {
-                const int token = i / CW, c = i % CW;
-                const int64_t ch = (int64_t)t.nb * 128 + rank * CW + c;
-                float f = 0.0f;
-                for (int s = 0; s < S; ++s) f += part[(s * n + token) * CW + c];
-                f *= alpha;
-                if (ch < p.N) p.y[(t.yrow + token) * p.N + ch] = p.f16 ? __half_as_ushort(__float2half_rn(f)) : __bfloat16_as_ushort(__float2bfloat16_rn(f));
+            const int c = threadIdx.x % CW;   // CW a power of two
+            const int64_t ch = (int64_t)(t.nb * CTAS + half) * 128 + run * CW + c;
+            const float *mine = part + c * pitch;
+            uint16_t *out = p.y + t.yrow * p.N + ch;
+            for (int r = threadIdx.x / CW * 4; r < t.rows; r += 384 / CW * 4) {
+                float4 f = *reinterpret_cast<const float4 *>(mine + r);
+                for (int s = 1; s < S; ++s) {
+                    const float4 v = *reinterpret_cast<const float4 *>(mine + (int64_t)s * CW * pitch + r);
+                    f.x += v.x; f.y += v.y; f.z += v.z; f.w += v.w;
+                }
+                if (ch < p.N) {
+                    out[(int64_t)r * p.N] = round_out(f.x * alpha, p.f16);
+                    if (r + 1 < t.rows) out[(int64_t)(r + 1) * p.N] = round_out(f.y * alpha, p.f16);
+                    if (r + 2 < t.rows) out[(int64_t)(r + 2) * p.N] = round_out(f.z * alpha, p.f16);
+                    if (r + 3 < t.rows) out[(int64_t)(r + 3) * p.N] = round_out(f.w * alpha, p.f16);
+                }
             }
         }
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (*dead && threadIdx.x == 0)   // a wait gave up: copies in flight land before the shared memory goes away
+    if (*dead && (warp == 0 || warp == 2))   // a wait gave up: copies in flight land before the shared memory goes away
         for (int i = it < ST ? 0 : it - ST; i < it; ++i) tc::mbar_wait(&full[i % ST], (i / ST) & 1, p.status, 52);
+    if (PAIR) { __syncwarp(); tc::cluster_sync(); }   // nothing of the pair is in flight towards a CTA that has left
     if (warp == 1) {
         tc::tc_fence_after();
-        tc::tmem_dealloc(tmem, 512);
+        if (PAIR) tc::tmem_dealloc_pair(TMEM, 512);
+        else tc::tmem_dealloc(TMEM, 512);
     }
 }
 
-template <int FMT, int BN, bool SPLIT>
+template <int FMT, bool PAIR, bool SPLIT>
 static cudaError_t launch(const GemmArgs &p, int S, int64_t items, unsigned grid, cudaStream_t st) {
+    using SH = Shape<FMT, PAIR, SPLIT>;
     static std::atomic<uint64_t> done{0};
-    const size_t smem = Shape<FMT, BN>::smem(p.E, p.offset != nullptr);
-    const cudaError_t e = ensure_func_attr(fp4_gemm_kernel<FMT, BN, SPLIT>, done, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<FMT, BN>::smem(MAX_EXPERTS, true));
+    const cudaError_t e = ensure_func_attr(fp4_gemm_kernel<FMT, PAIR, SPLIT>, done, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SH::smem(MAX_EXPERTS, true));
     if (e != cudaSuccess) return e;
-    return launch_overlapped(fp4_gemm_kernel<FMT, BN, SPLIT>, dim3(grid), 192u, smem, st, SPLIT ? S : 1, true, p, S, items);
+    return launch_overlapped(fp4_gemm_kernel<FMT, PAIR, SPLIT>, dim3(grid), 384u, SH::smem(p.E, p.offset != nullptr), st, SH::CTAS * (SPLIT ? S : 1), true, p, S, items);
 }
 
 }  // namespace fp4
@@ -313,21 +436,21 @@ cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, 
     GemmArgs p{};
     p.w = (const uint8_t *)w; p.x = (const uint8_t *)x; p.w_scale = w_scale; p.x_scale = x_scale; p.offset = offset; p.y = y; p.status = status;
     p.E = E; p.NB = (int)((N + 127) / 128); p.KT = (int)((K + KB - 1) / KB); p.steps = (int)((K + 63) / 64);
-    p.M = (int)M; p.N = N; p.f16 = f16;
-    const int64_t sms = sm_count();
-    int S = 1, BN = (offset ? M / E : M) > 128 ? 256 : 128;
-    if (!offset && M <= 256) {
-        BN = M > 128 ? 256 : 128;
-        while (S < 8 && 2 * S <= p.KT && 2 * S * p.NB <= sms) S *= 2;
-    }
-    p.token_tiles = (int)((M + BN - 1) / BN);
+    p.M = (int)M; p.N = N; p.f16 = f16; p.wide = N % 8 == 0;
+    const int sms = sm_count();
+    int S = 1, pair = (offset ? M / E : M) > 256, bt = pair ? 256 : 128;
+    if (!offset && M <= 256)
+        while (S < 4 && 2 * S <= p.KT && 2 * S * p.NB * ((M + 127) / 128) <= sms) S *= 2;
+    p.bt = bt;
+    p.token_tiles = (int)((M + bt - 1) / bt);
     p.band = 16;
-    const int64_t items = (int64_t)p.NB * p.token_tiles;
-    const unsigned grid = S > 1 ? (unsigned)(items * S) : (unsigned)(offset ? sms : items < sms ? items : sms);
+    const int ctas = pair ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sms / ctas;
+    const int64_t items = (int64_t)nbu * p.token_tiles;
+    const unsigned grid = (unsigned)(S > 1 ? items * S : offset ? places : items < places ? items : places) * ctas;
     auto go = [&](auto f) {
         constexpr int F = decltype(f)::value;
-        if (S > 1) return BN == 256 ? launch<F, 256, true>(p, S, items, grid, st) : launch<F, 128, true>(p, S, items, grid, st);
-        return BN == 256 ? launch<F, 256, false>(p, 1, items, grid, st) : launch<F, 128, false>(p, 1, items, grid, st);
+        if (S > 1) return pair ? launch<F, true, true>(p, S, items, grid, st) : launch<F, false, true>(p, S, items, grid, st);
+        return pair ? launch<F, true, false>(p, 1, items, grid, st) : launch<F, false, false>(p, 1, items, grid, st);
     };
     return fmt == MX ? go(std::integral_constant<int, MX>{}) : go(std::integral_constant<int, NV>{});
 }
