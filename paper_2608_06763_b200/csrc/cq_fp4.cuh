@@ -104,29 +104,103 @@ __device__ __forceinline__ float from_e4m3(uint32_t b) {
 __device__ __forceinline__ float from_e8m0(uint32_t b) {
     return __uint_as_float(b == 255u ? 0x7FFFFFFFu : b == 0u ? 0x00400000u : b << 23);
 }
-// the magnitude of a code is 2 x + ... : read off a word of half values in 4-bit fields would cost more than this
-__device__ __forceinline__ float from_e2m1(uint32_t c) {
-    const uint32_t m = c & 7u;
-    const float v = m < 2u ? 0.5f * (float)m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
-    return (c & 8u) ? -v : v;
+// eight codes to values, exactly (the conversion goes through binary16, which holds them all)
+__device__ __forceinline__ void from_e2m1x8(uint32_t c, float *v) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(c));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
+        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
 }
 
 // The scale byte of a block, and the factor its values are multiplied by before they are rounded to codes.  top: bits of the largest
-// |x| (a NaN or an infinity makes the scale NaN); r = 1 / g (NVFP4).
+// |x| (a NaN or an infinity makes the scale NaN and the factor 0).  NVFP4: r = 1 / g, factors: r / scale by scale byte (null: divided here).
 template <int FMT>
-__device__ __forceinline__ uint32_t block_scale(uint32_t top, float r, float &factor) {
+__device__ __forceinline__ uint32_t block_scale(uint32_t top, float r, const float *factors, float &factor) {
     if (FMT == MX) {
-        const uint32_t b = (top >> 23) > 2u ? (top >> 23) - 2u : 0u;   // floor(log2 top) - 2, not below -127
+        uint32_t b = (top >> 23) > 2u ? (top >> 23) - 2u : 0u;   // floor(log2 top) - 2, not below -127
         factor = __uint_as_float((254u - b) << 23);
-        if (top >= 0x7F800000u) { factor = 0.0f; return 255u; }
+        if (top >= 0x7F800000u) { factor = 0.0f; b = 255u; }
         return b;
     }
     // 2^-9 is the least scale that e4m3 has: a block of zeros or of less than that keeps a scale to be divided by
     const float s = fminf(fmaxf(__fdiv_rn(__fmul_rn(__uint_as_float(top), r), 6.0f), 0.001953125f), 448.0f);
-    const uint32_t b = to_e4m3(s);
-    factor = __fdiv_rn(r, from_e4m3(b));
-    if (top >= 0x7F800000u) { factor = 0.0f; return 127u; }
+    const uint32_t b = top >= 0x7F800000u ? 127u : to_e4m3(s);
+    factor = factors ? factors[b] : b == 127u ? 0.0f : __fdiv_rn(r, from_e4m3(b));
     return b;
+}
+
+// ---------------------------------------------------------------- two fp32 operations an instruction, each rounded by itself
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair_of(float a, float b) { Pair r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpair(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// ---------------------------------------------------------------- sixteen values of a row
+__device__ __forceinline__ uint4 load16(const void *p) { return *reinterpret_cast<const uint4 *>(p); }
+template <int DT>
+__device__ __forceinline__ float value_of(const uint32_t *w, int i) {
+    const uint32_t h = (i & 1) ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu;
+    return DT == DT_BF16 ? __uint_as_float(h << 16) : __half2float(__ushort_as_half((unsigned short)h));
+}
+// bits of the largest magnitude of sixteen 16-bit values; NaN counts as the largest
+template <int DT>
+__device__ __forceinline__ uint32_t top_of_16bit(const uint32_t *w) {
+    if (DT == DT_BF16) {
+        __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[0]));
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i])));
+        const uint32_t b = *reinterpret_cast<uint32_t *>(&m) & 0x7FFF7FFFu;
+        return max(b << 16, b & 0xFFFF0000u);
+    }
+    __half2 m = __habs2(*reinterpret_cast<const __half2 *>(&w[0]));
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __half2 *>(&w[i])));
+    return max(__float_as_uint(__low2float(m)) & 0x7FFFFFFFu, __float_as_uint(__high2float(m)) & 0x7FFFFFFFu);
+}
+
+template <int FMT>
+__device__ __forceinline__ uint32_t top_of_block(uint32_t top) {   // MXFP4: two threads hold a block
+    return FMT == MX ? max(top, __shfl_xor_sync(~0u, top, 1)) : top;
+}
+__device__ __forceinline__ uint2 round_codes(const float *v, float factor) {
+    float u[16];
+    const Pair f = pair_of(factor, factor);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) unpair(mul2(pair_of(v[i], v[i + 1]), f), u[i], u[i + 1]);
+    return make_uint2(to_e2m1x8(u), to_e2m1x8(u + 8));
+}
+// Four scales of a row, held by neighbouring lanes (a scale of MXFP4 by two), as they lie in memory.  All lanes take part.
+template <int FMT>
+__device__ __forceinline__ uint32_t gather_scales(uint32_t scale) {
+    const int lane = threadIdx.x & 31;
+    uint32_t word;
+    if (FMT == NV) {
+        word = scale << (8 * (lane & 3));
+        word |= __shfl_xor_sync(~0u, word, 1);
+        word |= __shfl_xor_sync(~0u, word, 2);
+    } else {
+        word = scale << (8 * ((lane >> 1) & 3));
+        word |= __shfl_xor_sync(~0u, word, 2);
+        word |= __shfl_xor_sync(~0u, word, 4);
+    }
+    return word;
+}
+// Sixteen values of a row in a model dtype to codes and the scale of their block; r = 1 / g.  All lanes take part.
+template <int FMT, int DT>
+__device__ __forceinline__ uint2 quantize_unit(const uint4 &a, const uint4 &b, float r, uint32_t &scale) {
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float v[16], factor;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = value_of<DT>(w, k);
+    scale = block_scale<FMT>(top_of_block<FMT>(top_of_16bit<DT>(w)), r, nullptr, factor);
+    return factor == 0.0f ? make_uint2(0, 0) : round_codes(v, factor);
 }
 
 }  // namespace fp4

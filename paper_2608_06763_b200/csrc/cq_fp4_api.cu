@@ -72,6 +72,8 @@ int product(const void *w, const float *w_scale, const void *x, int64_t ldx, int
     CQ_TRY(check_arch());
     cudaStream_t st = (cudaStream_t)stream;
     uint8_t *ws = (uint8_t *)workspace;
+    if (!quantised && !routed && fp4_few_ok(M, N, K))
+        return wrap(launch_fp4_few(w, w_scale, (const uint16_t *)x, ldx, x_scale, fmt, y, M, N, K, act_f16 != 0, (int *)ws, st));
     if (!quantised) {
         const Fp4Rows rows = routed ? Fp4Rows{route_token, offset, (int)E, M, M, T} : dense(1, M);
         CQ_TRY(wrap(launch_fp4_quantize(x, dtype, ldx, rows, fmt, K, x_scale, ws + STATUS_BYTES, st)));

@@ -20,7 +20,14 @@ struct GemmArgs {
     int M;                   // rows of x
     int64_t N;
     bool f16, wide;          // wide: rows of y start on 16-byte boundaries
+    const uint16_t *xr;      // FEW: rows of x in the model dtype, ldx apart
+    int64_t ldx, K;
 };
+
+// What a CTA computes.  ONE: 128 channels x up to 128 rows of x; TWO: a pair of CTAs 256 channels x up to 256 rows; FEW: 128 channels x up to 16
+// rows, which it quantises itself and keeps in shared memory.
+enum { ONE = 0, TWO = 1, FEW = 2 };
+constexpr int FEW_ROWS = 16, FEW_TILES = 16, FEW_MOST = 64;   // rows, and k tiles of them, that fit beside the ring
 
 // D[tmem] (+)= A B, codes by shared-memory descriptors, scales in tensor memory.  PAIR: by the tensor cores of two SMs, each with 128 of
 // the 256 rows of A and half of the columns of B in its shared memory.
@@ -73,23 +80,24 @@ __device__ __forceinline__ uint32_t pack_out(uint32_t lo, uint32_t hi, float alp
 }
 __device__ __forceinline__ uint16_t round_out(float v, bool f16) { return f16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
-// PAIR: two CTAs compute 256 channels x up to 256 rows of x; else one CTA 128 x up to 128.
-template <int FMT, bool PAIR, bool SPLIT>
+template <int FMT, int MODE, bool SPLIT>
 struct Shape {
-    static constexpr int BN = PAIR ? 256 : 128, CTAS = PAIR ? 2 : 1;
-    static constexpr int SB = scale_bytes(FMT), BLOCKS = PAIR ? 2 : 1;   // row blocks of x that a tile may touch
+    static constexpr bool PAIR = MODE == TWO;
+    static constexpr int BN = MODE == TWO ? 256 : MODE == ONE ? 128 : FEW_ROWS, CTAS = PAIR ? 2 : 1;
+    static constexpr int SB = scale_bytes(FMT), BLOCKS = PAIR ? 2 : 1;      // row blocks of x that a tile may touch
     static constexpr int A_BYTES = CODE_BYTES + SB, B_BYTES = CODE_BYTES;   // codes of x in this CTA: half of a pair's
-    static constexpr int STAGE = A_BYTES + B_BYTES + BLOCKS * SB;
-    static constexpr int STAGES = !PAIR && SPLIT ? 6 : 5;
-    static constexpr int ACCS = PAIR ? 1 : 2;                    // accumulators: while one is read the next tile fills the other
+    static constexpr int STAGE = A_BYTES + (MODE == FEW ? 0 : B_BYTES + BLOCKS * SB);
+    static constexpr int STAGES = MODE == FEW ? 8 : MODE == ONE && SPLIT ? 6 : 5;
+    static constexpr int ACCS = PAIR ? 1 : 2, ACC_COLS = BN < 32 ? 32 : BN;   // accumulators: while one is read the next tile fills the other
     static constexpr int ATOMS = SB / 512;                       // scale pieces of a row block and stage
     static constexpr int SF_COLS = ATOMS * 4 * (1 + BLOCKS);     // scale columns of a stage; each stage has its own
-    static constexpr int SF0 = ACCS * BN;
+    static constexpr int SF0 = ACCS * ACC_COLS;
     static constexpr int PITCH = 272;                            // bytes of a row of the staged output: 128 channels and a gap against bank conflicts
-    static constexpr int OUT_ROWS = 64, OUT_BYTES = SPLIT ? 0 : OUT_ROWS * PITCH;
+    static constexpr int X_CODES = FEW_ROWS * 128, X_BYTES = MODE == FEW ? FEW_TILES * (X_CODES + SB) : 0;   // FEW: codes of a k tile; all k tiles
+    static constexpr int OUT_BYTES = SPLIT ? 0 : (MODE == FEW ? 32 : 64) * PITCH;
     static_assert(SF0 + STAGES * SF_COLS <= 512, "tensor memory");
-    static constexpr size_t smem(int E, bool routed) { return (size_t)STAGES * STAGE + OUT_BYTES + 256 + (routed ? 3 * (size_t)(E + 1) * 4 : 0); }
-    static_assert(STAGES * STAGE + OUT_BYTES + 256 + 12 * (MAX_EXPERTS + 1) <= 232448, "shared memory");
+    static constexpr size_t smem(int E, bool routed) { return (size_t)STAGES * STAGE + X_BYTES + OUT_BYTES + 256 + (routed ? 3 * (size_t)(E + 1) * 4 : 0); }
+    static_assert(STAGES * STAGE + X_BYTES + OUT_BYTES + 256 + (MODE == FEW ? 0 : 12 * (MAX_EXPERTS + 1)) <= 232448, "shared memory");
 };
 
 // the MMAs issued so far arrive on this barrier in both CTAs of the pair (cluster ranks r & ~1 and the next) when they have completed
@@ -110,15 +118,14 @@ __device__ __forceinline__ bool epilogue_any(bool v) {
 }
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-struct Item { int e, nb, row0, rows, xblk, off; int64_t yrow; };   // matrix; row block (pair of them); rows of the tile; first row block of x and row in it; row of y
+struct Item { int e, nb, rows, xblk, off, yrow; };   // matrix; row block (pair of them); rows of the tile; first row block of x and row in it; row of y
 
 // The idx-th output tile.  Token tiles run fastest within a band of them, so that the CTAs that work at the same time share the
 // weights of few row blocks and the activations of one band; both then come from L2.
 template <bool PAIR>
 __device__ __forceinline__ Item item_of(const GemmArgs &p, int idx, const int *s_off, const int *s_blk, const int *s_item) {
     Item t;
-    int rows = p.M, tiles = p.token_tiles, first_blk = 0;
-    int64_t first_row = 0;
+    int rows = p.M, tiles = p.token_tiles, first_blk = 0, first_row = 0;
     t.e = 0;
     if (p.offset) {
         t.e = find_group(s_item, p.E, idx);
@@ -133,13 +140,39 @@ __device__ __forceinline__ Item item_of(const GemmArgs &p, int idx, const int *s
     const int wide = min(p.band, tiles - g * p.band);
     t.nb = rem / wide;
     const int tt = g * p.band + rem - t.nb * wide;
-    t.row0 = tt * p.bt;
-    t.rows = min(p.bt, rows - t.row0);
-    t.xblk = first_blk + t.row0 / ROWS;
-    t.off = t.row0 % ROWS;
-    t.yrow = first_row + t.row0;
+    const int row0 = tt * p.bt;
+    t.rows = min(p.bt, rows - row0);
+    t.xblk = first_blk + row0 / ROWS;
+    t.off = row0 % ROWS;
+    t.yrow = first_row + row0;
     return t;
 }
+// The tiles of a CTA, unit + i * stride, as each warp goes through them: 32 at a time, a lane for each, since the divisions of one by one
+// took as long as two stages of the tensor core.
+template <bool PAIR>
+struct Tiles {
+    const GemmArgs &p;
+    const int unit, stride, items;
+    const int *s_off, *s_blk, *s_item;
+    Item mine;
+    __device__ __forceinline__ bool has(int i) const { return unit + (int64_t)i * stride < items; }
+    __device__ __forceinline__ Item at(int i) {   // i = 0, 1, 2 ..; the whole warp
+        if ((i & 31) == 0) {
+            const int64_t idx = unit + (int64_t)(i + (int)(threadIdx.x & 31)) * stride;
+            if (idx < items) mine = item_of<PAIR>(p, (int)idx, s_off, s_blk, s_item);
+            __syncwarp();
+        }
+        Item t;
+        const int packed = __shfl_sync(~0u, mine.rows << 8 | mine.off, i & 31);
+        t.e = __shfl_sync(~0u, mine.e, i & 31);
+        t.nb = __shfl_sync(~0u, mine.nb, i & 31);
+        t.xblk = __shfl_sync(~0u, mine.xblk, i & 31);
+        t.yrow = __shfl_sync(~0u, mine.yrow, i & 31);
+        t.rows = packed >> 8;
+        t.off = packed & 255;
+        return t;
+    }
+};
 template <bool PAIR> __device__ __forceinline__ int columns_of(int rows) { return PAIR ? (rows + 31) & ~31 : (rows + 15) & ~15; }
 
 // Warps 0 and 2 bring tiles (bulk copies: 0 those of W, 2 those of x), warp 1 issues the MMAs (in the second CTA of a pair it tells the first
@@ -147,27 +180,31 @@ template <bool PAIR> __device__ __forceinline__ int columns_of(int rows) { retur
 // SPLIT: S CTAs (pairs) of a cluster share one output tile, each a run of its k tiles; the partial sums meet in the shared memory of the
 // cluster, where each of the S CTAs that hold the same 128 channels adds 128 / S of them in the order of the runs.  One tile a CTA
 // then; else CTAs (pairs) take tiles in turn.
-template <int FMT, bool PAIR, bool SPLIT>
+// FEW: warps 4 to 11 first quantise the rows for this CTA's k tiles, while the first weights are on their way.
+template <int FMT, int MODE, bool SPLIT>
 __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int S, int64_t n_items) {
-    using SH = Shape<FMT, PAIR, SPLIT>;
-    constexpr int ST = SH::STAGES, SB = SH::SB, ACCS = SH::ACCS, BN = SH::BN, CTAS = SH::CTAS;
+    using SH = Shape<FMT, MODE, SPLIT>;
+    constexpr bool PAIR = SH::PAIR;
+    constexpr int ST = SH::STAGES, SB = SH::SB, ACCS = SH::ACCS, BN = SH::BN, CTAS = SH::CTAS, ACC_COLS = SH::ACC_COLS;
     constexpr uint32_t TMEM = 0;   // a CTA takes all of tensor memory: its first column is column 0
     extern __shared__ __align__(1024) uint8_t ring[];   // the swizzle counts address bits from 1024 on
-    uint8_t *staged = ring + ST * SH::STAGE;
+    uint8_t *x_codes = ring + ST * SH::STAGE, *x_scales = x_codes + FEW_TILES * SH::X_CODES;
+    uint8_t *staged = x_codes + SH::X_BYTES;
     uint64_t *full = reinterpret_cast<uint64_t *>(staged + SH::OUT_BYTES), *empty = full + ST, *acc_full = empty + ST, *acc_empty = acc_full + ACCS;
-    uint64_t *drained = acc_empty + ACCS;
-    uint32_t *s_tmem = reinterpret_cast<uint32_t *>(drained + 1);
+    uint64_t *drained = acc_empty + ACCS, *x_ready = drained + 1;
+    uint32_t *s_tmem = reinterpret_cast<uint32_t *>(x_ready + 1);
     volatile int *dead = reinterpret_cast<volatile int *>(s_tmem + 1);
     int *s_off = reinterpret_cast<int *>(staged + SH::OUT_BYTES + 256), *s_blk = s_off + p.E + 1, *s_item = s_blk + p.E + 1;
-    static_assert((2 * ST + 2 * ACCS + 1) * 8 + 8 <= 256, "barriers");
+    static_assert((2 * ST + 2 * ACCS + 2) * 8 + 8 <= 256, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cluster_rank = PAIR || SPLIT ? (int)tc::cluster_rank() : 0;
     const int half = PAIR ? cluster_rank & 1 : 0, run = cluster_rank / CTAS;   // which 128 channels of the pair; which run of k
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < ST; ++i) { tc::mbar_init(&full[i], PAIR && half == 0 ? 3 : 2); tc::mbar_init(&empty[i], 1); }   // a pair's first CTA also waits for the other's tiles
+        for (int i = 0; i < ST; ++i) { tc::mbar_init(&full[i], MODE == FEW ? 1 : PAIR && half == 0 ? 3 : 2); tc::mbar_init(&empty[i], 1); }   // a pair's first CTA also waits for the other's tiles
         for (int i = 0; i < ACCS; ++i) { tc::mbar_init(&acc_full[i], 1); tc::mbar_init(&acc_empty[i], 8 * CTAS); }
         tc::mbar_init(drained, 1);
+        tc::mbar_init(x_ready, 8);
         *dead = 0;
         tc::fence_barrier_init();
     }
@@ -203,15 +240,16 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
     const int stride = SPLIT ? items : units;   // split: one tile
     const int k0 = SPLIT ? (int)((int64_t)p.KT * run / S) : 0, k1 = SPLIT ? (int)((int64_t)p.KT * (run + 1) / S) : p.KT;   // this CTA's k tiles
 
+    Tiles<PAIR> tiles{p, unit, stride, items, s_off, s_blk, s_item, {}};
     int it = 0;   // stages filled (warps 0 and 2) or used (warp 1) so far
-    if (warp == 0 || warp == 2) {
+    if (warp == 0 || (warp == 2 && MODE != FEW)) {
         // A lane for each piece of a stage: warp 0 the weights, warp 2 its rows of codes (from one row block or two) and the scales of all
         // rows of the tile.  One lane issuing all of them took 530 cycles a stage, more than the tensor core; five lanes of one warp 290.
         const int64_t block = (int64_t)p.KT * tile_bytes(FMT);   // from a row block to the next
         uint32_t s = 0, phase = 1;
         bool ok = true;
-        for (int idx = unit; idx < items && ok; idx += stride) {
-            const Item t = item_of<PAIR>(p, idx, s_off, s_blk, s_item);
+        for (int local = 0; ok && tiles.has(local); ++local) {
+            const Item t = tiles.at(local);
             const int n = columns_of<PAIR>(t.rows), mine = n / CTAS, nb = min(t.nb * CTAS + half, p.NB - 1);   // an odd last pair reads a block twice
             const int r0 = t.off + half * mine, b0 = r0 / ROWS, in0 = r0 % ROWS, n0 = min(mine, ROWS - in0), n1 = mine - n0;
             const bool two = t.off + n > ROWS;
@@ -239,14 +277,13 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         __syncwarp();
     } else if (warp == 1) {
         // The whole warp walks the loops and one lane issues: what the instructions take stays in uniform registers.
-        int local = 0;
         uint32_t s = 0, phase = 0;
-        bool ok = true;
-        for (int idx = unit; idx < items && ok; idx += stride, ++local) {
-            const Item t = item_of<PAIR>(p, idx, s_off, s_blk, s_item);
-            const uint32_t n = __shfl_sync(~0u, columns_of<PAIR>(t.rows), 0), sf_row = __shfl_sync(~0u, t.off / 32, 0);
+        bool ok = MODE != FEW || uniform_wait(x_ready, 0, p.status, 57, dead);
+        for (int local = 0; ok && tiles.has(local); ++local) {
+            const Item t = tiles.at(local);
+            const uint32_t n = columns_of<PAIR>(t.rows), sf_row = t.off / 32;
             const int acc = local % ACCS;
-            const uint32_t d = TMEM + acc * BN, desc = idesc_fp4<FMT, PAIR>(n, 0);
+            const uint32_t d = TMEM + acc * ACC_COLS, desc = idesc_fp4<FMT, PAIR>(n, 0);
             if (half == 0 && local >= ACCS) ok = uniform_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 53, dead);
             tc::tc_fence_after();
             for (int kt = k0; kt < k1 && ok; ++kt, ++it) {
@@ -257,7 +294,9 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
                 } else {
                     tc::tc_fence_after();
                     const uint32_t a = tc::smem_u32(ring) + s * SH::STAGE, sfa = TMEM + SH::SF0 + s * SH::SF_COLS, sfb = sfa + SH::ATOMS * 4, sfn = sfb + sf_row;
-                    const uint64_t da = tc::smem_desc_sw128(a), db = da + SH::A_BYTES / 16, dsa = smem_desc_plain(a + CODE_BYTES), dsb = dsa + (SB + SH::B_BYTES) / 16;
+                    const uint64_t da = tc::smem_desc_sw128(a), dsa = smem_desc_plain(a + CODE_BYTES);
+                    const uint64_t db = MODE == FEW ? tc::smem_desc_sw128(tc::smem_u32(x_codes) + (kt - k0) * SH::X_CODES) : da + SH::A_BYTES / 16;
+                    const uint64_t dsb = MODE == FEW ? smem_desc_plain(tc::smem_u32(x_scales) + (kt - k0) * SB) : dsa + (SB + SH::B_BYTES) / 16;
                     const int steps = p.steps - 4 * kt;
                     if (tc::elect_one()) {
 #pragma unroll
@@ -298,10 +337,32 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
     } else if (warp >= 4) {
         // Tensor memory is emptied into registers first, already in the type of y, so that the next tile's MMAs wait for no store;
         // then 64 rows of y at a time go through shared memory, where the 8x8 matrices are turned round, and out as whole rows.
+        if constexpr (MODE == FEW) {
+            const int tid = threadIdx.x - 128, units = (k1 - k0) * p.M * 16, KU = (int)(p.K >> 4);
+            const float r = FMT == NV && p.x_scale ? __fdiv_rn(1.0f, *p.x_scale) : 1.0f;
+            for (int i0 = 0; i0 < units; i0 += 256) {   // whole warps: they exchange scales
+                const int i = i0 + tid, u = i & 15, line = i >> 4, kt = line / p.M, row = line - kt * p.M, unit = (k0 + kt) * 16 + u;
+                const bool live = i < units, read = live && unit < KU;
+                const uint16_t *src = p.xr + row * p.ldx + (int64_t)unit * 16;
+                const uint4 a = read ? load16(src) : make_uint4(0, 0, 0, 0), b = read ? load16(src + 8) : make_uint4(0, 0, 0, 0);
+                uint32_t scale;
+                const uint2 codes = p.f16 ? quantize_unit<FMT, DT_F16>(a, b, r, scale) : quantize_unit<FMT, DT_BF16>(a, b, r, scale);
+                if (unit >= KU) scale = 0;   // behind K
+                // a tile's scales and codes as in the layout, the codes of sixteen rows alone
+                const uint32_t word = gather_scales<FMT>(scale);
+                if (live) {
+                    *reinterpret_cast<uint2 *>(x_codes + kt * SH::X_CODES + code_offset(row, u * 8)) = codes;
+                    uint8_t *sc = x_scales + kt * SB + scale_offset(row, FMT == NV ? u : u >> 1) - CODE_BYTES;
+                    if ((lane & (FMT == NV ? 3 : 7)) == 0) *reinterpret_cast<uint32_t *>(sc) = word;
+                }
+            }
+            tc::fence_proxy_async();   // the tensor core reads through the async proxy
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(x_ready);
+        }
         const int quad = warp & 3, part = (warp - 4) >> 2;   // the 32 lanes of tensor memory that a warp may read; its half of 64 columns
-        int local = 0;
-        for (int idx = unit; idx < items; idx += stride, ++local) {
-            const Item t = item_of<PAIR>(p, idx, s_off, s_blk, s_item);
+        for (int local = 0; tiles.has(local); ++local) {
+            const Item t = tiles.at(local);
             const int acc = local % ACCS;
             const bool ok = tc::mbar_wait(&acc_full[acc], (local / ACCS) & 1, p.status, 56, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
             if (epilogue_any(!ok)) { *dead = 1; break; }
@@ -309,12 +370,13 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             tc::tc_fence_after();
             const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
             const int nb = t.nb * CTAS + half;
-            uint32_t out16[BN / 64][16];
+            constexpr int GROUPS = (BN + 63) / 64;
+            uint32_t out16[GROUPS][16];
 #pragma unroll
-            for (int g = 0; g < BN / 64; ++g) {
+            for (int g = 0; g < GROUPS; ++g) {
                 if (g * 64 + part * 32 < t.rows) {
                     uint32_t lo[16], hi[16];
-                    const uint32_t from = TMEM + acc * BN + g * 64 + part * 32 + ((uint32_t)(quad * 32) << 16);
+                    const uint32_t from = TMEM + acc * ACC_COLS + g * 64 + part * 32 + ((uint32_t)(quad * 32) << 16);
                     tmem_ld_16x32(from, lo);
                     tmem_ld_16x32(from + (16u << 16), hi);
                     tc::tmem_ld_wait();
@@ -337,7 +399,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             const int tid = threadIdx.x - 128;
             const uint32_t at = tc::smem_u32(staged) + (part * 32 + (lane & 7)) * SH::PITCH + quad * 64 + (lane >> 3) * 16;
 #pragma unroll
-            for (int g = 0; g < BN / 64; ++g) {
+            for (int g = 0; g < GROUPS; ++g) {
                 if (g * 64 >= t.rows) break;
                 if (g * 64 + part * 32 < t.rows) {
 #pragma unroll
@@ -345,7 +407,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
                 }
                 epilogue_sync();
                 const int count = min(64, t.rows - g * 64);
-                uint16_t *out = p.y + (t.yrow + g * 64) * p.N + (int64_t)nb * 128;
+                uint16_t *out = p.y + ((int64_t)t.yrow + g * 64) * p.N + (int64_t)nb * 128;
                 if (p.wide) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {   // sixteen threads a row
@@ -363,7 +425,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
 
     if constexpr (SPLIT) {
         // every CTA's MMAs are done (the warps that read tensor memory waited for them), so the rings are free for partial sums
-        const Item t = item_of<PAIR>(p, unit, s_off, s_blk, s_item);
+        const Item t = tiles.at(0);
         const int CW = 128 / S, pitch = columns_of<PAIR>(t.rows) + 4;
         __syncthreads();
         tc::cluster_sync();
@@ -390,7 +452,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             const int c = threadIdx.x % CW;   // CW a power of two
             const int64_t ch = (int64_t)(t.nb * CTAS + half) * 128 + run * CW + c;
             const float *mine = part + c * pitch;
-            uint16_t *out = p.y + t.yrow * p.N + ch;
+            uint16_t *out = p.y + (int64_t)t.yrow * p.N + ch;
             for (int r = threadIdx.x / CW * 4; r < t.rows; r += 384 / CW * 4) {
                 float4 f = *reinterpret_cast<const float4 *>(mine + r);
                 for (int s = 1; s < S; ++s) {
@@ -418,39 +480,65 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
     }
 }
 
-template <int FMT, bool PAIR, bool SPLIT>
+template <int FMT, int MODE, bool SPLIT>
 static cudaError_t launch(const GemmArgs &p, int S, int64_t items, unsigned grid, cudaStream_t st) {
-    using SH = Shape<FMT, PAIR, SPLIT>;
+    using SH = Shape<FMT, MODE, SPLIT>;
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = ensure_func_attr(fp4_gemm_kernel<FMT, PAIR, SPLIT>, done, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SH::smem(MAX_EXPERTS, true));
+    const cudaError_t e = ensure_func_attr(fp4_gemm_kernel<FMT, MODE, SPLIT>, done, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SH::smem(MAX_EXPERTS, MODE != FEW));
     if (e != cudaSuccess) return e;
-    return launch_overlapped(fp4_gemm_kernel<FMT, PAIR, SPLIT>, dim3(grid), 384u, SH::smem(p.E, p.offset != nullptr), st, SH::CTAS * (SPLIT ? S : 1), true, p, S, items);
+    return launch_overlapped(fp4_gemm_kernel<FMT, MODE, SPLIT>, dim3(grid), 384u, SH::smem(p.E, p.offset != nullptr), st, SH::CTAS * (SPLIT ? S : 1), true, p, S, items);
 }
 
 }  // namespace fp4
 
 using namespace fp4;
 
+// Runs of k that an output tile of few row blocks is cut into, while the GPU has places for them.  Eight CTAs to a cluster leave SMs
+// without a cluster that fits (4096 x 4096, one row: 14.6 us with eight, 5.9 with four).
+static int runs_of(int tiles, int KT, int places) {
+    int S = 1;
+    while (S < 4 && 2 * S <= KT && 2 * S * tiles <= places) S *= 2;
+    return S;
+}
+static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scale, uint16_t *y, int64_t M, int64_t N, int64_t K, bool f16, int *status) {
+    GemmArgs p{};
+    p.w = (const uint8_t *)w; p.w_scale = w_scale; p.x_scale = x_scale; p.y = y; p.status = status;
+    p.E = 1; p.NB = (int)((N + 127) / 128); p.KT = (int)((K + KB - 1) / KB); p.steps = (int)((K + 63) / 64);
+    p.M = (int)M; p.N = N; p.K = K; p.f16 = f16; p.wide = N % 8 == 0;
+    p.band = 16;
+    return p;
+}
+
+bool fp4_few_ok(int64_t M, int64_t N, int64_t K) {
+    const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
+    return M <= FEW_ROWS && most <= FEW_TILES && M * most <= FEW_MOST;
+}
+cudaError_t launch_fp4_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, const float *x_scale, int fmt, uint16_t *y, int64_t M, int64_t N, int64_t K,
+                           bool f16, int *status, cudaStream_t st) {
+    GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
+    p.xr = x; p.ldx = ldx; p.bt = FEW_ROWS; p.token_tiles = 1;
+    const int places = sm_count(), S = runs_of(p.NB, p.KT, places);
+    const unsigned grid = (unsigned)(S > 1 ? p.NB * S : p.NB < places ? p.NB : places);
+    if (fmt == MX) return S > 1 ? launch<MX, FEW, true>(p, S, p.NB, grid, st) : launch<MX, FEW, false>(p, 1, p.NB, grid, st);
+    return S > 1 ? launch<NV, FEW, true>(p, S, p.NB, grid, st) : launch<NV, FEW, false>(p, 1, p.NB, grid, st);
+}
+
 cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, int fmt, uint16_t *y, int64_t M,
                             int64_t N, int64_t K, bool f16, int *status, cudaStream_t st) {
-    GemmArgs p{};
-    p.w = (const uint8_t *)w; p.x = (const uint8_t *)x; p.w_scale = w_scale; p.x_scale = x_scale; p.offset = offset; p.y = y; p.status = status;
-    p.E = E; p.NB = (int)((N + 127) / 128); p.KT = (int)((K + KB - 1) / KB); p.steps = (int)((K + 63) / 64);
-    p.M = (int)M; p.N = N; p.f16 = f16; p.wide = N % 8 == 0;
+    GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
+    p.x = (const uint8_t *)x; p.offset = offset; p.E = E;
     const int sms = sm_count();
     int S = 1, pair = (offset ? M / E : M) > 256, bt = pair ? 256 : 128;
-    if (!offset && M <= 256)
-        while (S < 4 && 2 * S <= p.KT && 2 * S * p.NB * ((M + 127) / 128) <= sms) S *= 2;
+    if (!offset && M <= 256) S = runs_of(p.NB * (int)((M + 127) / 128), p.KT, sms);
     p.bt = bt;
     p.token_tiles = (int)((M + bt - 1) / bt);
-    p.band = 16;
     const int ctas = pair ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sms / ctas;
     const int64_t items = (int64_t)nbu * p.token_tiles;
     const unsigned grid = (unsigned)(S > 1 ? items * S : offset ? places : items < places ? items : places) * ctas;
     auto go = [&](auto f) {
         constexpr int F = decltype(f)::value;
-        if (S > 1) return pair ? launch<F, true, true>(p, S, items, grid, st) : launch<F, false, true>(p, S, items, grid, st);
-        return pair ? launch<F, true, false>(p, 1, items, grid, st) : launch<F, false, false>(p, 1, items, grid, st);
+        if (S > 1) return pair ? launch<F, TWO, true>(p, S, items, grid, st) : launch<F, ONE, true>(p, S, items, grid, st);
+        return pair ? launch<F, TWO, false>(p, 1, items, grid, st) : launch<F, ONE, false>(p, 1, items, grid, st);
     };
     return fmt == MX ? go(std::integral_constant<int, MX>{}) : go(std::integral_constant<int, NV>{});
 }

@@ -7,36 +7,7 @@
 namespace cq {
 namespace fp4 {
 
-// ---------------------------------------------------------------- sixteen values of a row
-struct Raw16 { uint4 v[2]; };
-__device__ __forceinline__ uint4 load16(const void *p) { return *reinterpret_cast<const uint4 *>(p); }
-template <int DT>
-__device__ __forceinline__ float value_of(const uint32_t *w, int i) {
-    const uint32_t h = (i & 1) ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu;
-    return DT == DT_BF16 ? __uint_as_float(h << 16) : __half2float(__ushort_as_half((unsigned short)h));
-}
-// bits of the largest magnitude of sixteen 16-bit values; NaN counts as the largest
-template <int DT>
-__device__ __forceinline__ uint32_t top_of_16bit(const uint32_t *w) {
-    if (DT == DT_BF16) {
-        __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[0]));
-#pragma unroll
-        for (int i = 1; i < 8; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i])));
-        const uint32_t b = *reinterpret_cast<uint32_t *>(&m) & 0x7FFF7FFFu;
-        return max(b << 16, b & 0xFFFF0000u);
-    }
-    __half2 m = __habs2(*reinterpret_cast<const __half2 *>(&w[0]));
-#pragma unroll
-    for (int i = 1; i < 8; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __half2 *>(&w[i])));
-    return max(__float_as_uint(__low2float(m)) & 0x7FFFFFFFu, __float_as_uint(__high2float(m)) & 0x7FFFFFFFu);
-}
-
-template <int FMT>
-__device__ __forceinline__ uint32_t top_of_block(uint32_t top) {   // MXFP4: two threads hold a block
-    return FMT == MX ? max(top, __shfl_xor_sync(~0u, top, 1)) : top;
-}
-
-// ---------------------------------------------------------------- where a row goes
+// ---------------------------------------------------------------- which rows, and where they go
 struct Rows {
     const int32_t *route_token;   // routed: the row of x that row r takes (null: r itself)
     const int32_t *offset;        // routed: first rows of the groups, on the device (null: rows are dense)
@@ -55,25 +26,49 @@ __device__ __forceinline__ int64_t padded_row(const Rows &q, int64_t r, const in
     const int64_t e = r / q.per;
     return e * ((q.per + ROWS - 1) / ROWS * ROWS) + (r - e * q.per);
 }
+__device__ __forceinline__ void scan_if_routed(const Rows &q, int *s_off, int *s_blk) {
+    if (!q.offset) return;
+    if (threadIdx.x < 32) scan_groups(q.offset, q.E, (int)q.rows, s_off, s_blk);
+    __syncthreads();
+}
 
-// Sixteen codes of (row, unit of 16 k) and their scales into the layout.  All lanes take part in the exchange of the scale
+// The quantisers' work is cut into pieces of 32 rows x 256 k of a tile; a block of 256 threads takes them in turn.  Sixteen threads hold the
+// 256 k of a row, a thread sixteen k of two rows, so that what depends on the place is worked out once a piece: with a flat
+// index a value cost sixteen instructions, most of them for its address.
+constexpr int PIECE = 32;
+struct Piece { int64_t first; int blk, kt, from, rows, e; };   // first row of the row block; row block, k tile; first row of the piece in it; rows that the row block has; matrix
+__device__ __forceinline__ int64_t pieces_of(const Rows &q, int KT, const int *s_blk) {
+    const int64_t blocks = q.offset ? s_blk[q.E] : q.E * ((q.per + ROWS - 1) / ROWS);
+    return blocks * KT * (ROWS / PIECE);
+}
+__device__ __forceinline__ Piece piece_at(const Rows &q, int KT, int64_t i, const int *s_off, const int *s_blk) {
+    Piece c;
+    const int64_t line = i <= 0xFFFFFFFFll ? (int64_t)((uint32_t)i / (uint32_t)KT) : i / KT;
+    c.kt = (int)(i - line * KT);
+    c.blk = (int)(line / (ROWS / PIECE));
+    c.from = (int)(line % (ROWS / PIECE)) * PIECE;
+    if (q.offset) {
+        c.e = find_group(s_blk, q.E, c.blk);
+        const int in = (c.blk - s_blk[c.e]) * ROWS;
+        c.first = s_off[c.e] + in;
+        c.rows = min(ROWS, s_off[c.e + 1] - s_off[c.e] - in);
+    } else {
+        const int per = (int)((q.per + ROWS - 1) / ROWS);
+        c.e = q.E == 1 ? 0 : c.blk / per;
+        const int64_t in = (int64_t)(c.blk - c.e * per) * ROWS;
+        c.first = c.e * q.per + in;
+        c.rows = (int)min((int64_t)ROWS, q.per - in);
+    }
+    return c;
+}
+
+// Sixteen codes of (row r, unit u of sixteen k) of a tile and their scales.  All lanes take part in the exchange of the scale
 // bytes: four scales of a row are neighbours in memory and are written as one word.
 template <int FMT>
-__device__ __forceinline__ void store_unit(uint8_t *layout, int64_t prow, int unit, int KT, uint2 codes, uint32_t scale) {
+__device__ __forceinline__ void store_unit(uint8_t *tile, int r, int u, bool live, uint2 codes, uint32_t scale) {
     const int lane = threadIdx.x & 31;
-    uint32_t word;
-    if (FMT == NV) {
-        word = scale << (8 * (lane & 3));
-        word |= __shfl_xor_sync(~0u, word, 1);
-        word |= __shfl_xor_sync(~0u, word, 2);
-    } else {
-        word = scale << (8 * ((lane >> 1) & 3));
-        word |= __shfl_xor_sync(~0u, word, 2);
-        word |= __shfl_xor_sync(~0u, word, 4);
-    }
-    if (prow < 0) return;
-    const int r = (int)(prow & (ROWS - 1)), u = unit & 15;
-    uint8_t *tile = layout + ((prow >> 7) * KT + (unit >> 4)) * (int64_t)tile_bytes(FMT);
+    const uint32_t word = gather_scales<FMT>(scale);
+    if (!live) return;
     *reinterpret_cast<uint2 *>(tile + code_offset(r, u * 8)) = codes;
     if (FMT == NV) {
         if ((lane & 3) == 0) *reinterpret_cast<uint32_t *>(tile + scale_offset(r, u)) = word;
@@ -81,19 +76,9 @@ __device__ __forceinline__ void store_unit(uint8_t *layout, int64_t prow, int un
         *reinterpret_cast<uint32_t *>(tile + scale_offset(r, u >> 1)) = word;
     }
 }
-
-template <int FMT>
-__device__ __forceinline__ uint2 round_codes(const float *v, float factor) {
-    float u[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) u[i] = __fmul_rn(v[i], factor);
-    return make_uint2(to_e2m1x8(u), to_e2m1x8(u + 8));
-}
-
-__device__ __forceinline__ void scan_if_routed(const Rows &q, int *s_off, int *s_blk) {
-    if (!q.offset) return;
-    if (threadIdx.x < 32) scan_groups(q.offset, q.E, (int)q.rows, s_off, s_blk);
-    __syncthreads();
+// NVFP4: what values are multiplied by under each scale byte, r / scale (the byte of NaN: 0), in shared memory
+__device__ __forceinline__ void fill_factors(float *s_factor, float r) {
+    if (threadIdx.x < 128) s_factor[threadIdx.x] = threadIdx.x < 127 ? __fdiv_rn(r, from_e4m3(threadIdx.x)) : 0.0f;
 }
 
 // ---------------------------------------------------------------- the quantiser
@@ -101,200 +86,234 @@ __device__ __forceinline__ void scan_if_routed(const Rows &q, int *s_off, int *s
 template <int FMT, int DT>
 __global__ void __launch_bounds__(256) quantize_kernel(const void *x, int64_t ldx, Rows q, int64_t K, int KT, const float *tensor_scale, uint8_t *layout) {
     extern __shared__ int s_tab[];
+    __shared__ float s_factor[128];
     tc::wait_for_previous_kernel();
     int *s_off = s_tab, *s_blk = s_tab + q.E + 1;
     scan_if_routed(q, s_off, s_blk);
-    const uint32_t U = (uint32_t)KT * 16u, KU = (uint32_t)(K >> 4);
-    const int64_t total = q.rows * U;
-    for (int64_t base = (int64_t)blockIdx.x * 256; base < total; base += (int64_t)gridDim.x * 256) {   // whole warps stay together
-        const int64_t idx = base + threadIdx.x;
-        const int64_t row = total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)idx / U) : idx / U;
-        const uint32_t unit = (uint32_t)(idx - row * U);
-        const int64_t prow = idx < total ? padded_row(q, row, s_off, s_blk) : -1;
-        int64_t src = row;
-        bool read = prow >= 0 && unit < KU;
-        if (read && q.route_token) {
-            src = q.route_token[row];
-            read = src >= 0 && src < q.T;   // any other token is a row of zeros
-        }
-        const float r = FMT == NV ? (tensor_scale ? __fdiv_rn(1.0f, tensor_scale[q.offset || q.E == 1 || row >= q.rows ? 0 : row / q.per]) : 1.0f) : 1.0f;
-        float v[16];
-        uint32_t top;
-        if (DT == DT_F32) {
-            const float *p = reinterpret_cast<const float *>(x) + src * ldx + (int64_t)unit * 16;
-            top = 0;
+    const int u = threadIdx.x & 15, KU = (int)(K >> 4);
+    const int64_t pieces = pieces_of(q, KT, s_blk);
+    int scaled_for = -1;   // the matrix that r and the factors belong to
+    float r = 1.0f;
+    for (int64_t i = blockIdx.x; i < pieces; i += gridDim.x) {
+        const Piece c = piece_at(q, KT, i, s_off, s_blk);
+        if (c.from >= c.rows) continue;
+        const int e = q.offset ? 0 : c.e;
+        const int unit = c.kt * 16 + u;
+        uint8_t *tile = layout + ((int64_t)c.blk * KT + c.kt) * tile_bytes(FMT);
+        uint4 raw[2][DT == DT_F32 ? 4 : 2];
+        bool live[2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 w = read ? load16(p + 4 * i) : make_uint4(0, 0, 0, 0);
-                v[4 * i] = __uint_as_float(w.x); v[4 * i + 1] = __uint_as_float(w.y);
-                v[4 * i + 2] = __uint_as_float(w.z); v[4 * i + 3] = __uint_as_float(w.w);
+        for (int j = 0; j < 2; ++j) {
+            const int row = c.from + (threadIdx.x >> 4) + 16 * j;
+            live[j] = row < c.rows;
+            int64_t src = c.first + row;
+            bool read = live[j] && unit < KU;
+            if (read && q.route_token) {
+                src = q.route_token[src];
+                read = src >= 0 && src < q.T;   // any other token is a row of zeros
             }
+            const uint8_t *p = reinterpret_cast<const uint8_t *>(x) + (src * ldx + (int64_t)unit * 16) * (DT == DT_F32 ? 4 : 2);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-        } else {
-            const uint16_t *p = reinterpret_cast<const uint16_t *>(x) + src * ldx + (int64_t)unit * 16;
-            uint4 a = make_uint4(0, 0, 0, 0), b = a;
-            if (read) { a = load16(p); b = load16(p + 8); }
-            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            top = top_of_16bit<DT>(w);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = value_of<DT>(w, i);
+            for (int k = 0; k < (DT == DT_F32 ? 4 : 2); ++k) raw[j][k] = read ? load16(p + 16 * k) : make_uint4(0, 0, 0, 0);
         }
-        float factor;
-        uint32_t scale = block_scale<FMT>(top_of_block<FMT>(top), r, factor);
-        uint2 codes = round_codes<FMT>(v, factor);
-        if (factor == 0.0f) codes = make_uint2(0, 0);   // a block with a NaN or an infinity: what counts is its scale
-        if (unit >= KU) scale = 0;                      // behind K
-        store_unit<FMT>(layout, prow, (int)unit, KT, codes, scale);
+        if (FMT == NV && e != scaled_for) {
+            if (scaled_for >= 0) __syncthreads();
+            if (tensor_scale) r = __fdiv_rn(1.0f, tensor_scale[e]);
+            fill_factors(s_factor, r);
+            __syncthreads();
+            scaled_for = e;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (c.from + 16 * j >= c.rows) break;
+            float v[16];
+            uint32_t top;
+            if (DT == DT_F32) {
+                top = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint4 w = raw[j][DT == DT_F32 ? k : 0];
+                    v[4 * k] = __uint_as_float(w.x); v[4 * k + 1] = __uint_as_float(w.y);
+                    v[4 * k + 2] = __uint_as_float(w.z); v[4 * k + 3] = __uint_as_float(w.w);
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) top = max(top, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+            } else {
+                const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w, raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
+                top = top_of_16bit<DT>(w);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] = value_of<DT>(w, k);
+            }
+            float factor;
+            uint32_t scale = block_scale<FMT>(top_of_block<FMT>(top), r, s_factor, factor);
+            uint2 codes = round_codes(v, factor);
+            if (factor == 0.0f) codes = make_uint2(0, 0);   // a block with a NaN or an infinity: what counts is its scale
+            if (unit >= KU) scale = 0;                      // behind K
+            store_unit<FMT>(tile, c.from + (threadIdx.x >> 4) + 16 * j, u, live[j], codes, scale);
+        }
     }
 }
 
 // ---------------------------------------------------------------- gated activation and quantiser
 // act = silu(gate) * up = gate up / (1 + exp(-gate)), rounded to the model dtype, then quantised; the activation itself reaches no memory.
 // A code changes when a rounding to the model dtype falls on the other side of a border between two codes, so that rounding has to
-// be right, and 32 bits leave it open where the value lies next to a border of the model dtype.  gate * up is exact in 32 bits, exp
-// is off by 1 ulp, the sum by half, the division by 2: four ulps.  Where no value lies within BAND = 8 ulps of a border
-// the roundings stand; in a unit where one does (one in 180 in bfloat16, one in 23 in binary16), its two candidates are
-// quantised both ways, and only when the scale or a code differ is the value formed in 64 bits.  Far negative gates
-// (exp(60) is still finite in 32 bits, with room) go that way at once.
-constexpr int BAND = 8;
-template <int DT>
-__device__ __forceinline__ uint32_t round16(float v) {
-    return DT == DT_BF16 ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v)) : (uint32_t)__half_as_ushort(__float2half_rn(v));
-}
+// be right, and 32 bits leave it open where the value lies next to a border of the model dtype.  In units of 2^-24 of the value:
+// gate * up is exact; exp(-g) = 2^h (1 + l ln 2), h + l = -g log2(e) with the constant in two parts, ex2.approx 4 and the two products 2; the
+// sum 1, the reciprocal 2, the last product 1: ten.  Where no value lies within BAND = 12 units of the last place (each at least such a unit)
+// of a border, the roundings stand.  In a unit of sixteen where one does (one in 170 in bfloat16, one in 22 in binary16) the
+// candidates on both sides are quantised, and only where a scale or a code differs is the activation formed in 64 bits.  Gates beyond 60
+// either way go there at once (exp(60) leaves room in 32 bits for the denominator and its reciprocal).
+constexpr int BAND = 12;
 template <int DT>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     if (DT == DT_BF16) { const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const uint32_t *>(&p); }
     const __half2 p = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
 }
-template <int DT>
-__device__ __noinline__ uint32_t gated_in_64_bits(float g, float u) {
-    const double y = (double)g * (double)u / (1.0 + exp(-(double)g));
-    return round16<DT>((float)y);
-}
+__device__ __noinline__ float gated_in_64_bits(float g, float u) { return (float)((double)g * (double)u / (1.0 + exp(-(double)g))); }
 __device__ __forceinline__ float ulps_away(float v, int n) { return __uint_as_float(__float_as_uint(v) + n); }   // n > 0: away from zero
+// two activations
+__device__ __forceinline__ void gated_in_32_bits(float g0, float g1, float u0, float u1, float &y0, float &y1) {
+    const Pair g = pair_of(g0, g1), major = pair_of(-1.44269502f, -1.44269502f), minor = pair_of(-1.92596303e-8f, -1.92596303e-8f);   // log2(e) = their sum, negated
+    const Pair h = mul2(g, major);
+    float h0, h1, d0, d1;
+    unpair(h, h0, h1);
+    const Pair l = fma2(g, minor, fma2(g, major, pair_of(-h0, -h1)));
+    float e0, e1;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(h0));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(h1));
+    const Pair e = pair_of(e0, e1);
+    unpair(add2(fma2(e, mul2(l, pair_of(0.693147181f, 0.693147181f)), e), pair_of(1.0f, 1.0f)), d0, d1);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(d0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(d1));
+    unpair(mul2(mul2(g, pair_of(u0, u1)), pair_of(e0, e1)), y0, y1);
+}
+// The least distance, as (bits - border + BAND) in the bits that rounding to the model dtype drops (binary16: in their eighths), of two values
+// and of those before; borders lie in the middle of these bits.
+template <int DT>
+__device__ __forceinline__ uint32_t nearer(uint32_t near, float y0, float y1) {
+    const uint32_t low = __byte_perm(__float_as_uint(y0), __float_as_uint(y1), 0x5410);
+    constexpr uint32_t SHIFT = DT == DT_BF16 ? 1 : 8, ADD = (0x8000u + BAND * SHIFT) & 0xFFFFu;
+    return __viaddmin_u16x2(DT == DT_BF16 ? low : (low & 0x1FFF1FFFu) * 8u, ADD << 16 | ADD, near);
+}
 
 template <int FMT, int DT>
-__global__ void __launch_bounds__(256) swiglu_quantize_kernel(const uint16_t *h, int64_t ldh, Rows q, int64_t I, int KT, const float *tensor_scale, uint8_t *layout) {
+__global__ void __launch_bounds__(256, 4) swiglu_quantize_kernel(const uint16_t *h, int64_t ldh, Rows q, int64_t I, int KT, const float *tensor_scale, uint8_t *layout) {
     extern __shared__ int s_tab[];
+    __shared__ float s_factor[128];
     tc::wait_for_previous_kernel();
     int *s_off = s_tab, *s_blk = s_tab + q.E + 1;
-    scan_if_routed(q, s_off, s_blk);
-    const uint32_t U = (uint32_t)KT * 16u, KU = (uint32_t)(I >> 4);
-    const int64_t total = q.rows * U;
     const float r = FMT == NV && tensor_scale ? __fdiv_rn(1.0f, *tensor_scale) : 1.0f;
-    for (int64_t base = (int64_t)blockIdx.x * 256; base < total; base += (int64_t)gridDim.x * 256) {
-        const int64_t idx = base + threadIdx.x;
-        const int64_t row = total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)idx / U) : idx / U;
-        const uint32_t unit = (uint32_t)(idx - row * U);
-        const int64_t prow = idx < total ? padded_row(q, row, s_off, s_blk) : -1;
-        const bool read = prow >= 0 && unit < KU;
-        const uint16_t *pg = h + row * ldh + (int64_t)unit * 16, *pu = pg + I;
-        uint32_t gw[8] = {}, uw[8] = {}, act[8];
-        if (read) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint4 a = load16(pg + 8 * i), b = load16(pu + 8 * i);
-                gw[4 * i] = a.x; gw[4 * i + 1] = a.y; gw[4 * i + 2] = a.z; gw[4 * i + 3] = a.w;
-                uw[4 * i] = b.x; uw[4 * i + 1] = b.y; uw[4 * i + 2] = b.z; uw[4 * i + 3] = b.w;
-            }
-        }
-        float y[16];
-        // least distance to a border of the model dtype, in ulps, less BAND; borders lie in the middle of the bits that are dropped
-        constexpr uint32_t DROP = DT == DT_BF16 ? 0xFFFFu : 0x1FFFu, HALF = DT == DT_BF16 ? 0x8000u : 0x1000u;
-        uint32_t near = ~0u;
-        float least = 0.0f, small = 1.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float g = value_of<DT>(gw, i), u = value_of<DT>(uw, i);
-            y[i] = __fdividef(__fmul_rn(g, u), 1.0f + expf(-g));
-            near = min(near, (__float_as_uint(y[i]) - HALF + BAND) & DROP);
-            least = fminf(least, g);
-            if (DT == DT_F16) small = fminf(small, y[i] == 0.0f ? 1.0f : fabsf(y[i]));   // subnormal halves have their borders elsewhere
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) act[i] = pack16<DT>(y[2 * i], y[2 * i + 1]);
-        const bool far = least < -60.0f;
-        const bool open = near <= 2 * BAND || far || (DT == DT_F16 && small < 6.103515625e-05f);
-        uint32_t top = top_of_block<FMT>(top_of_16bit<DT>(act));
-        if (__any_sync(~0u, open)) {
-            // the candidates on both sides: a unit without open values has the same ones
-            uint32_t a0[8], a1[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                a0[i] = pack16<DT>(ulps_away(y[2 * i], -BAND), ulps_away(y[2 * i + 1], -BAND));
-                a1[i] = pack16<DT>(ulps_away(y[2 * i], BAND), ulps_away(y[2 * i + 1], BAND));
-                if (!open) a0[i] = a1[i] = act[i];
-            }
-            const uint32_t t0 = top_of_block<FMT>(top_of_16bit<DT>(a0)), t1 = top_of_block<FMT>(top_of_16bit<DT>(a1));
-            float f0, f1, v0[16], v1[16];
-            const uint32_t s0 = block_scale<FMT>(t0, r, f0), s1 = block_scale<FMT>(t1, r, f1);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) { v0[i] = value_of<DT>(a0, i); v1[i] = value_of<DT>(a1, i); }
-            const uint2 c0 = round_codes<FMT>(v0, f0), c1 = round_codes<FMT>(v1, f1);
-            const bool differ = open && (far || s0 != s1 || c0.x != c1.x || c0.y != c1.y);
-            if (differ) {
+    if (FMT == NV) fill_factors(s_factor, r);
+    scan_if_routed(q, s_off, s_blk);
+    __syncthreads();
+    const int u = threadIdx.x & 15, KU = (int)(I >> 4);
+    const int64_t pieces = pieces_of(q, KT, s_blk);
+    for (int64_t i = blockIdx.x; i < pieces; i += gridDim.x) {
+        const Piece c = piece_at(q, KT, i, s_off, s_blk);
+        if (c.from >= c.rows) continue;
+        const int unit = c.kt * 16 + u;
+        uint8_t *tile = layout + ((int64_t)c.blk * KT + c.kt) * tile_bytes(FMT);
 #pragma unroll 1
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t g2 = gw[i], u2 = uw[i];
-                    uint32_t lo = gated_in_64_bits<DT>(value_of<DT>(&g2, 0), value_of<DT>(&u2, 0));
-                    act[i] = lo | gated_in_64_bits<DT>(value_of<DT>(&g2, 1), value_of<DT>(&u2, 1)) << 16;
+        for (int j = 0; j < 2 && c.from + 16 * j < c.rows; ++j) {   // one unit at a time: its registers leave room for the threads that hide the loads
+            const int row = c.from + (threadIdx.x >> 4) + 16 * j;
+            const bool live = row < c.rows, read = live && unit < KU;
+            const uint16_t *pg = h + (c.first + row) * ldh + (int64_t)unit * 16, *pu = pg + I;
+            uint32_t gw[8] = {}, uw[8] = {};
+            if (read) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint4 a = load16(pg + 8 * k), b = load16(pu + 8 * k);
+                    gw[4 * k] = a.x; gw[4 * k + 1] = a.y; gw[4 * k + 2] = a.z; gw[4 * k + 3] = a.w;
+                    uw[4 * k] = b.x; uw[4 * k + 1] = b.y; uw[4 * k + 2] = b.z; uw[4 * k + 3] = b.w;
                 }
             }
-            top = top_of_block<FMT>(top_of_16bit<DT>(act));
-        }
-        float factor, v[16];
-        uint32_t scale = block_scale<FMT>(top, r, factor);
+            uint32_t act[8], near = ~0u;
+            float y[16], small = 1.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = value_of<DT>(act, i);
-        uint2 codes = round_codes<FMT>(v, factor);
-        if (factor == 0.0f) codes = make_uint2(0, 0);
-        if (unit >= KU) scale = 0;
-        store_unit<FMT>(layout, prow, (int)unit, KT, codes, scale);
+            for (int k = 0; k < 16; k += 2) {
+                gated_in_32_bits(value_of<DT>(gw, k), value_of<DT>(gw, k + 1), value_of<DT>(uw, k), value_of<DT>(uw, k + 1), y[k], y[k + 1]);
+                near = nearer<DT>(near, y[k], y[k + 1]);
+                act[k / 2] = pack16<DT>(y[k], y[k + 1]);
+                if (DT == DT_F16) small = fminf(small, fminf(y[k] == 0.0f ? 1.0f : fabsf(y[k]), y[k + 1] == 0.0f ? 1.0f : fabsf(y[k + 1])));   // subnormal halves have their borders elsewhere
+            }
+            constexpr uint32_t WIDE = 2 * BAND * (DT == DT_BF16 ? 1 : 8);
+            const bool far = top_of_16bit<DT>(gw) > 0x42700000u;   // 60
+            const bool open = (near & 0xFFFFu) <= WIDE || (near >> 16) <= WIDE || far || (DT == DT_F16 && small < 6.103515625e-05f);
+            uint32_t top = top_of_block<FMT>(top_of_16bit<DT>(act));
+            if (__any_sync(~0u, open)) {
+                uint32_t a0[8], a1[8];   // a unit without open values has one candidate
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    a0[k] = open ? pack16<DT>(ulps_away(y[2 * k], -BAND), ulps_away(y[2 * k + 1], -BAND)) : act[k];
+                    a1[k] = open ? pack16<DT>(ulps_away(y[2 * k], BAND), ulps_away(y[2 * k + 1], BAND)) : act[k];
+                }
+                float f0, f1, v0[16], v1[16];
+                const uint32_t s0 = block_scale<FMT>(top_of_block<FMT>(top_of_16bit<DT>(a0)), r, s_factor, f0);
+                const uint32_t s1 = block_scale<FMT>(top_of_block<FMT>(top_of_16bit<DT>(a1)), r, s_factor, f1);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) { v0[k] = value_of<DT>(a0, k); v1[k] = value_of<DT>(a1, k); }
+                const uint2 c0 = round_codes(v0, f0), c1 = round_codes(v1, f1);
+                if (open && (far || s0 != s1 || c0.x != c1.x || c0.y != c1.y)) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (far || a0[k] != a1[k])
+                            act[k] = pack16<DT>(gated_in_64_bits(value_of<DT>(gw, 2 * k), value_of<DT>(uw, 2 * k)), gated_in_64_bits(value_of<DT>(gw, 2 * k + 1), value_of<DT>(uw, 2 * k + 1)));
+                }
+                top = top_of_block<FMT>(top_of_16bit<DT>(act));
+            }
+            float factor, v[16];
+            uint32_t scale = block_scale<FMT>(top, r, s_factor, factor);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = value_of<DT>(act, k);
+            uint2 codes = round_codes(v, factor);
+            if (factor == 0.0f) codes = make_uint2(0, 0);
+            if (unit >= KU) scale = 0;
+            store_unit<FMT>(tile, row, u, live, codes, scale);
+        }
     }
 }
 
 // ---------------------------------------------------------------- back to values
-// code * fl32(scale * g), rounded once to the type asked for.  Reads what the layout stores, writes 2 or 4 bytes a value.
+// code * fl32(scale * g), rounded once to the type asked for.  Reads what the layout stores, writes 2 or 4 bytes a value: bound by the
+// stores, so a thread takes eight values, neighbours in memory to its neighbours'.
 template <int FMT, int DT>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t *layout, Rows q, int64_t K, int KT, const float *tensor_scale, void *y) {
     extern __shared__ int s_tab[];
     tc::wait_for_previous_kernel();
     int *s_off = s_tab, *s_blk = s_tab + q.E + 1;
     scan_if_routed(q, s_off, s_blk);
-    const uint32_t KU = (uint32_t)(K >> 4);
-    const int64_t total = q.rows * KU;
-    for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (int64_t)gridDim.x * 256) {
-        const int64_t row = total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)idx / KU) : idx / KU;
-        const int unit = (int)(idx - row * KU), u = unit & 15;
-        const int64_t prow = padded_row(q, row, s_off, s_blk);
-        if (prow < 0) continue;
-        const int r = (int)(prow & (ROWS - 1));
-        const uint8_t *tile = layout + ((prow >> 7) * KT + (unit >> 4)) * (int64_t)tile_bytes(FMT);
-        const uint2 codes = *reinterpret_cast<const uint2 *>(tile + code_offset(r, u * 8));
-        float s;
-        if (FMT == NV) {
-            s = from_e4m3(tile[scale_offset(r, u)]);
-            if (tensor_scale) s = __fmul_rn(s, tensor_scale[q.offset || q.E == 1 ? 0 : row / q.per]);
-        } else {
-            s = from_e8m0(tile[scale_offset(r, u >> 1)]);
+    const int u = threadIdx.x & 31, KU = (int)(K >> 3);
+    const int64_t pieces = pieces_of(q, KT, s_blk);
+    for (int64_t i = blockIdx.x; i < pieces; i += gridDim.x) {
+        const Piece c = piece_at(q, KT, i, s_off, s_blk);
+        if (c.from >= c.rows || c.kt * 32 + u >= KU) continue;
+        const uint8_t *tile = layout + ((int64_t)c.blk * KT + c.kt) * tile_bytes(FMT);
+        const float g = FMT == NV && tensor_scale ? tensor_scale[q.offset ? 0 : c.e] : 1.0f;
+        uint32_t codes[4], scales[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = c.from + (threadIdx.x >> 5) + 8 * j;   // what lies behind the last row is inside the tile too
+            codes[j] = *reinterpret_cast<const uint32_t *>(tile + code_offset(r, u * 4));
+            scales[j] = tile[scale_offset(r, FMT == NV ? u >> 1 : u >> 2)];
         }
-        float v[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = from_e2m1((i < 8 ? codes.x : codes.y) >> (4 * (i & 7))) * s;
-        const int64_t at = row * K + (int64_t)unit * 16;
-        if (DT == DT_F32) {
-            float4 *p = reinterpret_cast<float4 *>(reinterpret_cast<float *>(y) + at);
+        for (int j = 0; j < 4; ++j) {
+            const int r = c.from + (threadIdx.x >> 5) + 8 * j;
+            if (r >= c.rows) break;
+            const float s = FMT == NV ? __fmul_rn(from_e4m3(scales[j]), g) : from_e8m0(scales[j]);
+            float v[8];
+            from_e2m1x8(codes[j], v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        } else {
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = pack16<DT>(v[2 * i], v[2 * i + 1]);
-            uint4 *p = reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(y) + at);
-            p[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            p[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            for (int k = 0; k < 8; ++k) v[k] *= s;
+            const int64_t at = (c.first + r) * K + c.kt * KB + u * 8;
+            if (DT == DT_F32) {
+                float4 *p = reinterpret_cast<float4 *>(reinterpret_cast<float *>(y) + at);
+                p[0] = make_float4(v[0], v[1], v[2], v[3]);
+                p[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+                *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(y) + at) = make_uint4(pack16<DT>(v[0], v[1]), pack16<DT>(v[2], v[3]), pack16<DT>(v[4], v[5]), pack16<DT>(v[6], v[7]));
+            }
         }
     }
 }
@@ -326,10 +345,16 @@ __global__ void __launch_bounds__(256) exchange_kernel(uint8_t *codes, uint8_t *
 }
 
 // ---------------------------------------------------------------- launchers
-// Enough blocks to fill the SMs eight deep; the rest of the rows follow in a loop (the table of the groups is read once a block).
-static unsigned grid_for(int64_t units) {
-    const int64_t blocks = (units + 255) / 256, most = 8 * (int64_t)sm_count();
+// Enough blocks to fill the SMs eight deep; the rest follows in a loop (the tables of a block are filled once).
+static unsigned grid_of(int64_t blocks) {
+    const int64_t most = 8 * (int64_t)sm_count();
     return (unsigned)(blocks < most ? blocks : most);
+}
+static unsigned grid_for(int64_t units) { return grid_of((units + 255) / 256); }
+// pieces of all row blocks that may have rows (routed: every group may end a block early); of the last row block of a single matrix only those that have
+static unsigned grid_for_pieces(const Rows &q, int KT) {
+    const int64_t per = q.offset ? (q.rows + (ROWS - 1) * (q.E < q.rows ? q.E : q.rows)) / ROWS * ROWS : q.E == 1 ? q.rows : (q.per + ROWS - 1) / ROWS * ROWS * q.E;
+    return grid_of((per + PIECE - 1) / PIECE * KT);
 }
 static size_t table_bytes(const Rows &q) { return q.offset ? 2 * (size_t)(q.E + 1) * sizeof(int) : 0; }
 static Rows rows_of(const Fp4Rows &s) { return Rows{s.route_token, s.offset, s.E, s.per, s.rows, s.T}; }
@@ -343,7 +368,7 @@ cudaError_t launch_fp4_quantize(const void *x, int dtype, int64_t ldx, const Fp4
     const Rows q = rows_of(s);
     const int KT = kt_of(K);
     auto go = [&](auto kern) {
-        return launch_overlapped(kern, dim3(grid_for(q.rows * KT * 16)), 256u, table_bytes(q), st, 1, true, x, ldx, q, K, KT, tensor_scale, (uint8_t *)layout);
+        return launch_overlapped(kern, dim3(grid_for_pieces(q, KT)), 256u, table_bytes(q), st, 1, true, x, ldx, q, K, KT, tensor_scale, (uint8_t *)layout);
     };
     if (fmt == MX) return dtype == DT_BF16 ? go(quantize_kernel<MX, DT_BF16>) : dtype == DT_F16 ? go(quantize_kernel<MX, DT_F16>) : go(quantize_kernel<MX, DT_F32>);
     return dtype == DT_BF16 ? go(quantize_kernel<NV, DT_BF16>) : dtype == DT_F16 ? go(quantize_kernel<NV, DT_F16>) : go(quantize_kernel<NV, DT_F32>);
@@ -353,7 +378,7 @@ cudaError_t launch_fp4_swiglu_quantize(const void *h, int dtype, int64_t ldh, co
     const Rows q = rows_of(s);
     const int KT = kt_of(I);
     auto go = [&](auto kern) {
-        return launch_overlapped(kern, dim3(grid_for(q.rows * KT * 16)), 256u, table_bytes(q), st, 1, true, (const uint16_t *)h, ldh, q, I, KT, tensor_scale, (uint8_t *)layout);
+        return launch_overlapped(kern, dim3(grid_for_pieces(q, KT)), 256u, table_bytes(q), st, 1, true, (const uint16_t *)h, ldh, q, I, KT, tensor_scale, (uint8_t *)layout);
     };
     if (fmt == MX) return dtype == DT_BF16 ? go(swiglu_quantize_kernel<MX, DT_BF16>) : go(swiglu_quantize_kernel<MX, DT_F16>);
     return dtype == DT_BF16 ? go(swiglu_quantize_kernel<NV, DT_BF16>) : go(swiglu_quantize_kernel<NV, DT_F16>);
@@ -363,7 +388,7 @@ cudaError_t launch_fp4_dequantize(const void *layout, const Fp4Rows &s, int fmt,
     const Rows q = rows_of(s);
     const int KT = kt_of(K);
     auto go = [&](auto kern) {
-        return launch_overlapped(kern, dim3(grid_for(q.rows * (K / 16))), 256u, table_bytes(q), st, 1, true, (const uint8_t *)layout, q, K, KT, tensor_scale, y);
+        return launch_overlapped(kern, dim3(grid_for_pieces(q, KT)), 256u, table_bytes(q), st, 1, true, (const uint8_t *)layout, q, K, KT, tensor_scale, y);
     };
     if (fmt == MX) return dtype == DT_BF16 ? go(dequantize_kernel<MX, DT_BF16>) : dtype == DT_F16 ? go(dequantize_kernel<MX, DT_F16>) : go(dequantize_kernel<MX, DT_F32>);
     return dtype == DT_BF16 ? go(dequantize_kernel<NV, DT_BF16>) : dtype == DT_F16 ? go(dequantize_kernel<NV, DT_F16>) : go(dequantize_kernel<NV, DT_F32>);

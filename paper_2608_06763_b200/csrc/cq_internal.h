@@ -156,6 +156,10 @@ cudaError_t launch_fp4_swiglu_quantize(const void *h, int dtype, int64_t ldh, co
 cudaError_t launch_fp4_dequantize(const void *layout, const Fp4Rows &rows, int fmt, int64_t K, const float *tensor_scale, void *y, int dtype, cudaStream_t st);
 // in: checkpoint form to layout; else back
 cudaError_t launch_fp4_exchange(uint8_t *codes, uint8_t *scales, const Fp4Rows &rows, int fmt, int64_t K, void *layout, bool in, cudaStream_t st);
+// few rows in the model dtype, quantised by the product itself; for the sizes that fp4_few_ok allows
+bool fp4_few_ok(int64_t M, int64_t N, int64_t K);
+cudaError_t launch_fp4_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, const float *x_scale, int fmt, uint16_t *y, int64_t M, int64_t N, int64_t K,
+                           bool f16, int *status, cudaStream_t st);
 // y[M][N] = x W^T of two layouts; offset != null: E groups of rows, group e times matrix e
 cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, int fmt, uint16_t *y, int64_t M,
                             int64_t N, int64_t K, bool f16, int *status, cudaStream_t st);

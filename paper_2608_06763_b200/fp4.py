@@ -45,12 +45,23 @@ def _need(ok, what: str):
         raise CubicQuantError(what)
 
 
-def _here(*tensors):
-    """Every tensor on the current device: the call goes to that device's current stream."""
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _device() -> int:
+    """The current device; -2 where there is none, which no tensor is on."""
+    if torch.cuda.is_initialized():
+        return _current_device()
+    return torch.cuda.current_device() if torch.cuda.is_available() else -2
+
+
+def _here(*tensors) -> int:
+    """The stream to launch on.  Every tensor has to be on the current device: the call goes to that device's current stream."""
+    dev = _device()
     for t in tensors:
-        if t is not None and not (t.is_cuda and t.device.index == dev):
-            raise CubicQuantError(f"a tensor on {t.device}, with device {dev} current: switch with torch.cuda.device")
+        if t is not None and t.get_device() != dev:
+            raise CubicQuantError(f"a tensor on {t.device} with device {dev} current: switch with torch.cuda.device")
+    return binding._raw_stream(dev) if binding._raw_stream is not None else _stream()
 
 
 def _at(t):
@@ -70,32 +81,47 @@ class Fp4Tensor:
     expert_offset: torch.Tensor | None = None    # routed rows: int32 [groups + 1] on the device
 
 
+# The checks below cost a call more than what they look at: no text is built, and no tensor asked twice, before something is wrong.
 def _check_format(fmt: int, K: int):
-    _need(fmt in (CQ_MXFP4, CQ_NVFP4), "fmt is CQ_MXFP4 or CQ_NVFP4")
-    _need(K > 0 and K % _BLOCK[fmt] == 0, f"K = {K} is not a multiple of the block of {_BLOCK[fmt]}")
+    if fmt != CQ_MXFP4 and fmt != CQ_NVFP4:
+        raise CubicQuantError("fmt is CQ_MXFP4 or CQ_NVFP4")
+    if K <= 0 or K % _BLOCK[fmt]:
+        raise CubicQuantError(f"K = {K} is not a multiple of the block of {_BLOCK[fmt]}")
 
 
 def _check_scale(scale, fmt: int, matrices: int = 1):
     if scale is None:
         return
-    _need(fmt == CQ_NVFP4, "MXFP4 has no tensor scale")
-    _need(scale.dtype == torch.float32 and scale.numel() == matrices and scale.is_contiguous(),
-          f"tensor_scale is {matrices} fp32 value(s) on the device")
+    if fmt != CQ_NVFP4:
+        raise CubicQuantError("MXFP4 has no tensor scale")
+    if scale.dtype != torch.float32 or scale.numel() != matrices or not scale.is_contiguous():
+        raise CubicQuantError(f"tensor_scale is {matrices} fp32 value(s) on the device")
 
 
 def _check_offset(offset, groups=None):
-    _need(isinstance(offset, torch.Tensor) and offset.dtype == torch.int32 and offset.dim() == 1 and offset.is_contiguous() and
-          (offset.numel() >= 2 if groups is None else offset.numel() == groups + 1),
-          "expert_offset is an int32 tensor of one more value than there are matrices")
+    if not (isinstance(offset, torch.Tensor) and offset.dtype == torch.int32 and offset.dim() == 1 and offset.is_contiguous() and
+            (offset.numel() >= 2 if groups is None else offset.numel() == groups + 1)):
+        raise CubicQuantError("expert_offset is an int32 tensor of one more value than there are matrices")
 
 
 def _check_rows(x, name="x"):
-    """Rows of contiguous values, any distance of whole 16 bytes apart; a row by itself, any."""
-    _need(x.dtype in _DTYPE, f"{name} is bfloat16, float16 or float32")
-    _need(x.dim() == 2 and (x.shape[1] == 1 or x.stride(1) == 1), f"{name} is a matrix whose rows are contiguous")
-    ld = x.stride(0) if x.shape[0] > 1 else x.shape[1]
-    _need(ld >= x.shape[1] and x.data_ptr() % 16 == 0 and ld * x.element_size() % 16 == 0, f"rows of {name} start on 16-byte boundaries and do not overlap")
-    return ld
+    """(rows, values of a row, distance of rows, address, code of the dtype): rows of contiguous values, any distance of whole 16 bytes apart; a row
+    by itself, any."""
+    dtype = _DTYPE.get(x.dtype)
+    if dtype is None:
+        raise CubicQuantError(f"{name} is bfloat16, float16 or float32")
+    if x.dim() != 2:
+        raise CubicQuantError(f"{name} is a matrix whose rows are contiguous")
+    M, K = x.shape
+    ld, one = x.stride()
+    if one != 1 and K > 1:
+        raise CubicQuantError(f"{name} is a matrix whose rows are contiguous")
+    if M <= 1:
+        ld = K
+    at = x.data_ptr()
+    if ld < K or at % 16 or ld % (4 if dtype == 2 else 8):
+        raise CubicQuantError(f"rows of {name} start on 16-byte boundaries and do not overlap")
+    return M, K, ld, at, dtype
 
 
 def cq_fp4_empty(fmt: int, M: int, K: int, matrices: int = 1, groups: int | None = None, device=None) -> Fp4Tensor:
@@ -113,7 +139,8 @@ def cq_fp4_empty(fmt: int, M: int, K: int, matrices: int = 1, groups: int | None
 def _into(out, fmt, M, K, matrices=1, groups=None, device=None) -> Fp4Tensor:
     if out is None:
         return cq_fp4_empty(fmt, M, K, matrices, groups, device)
-    _need((out.fmt, out.matrices, out.M, out.K, out.groups) == (fmt, matrices, M, K, groups or 0), "out is of another format or shape")
+    if out.fmt != fmt or out.M != M or out.K != K or out.matrices != matrices or out.groups != (groups or 0):
+        raise CubicQuantError("out is of another format or shape")
     return out
 
 
@@ -150,25 +177,29 @@ def cq_fp4_quantize(x: torch.Tensor, fmt: int, tensor_scale: torch.Tensor | None
     if x.dim() == 3:
         _need(x.is_contiguous() and route_token is None, "several matrices are one contiguous tensor")
         E, x = x.shape[0], x.flatten(0, 1)
-    ld = _check_rows(x)
-    K = x.shape[1]
+        _need(E > 0, "no matrix")
+    M, K, ld, at, dtype = _check_rows(x)
     _check_format(fmt, K)
     _check_scale(tensor_scale, fmt, E)
-    _need((route_token is None) == (expert_offset is None), "route_token and expert_offset come together")
-    _here(x, tensor_scale, route_token, expert_offset, out.layout if out is not None else None)
+    if (route_token is None) != (expert_offset is None):
+        raise CubicQuantError("route_token and expert_offset come together")
     if route_token is None:
-        q = _into(out, fmt, x.shape[0] // E if E else 0, K, E, device=x.device)
-        if x.shape[0]:
-            _check(_lib().cq_fp4_quantize(x.data_ptr(), _DTYPE[x.dtype], ld, fmt, E, q.M, K, _at(tensor_scale), q.layout.data_ptr(), _stream()), "cq_fp4_quantize")
+        stream = _here(x, tensor_scale, None if out is None else out.layout)
+        q = _into(out, fmt, M // E, K, E, device=x.device)
+        if M:
+            status = (_L or _lib()).cq_fp4_quantize(at, dtype, ld, fmt, E, q.M, K, _at(tensor_scale), q.layout.data_ptr(), stream)
+            if status != 0:
+                _check(status, "cq_fp4_quantize")
     else:
         _check_offset(expert_offset)
         _need(route_token.dtype == torch.int32 and route_token.dim() == 1 and route_token.is_contiguous(), "route_token is an int32 tensor")
+        stream = _here(x, tensor_scale, route_token, expert_offset, None if out is None else out.layout)
         R, groups = route_token.numel(), expert_offset.numel() - 1
         q = _into(out, fmt, R, K, 1, groups, device=x.device)
         q.expert_offset = expert_offset
         if R:
-            _check(_lib().cq_fp4_quantize_routed(x.data_ptr(), _DTYPE[x.dtype], ld, x.shape[0], route_token.data_ptr(), expert_offset.data_ptr(), groups, R, fmt, K,
-                                                 _at(tensor_scale), q.layout.data_ptr(), _stream()), "cq_fp4_quantize")
+            _check((_L or _lib()).cq_fp4_quantize_routed(at, dtype, ld, M, route_token.data_ptr(), expert_offset.data_ptr(), groups, R, fmt, K, _at(tensor_scale),
+                                                         q.layout.data_ptr(), stream), "cq_fp4_quantize")
     q.tensor_scale = tensor_scale
     return q
 
@@ -176,20 +207,23 @@ def cq_fp4_quantize(x: torch.Tensor, fmt: int, tensor_scale: torch.Tensor | None
 def cq_fp4_swiglu_quantize(h: torch.Tensor, fmt: int, tensor_scale: torch.Tensor | None = None, expert_offset: torch.Tensor | None = None,
                            out: Fp4Tensor | None = None) -> Fp4Tensor:
     """h [M, 2 I] (gate | up; bfloat16 or float16) -> silu(gate) * up, rounded to h's dtype, quantised.  expert_offset: the rows are routed."""
-    ld = _check_rows(h, "h")
-    _need(h.dtype != torch.float32 and h.shape[1] % 2 == 0, "h is [M, 2 I] in bfloat16 or float16")
-    M, K = h.shape[0], h.shape[1] // 2
+    M, K, ld, at, dtype = _check_rows(h, "h")
+    if dtype == 2 or K % 2:
+        raise CubicQuantError("h is [M, 2 I] in bfloat16 or float16")
+    K //= 2
     _check_format(fmt, K)
     _check_scale(tensor_scale, fmt)
+    groups = None
     if expert_offset is not None:
         _check_offset(expert_offset)
-    _here(h, tensor_scale, expert_offset, out.layout if out is not None else None)
-    groups = expert_offset.numel() - 1 if expert_offset is not None else None
+        groups = expert_offset.numel() - 1
+    stream = _here(h, tensor_scale, expert_offset, None if out is None else out.layout)
     q = _into(out, fmt, M, K, 1, groups, device=h.device)
     q.tensor_scale, q.expert_offset = tensor_scale, expert_offset
     if M:
-        _check(_lib().cq_fp4_swiglu_quantize(h.data_ptr(), _DTYPE[h.dtype], ld, fmt, M, K, _at(expert_offset), groups or 0, _at(tensor_scale), q.layout.data_ptr(), _stream()),
-               "cq_fp4_swiglu_quantize")
+        status = (_L or _lib()).cq_fp4_swiglu_quantize(at, dtype, ld, fmt, M, K, _at(expert_offset), groups or 0, _at(tensor_scale), q.layout.data_ptr(), stream)
+        if status != 0:
+            _check(status, "cq_fp4_swiglu_quantize")
     return q
 
 
@@ -198,11 +232,14 @@ def cq_fp4_dequantize(q: Fp4Tensor, dtype: torch.dtype = torch.bfloat16, out: to
     shape = (q.matrices, q.M, q.K) if q.matrices > 1 else (q.M, q.K)
     if out is None:
         out = (torch.zeros if q.groups else torch.empty)(shape, dtype=dtype, device=q.layout.device)
-    _need(out.dtype in _DTYPE and tuple(out.shape) == shape and out.is_contiguous() and out.data_ptr() % 16 == 0, f"out is a contiguous tensor of shape {shape}")
-    _here(q.layout, q.tensor_scale, q.expert_offset, out)
+    code, at = _DTYPE.get(out.dtype), out.data_ptr()
+    if code is None or out.shape != shape or at % 16 or not out.is_contiguous():
+        raise CubicQuantError(f"out is a contiguous tensor of shape {shape}")
+    stream = _here(q.layout, q.tensor_scale, q.expert_offset, out)
     if q.M:
-        _check(_lib().cq_fp4_dequantize(q.layout.data_ptr(), q.fmt, q.groups or q.matrices, q.M, q.K, _at(q.expert_offset), _at(q.tensor_scale), out.data_ptr(),
-                                        _DTYPE[out.dtype], _stream()), "cq_fp4_dequantize")
+        status = (_L or _lib()).cq_fp4_dequantize(q.layout.data_ptr(), q.fmt, q.groups or q.matrices, q.M, q.K, _at(q.expert_offset), _at(q.tensor_scale), at, code, stream)
+        if status != 0:
+            _check(status, "cq_fp4_dequantize")
     return out
 
 
@@ -212,50 +249,51 @@ def cq_fp4_workspace(w: Fp4Tensor, M: int) -> torch.Tensor:
     return torch.zeros(max(n, 512), dtype=torch.uint8, device=w.layout.device)
 
 
-def _product_args(w, x, M, tensor_scale, workspace, out):
-    """What the dense and the routed product check alike; returns (workspace, out, 16-bit output is binary16)."""
-    _need(isinstance(w, Fp4Tensor) and not w.groups, "w is a matrix of cq_fp4_pack or cq_fp4_quantize")
-    quantised = isinstance(x, Fp4Tensor)
-    if quantised:
-        _need(x.fmt == w.fmt and x.matrices == 1 and x.K == w.K, "x and w differ in format or K")
-        _need(tensor_scale is None, "x carries its own tensor scale")
-        dtype = out.dtype if out is not None else torch.bfloat16
-    else:
-        _need(x.dtype != torch.float32 and x.shape[1] == w.K, f"x is [M, {w.K}] in bfloat16 or float16")
-        _check_scale(tensor_scale, w.fmt)
-        dtype = x.dtype
-    dev = w.layout.device
+def _output(w, M, dtype, workspace, out, own_workspace):
+    """(workspace, out, address of out, code of its dtype), made where they are not given."""
     if out is None:
-        out = torch.empty((M, w.M), dtype=dtype, device=dev)
-    _need(out.dtype == dtype and dtype in (torch.bfloat16, torch.float16) and tuple(out.shape) == (M, w.M) and out.is_contiguous() and out.data_ptr() % 16 == 0,
-          f"out is a contiguous [{M}, {w.M}] tensor in the dtype of x")
+        out = torch.empty((M, w.M), dtype=dtype, device=w.layout.device)
+    code, at = _DTYPE.get(out.dtype), out.data_ptr()
+    if out.dtype != dtype or code == 2 or out.shape != (M, w.M) or at % 16 or not out.is_contiguous():
+        raise CubicQuantError(f"out is a contiguous [{M}, {w.M}] tensor of 16-byte alignment in the dtype of x, bfloat16 or float16")
     if workspace is None:
-        workspace = torch.zeros(512, dtype=torch.uint8, device=dev) if quantised else cq_fp4_workspace(w, M)
-    _need(workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace is a contiguous uint8 tensor")
-    return workspace, out, 1 if dtype == torch.float16 else 0
+        workspace = cq_fp4_workspace(w, M) if own_workspace else torch.zeros(512, dtype=torch.uint8, device=w.layout.device)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise CubicQuantError("workspace is a contiguous uint8 tensor")
+    return workspace, out, at, code
+
+
+def _check_quantised(w, x, tensor_scale):
+    _need(x.fmt == w.fmt and x.matrices == 1 and x.K == w.K, "x and w differ in format or K")
+    _need(tensor_scale is None, "x carries its own tensor scale")
 
 
 def cq_fp4_gemm(w: Fp4Tensor, x, tensor_scale: torch.Tensor | None = None, workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """y[M, N] = x W^T.  x: [M, K] in the model dtype (quantised on the way, NVFP4 with tensor_scale) or an Fp4Tensor; y has the dtype of x
-    (of out, or bfloat16)."""
-    M = x.M if isinstance(x, Fp4Tensor) else x.shape[0]
-    _need(w.matrices == 1, "several matrices: cq_fp4_gemm_routed")
+    (for an Fp4Tensor that of out, or bfloat16)."""
+    if w.matrices != 1 or w.groups:
+        raise CubicQuantError("w is one matrix of cq_fp4_pack or cq_fp4_quantize (several: cq_fp4_gemm_routed)")
     if isinstance(x, Fp4Tensor):
         _need(not x.groups, "routed rows: cq_fp4_gemm_routed")
-        workspace, out, f16 = _product_args(w, x, M, tensor_scale, workspace, out)
-        _here(w.layout, w.tensor_scale, x.layout, x.tensor_scale, workspace, out)
+        _check_quantised(w, x, tensor_scale)
+        M = x.M
+        workspace, out, at, f16 = _output(w, M, torch.bfloat16 if out is None else out.dtype, workspace, out, False)
+        stream = _here(w.layout, w.tensor_scale, x.layout, x.tensor_scale, workspace, out)
         if M:
-            status = _lib().cq_fp4_gemm(w.layout.data_ptr(), _at(w.tensor_scale), x.layout.data_ptr(), _at(x.tensor_scale), w.fmt, out.data_ptr(), f16, M, w.M, w.K,
-                                        workspace.data_ptr(), workspace.numel(), _stream())
+            status = (_L or _lib()).cq_fp4_gemm(w.layout.data_ptr(), _at(w.tensor_scale), x.layout.data_ptr(), _at(x.tensor_scale), w.fmt, at, f16, M, w.M, w.K,
+                                                workspace.data_ptr(), workspace.numel(), stream)
             if status != 0:
                 _check(status, "cq_fp4_gemm")
         return out
-    ld = _check_rows(x)
-    workspace, out, f16 = _product_args(w, x, M, tensor_scale, workspace, out)
-    _here(w.layout, w.tensor_scale, x, tensor_scale, workspace, out)
+    M, K, ld, x_at, dtype = _check_rows(x)
+    if dtype == 2 or K != w.K:
+        raise CubicQuantError(f"x is [M, {w.K}] in bfloat16 or float16")
+    _check_scale(tensor_scale, w.fmt)
+    workspace, out, at, f16 = _output(w, M, x.dtype, workspace, out, True)
+    stream = _here(w.layout, w.tensor_scale, x, tensor_scale, workspace, out)
     if M:
-        status = _lib().cq_fp4_linear(w.layout.data_ptr(), _at(w.tensor_scale), x.data_ptr(), ld, _at(tensor_scale), w.fmt, out.data_ptr(), f16, M, w.M, w.K,
-                                      workspace.data_ptr(), workspace.numel(), _stream())
+        status = (_L or _lib()).cq_fp4_linear(w.layout.data_ptr(), _at(w.tensor_scale), x_at, ld, _at(tensor_scale), w.fmt, at, f16, M, w.M, K, workspace.data_ptr(),
+                                              workspace.numel(), stream)
         if status != 0:
             _check(status, "cq_fp4_gemm")
     return out
@@ -266,23 +304,33 @@ def cq_fp4_gemm_routed(w: Fp4Tensor, x, route_token: torch.Tensor | None, expert
     """Route-major y[R, N]: rows [expert_offset[e], expert_offset[e + 1]) meet matrix e of w.  x: [T, K] in the model dtype with route_token
     (int32 [R] on the device), or an Fp4Tensor of R routed rows with route_token None.  expert_offset: int32 on the device; rows from
     its last value on are left as they were (in a new tensor: undefined)."""
+    if w.groups:
+        raise CubicQuantError("w holds the matrices of cq_fp4_pack or cq_fp4_quantize")
     _check_offset(expert_offset, w.matrices)
     if isinstance(x, Fp4Tensor):
         _need(route_token is None and x.groups == w.matrices, "x holds the routed rows of as many groups as w has matrices")
+        _check_quantised(w, x, tensor_scale)
         R = x.M
-        workspace, out, f16 = _product_args(w, x, R, tensor_scale, workspace, out)
-        _here(w.layout, w.tensor_scale, x.layout, x.tensor_scale, expert_offset, workspace, out)
+        workspace, out, at, f16 = _output(w, R, torch.bfloat16 if out is None else out.dtype, workspace, out, False)
+        stream = _here(w.layout, w.tensor_scale, x.layout, x.tensor_scale, expert_offset, workspace, out)
         if R:
-            _check(_lib().cq_fp4_gemm_routed(w.layout.data_ptr(), _at(w.tensor_scale), x.layout.data_ptr(), _at(x.tensor_scale), expert_offset.data_ptr(), w.matrices, w.fmt,
-                                             out.data_ptr(), f16, R, w.M, w.K, workspace.data_ptr(), workspace.numel(), _stream()), "cq_fp4_gemm_routed")
+            status = (_L or _lib()).cq_fp4_gemm_routed(w.layout.data_ptr(), _at(w.tensor_scale), x.layout.data_ptr(), _at(x.tensor_scale), expert_offset.data_ptr(), w.matrices,
+                                                       w.fmt, at, f16, R, w.M, w.K, workspace.data_ptr(), workspace.numel(), stream)
+            if status != 0:
+                _check(status, "cq_fp4_gemm_routed")
         return out
-    ld = _check_rows(x)
-    _need(route_token is not None and route_token.dtype == torch.int32 and route_token.dim() == 1 and route_token.is_contiguous(), "route_token is an int32 tensor")
+    T, K, ld, x_at, dtype = _check_rows(x)
+    if dtype == 2 or K != w.K:
+        raise CubicQuantError(f"x is [T, {w.K}] in bfloat16 or float16")
+    _check_scale(tensor_scale, w.fmt)
+    if route_token is None or route_token.dtype != torch.int32 or route_token.dim() != 1 or not route_token.is_contiguous():
+        raise CubicQuantError("route_token is an int32 tensor")
     R = route_token.numel()
-    workspace, out, f16 = _product_args(w, x, R, tensor_scale, workspace, out)
-    _here(w.layout, w.tensor_scale, x, tensor_scale, route_token, expert_offset, workspace, out)
+    workspace, out, at, f16 = _output(w, R, x.dtype, workspace, out, True)
+    stream = _here(w.layout, w.tensor_scale, x, tensor_scale, route_token, expert_offset, workspace, out)
     if R:
-        _check(_lib().cq_fp4_linear_routed(w.layout.data_ptr(), _at(w.tensor_scale), x.data_ptr(), ld, x.shape[0], route_token.data_ptr(), _at(tensor_scale),
-                                           expert_offset.data_ptr(), w.matrices, w.fmt, out.data_ptr(), f16, R, w.M, w.K, workspace.data_ptr(), workspace.numel(), _stream()),
-               "cq_fp4_gemm_routed")
+        status = (_L or _lib()).cq_fp4_linear_routed(w.layout.data_ptr(), _at(w.tensor_scale), x_at, ld, T, route_token.data_ptr(), _at(tensor_scale),
+                                                     expert_offset.data_ptr(), w.matrices, w.fmt, at, f16, R, w.M, w.K, workspace.data_ptr(), workspace.numel(), stream)
+        if status != 0:
+            _check(status, "cq_fp4_gemm_routed")
     return out

@@ -135,6 +135,8 @@ def test_swiglu_far_gates_and_subnormal_activations(fmt):
         gate = torch.linspace(-top, top, 16 * I).reshape(16, I)
         up = torch.tensor([1.0, -2.0, 1e-6, 3e4]).repeat(4)[:, None].expand(16, I)
         h = torch.cat([gate, up], dim=1).to(DTYPE[dtype])
+        if dtype == "bf16":
+            h[1, 0], h[2, 1], h[1, I], h[2, I + 1] = 3.3e38, 2.4e38, 0.5, 1e-20
         h[3, 7], h[5, I + 9], h[6, 2] = float("nan"), float("inf"), -float("inf")
         q = cq.cq_fp4_swiglu_quantize(h.cuda(), FMT[fmt])
         v = as64(h)
