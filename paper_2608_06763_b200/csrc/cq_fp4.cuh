@@ -41,31 +41,41 @@ __host__ __device__ inline int scale_offset(int r, int j) { return CODE_BYTES + 
 // ---- groups of routed rows ------------------------------------------------------------------
 // offset[e] .. offset[e + 1] are the rows of group e, as the router left them on the GPU.  What does not ascend, or leaves
 // [0, R], is brought back into it: the largest value so far, at most R.  One warp writes the offsets and the first row
-// block of each group (E + 1 values each); the block synchronises before it reads them.
-__device__ __forceinline__ void scan_groups(const int32_t *offset, int E, int R, int *s_off, int *s_blk) {
+// block of each group (E + 1 values each), and, for a product, its first tile (bt rows of x to a tile, `times` of them); the
+// block synchronises before it reads them.
+__device__ __forceinline__ void scan_groups(const int32_t *offset, int E, int R, int *s_off, int *s_blk, int *s_item = nullptr, int bt = 1, int times = 0) {
     const int lane = threadIdx.x & 31;
-    int top = 0, blk = 0;   // of what lies in front
+    int top = 0, blk = 0, item = 0;   // of what lies in front
     for (int e0 = 0; e0 <= E; e0 += 32) {
         const int e = e0 + lane;
-        int o = e <= E ? min(max(offset[e], 0), R) : 0;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int v = __shfl_up_sync(~0u, o, d);
-            if (lane >= d) o = max(o, v);
-        }
-        o = max(o, top);
+        int o = max(e <= E ? min(max(offset[e], 0), R) : 0, top);
         int before = __shfl_up_sync(~0u, o, 1);
         if (lane == 0) before = e0 == 0 ? o : top;
-        int b = (o - before + ROWS - 1) / ROWS;   // row blocks of the group that ends here
+        if (__any_sync(~0u, e <= E ? o < before : o != top)) {   // not ascending, or the last 32 of them
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int v = __shfl_up_sync(~0u, o, d);
+                if (lane >= d) o = max(o, v);
+            }
+            before = __shfl_up_sync(~0u, o, 1);
+            if (lane == 0) before = e0 == 0 ? o : top;
+        }
+        int b = (o - before + ROWS - 1) / ROWS, n = s_item ? (o - before + bt - 1) / bt : 0;   // row blocks and tiles of the group that ends here
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int v = __shfl_up_sync(~0u, b, d);
-            if (lane >= d) b += v;
+            const int v = __shfl_up_sync(~0u, b, d), u = __shfl_up_sync(~0u, n, d);
+            if (lane >= d) { b += v; n += u; }
         }
         b += blk;
-        if (e <= E) { s_off[e] = o; s_blk[e] = b; }
+        n += item;
+        if (e <= E) {
+            s_off[e] = o;
+            s_blk[e] = b;
+            if (s_item) s_item[e] = n * times;
+        }
         top = __shfl_sync(~0u, o, 31);
         blk = __shfl_sync(~0u, b, 31);
+        item = __shfl_sync(~0u, n, 31);
     }
 }
 // the group that a row or a tile belongs to: the last e with table[e] <= v (v < table[E])

@@ -25,8 +25,8 @@ struct GemmArgs {
 };
 
 // What a CTA computes.  ONE: 128 channels x up to 128 rows of x; TWO: a pair of CTAs 256 channels x up to 256 rows; FEW: 128 channels x up to 16
-// rows, which it quantises itself and keeps in shared memory.
-enum { ONE = 0, TWO = 1, FEW = 2 };
+// rows, which it quantises itself and keeps in shared memory; SMALL: 128 channels x up to 64 rows.
+enum { ONE = 0, TWO = 1, FEW = 2, SMALL = 3 };
 constexpr int FEW_ROWS = 16, FEW_TILES = 16, FEW_MOST = 64;   // rows, and k tiles of them, that fit beside the ring
 
 // D[tmem] (+)= A B, codes by shared-memory descriptors, scales in tensor memory.  PAIR: by the tensor cores of two SMs, each with 128 of
@@ -83,18 +83,21 @@ __device__ __forceinline__ uint16_t round_out(float v, bool f16) { return f16 ? 
 template <int FMT, int MODE, bool SPLIT>
 struct Shape {
     static constexpr bool PAIR = MODE == TWO;
-    static constexpr int BN = MODE == TWO ? 256 : MODE == ONE ? 128 : FEW_ROWS, CTAS = PAIR ? 2 : 1;
+    static constexpr int BN = MODE == TWO ? 256 : MODE == ONE ? 128 : MODE == SMALL ? 64 : FEW_ROWS, CTAS = PAIR ? 2 : 1;
     static constexpr int SB = scale_bytes(FMT), BLOCKS = PAIR ? 2 : 1;      // row blocks of x that a tile may touch
-    static constexpr int A_BYTES = CODE_BYTES + SB, B_BYTES = CODE_BYTES;   // codes of x in this CTA: half of a pair's
+    static constexpr int A_BYTES = CODE_BYTES + SB, B_BYTES = MODE == SMALL ? BN * 128 : CODE_BYTES;   // codes of x in this CTA: half of a pair's
     static constexpr int STAGE = A_BYTES + (MODE == FEW ? 0 : B_BYTES + BLOCKS * SB);
-    static constexpr int STAGES = MODE == FEW ? 8 : MODE == ONE && SPLIT ? 6 : 5;
+    static constexpr int STAGES = MODE == FEW ? 8 : MODE == SMALL ? 6 : MODE == ONE && SPLIT ? 4 : 5;
     static constexpr int ACCS = PAIR ? 1 : 2, ACC_COLS = BN < 32 ? 32 : BN;   // accumulators: while one is read the next tile fills the other
     static constexpr int ATOMS = SB / 512;                       // scale pieces of a row block and stage
     static constexpr int SF_COLS = ATOMS * 4 * (1 + BLOCKS);     // scale columns of a stage; each stage has its own
-    static constexpr int SF0 = ACCS * ACC_COLS;
+    // Up to 64 rows a stage's MMAs are short, and what bounds the stage is the warp that issues them (waiting, fencing, eight or twelve instructions,
+    // committing: 500 cycles).  Two warps take turns then, each with accumulators of its own, which are added at the end.
+    static constexpr int MMAS = MODE == FEW || MODE == SMALL ? 2 : 1;
+    static constexpr int SF0 = ACCS * MMAS * ACC_COLS;
     static constexpr int PITCH = 272;                            // bytes of a row of the staged output: 128 channels and a gap against bank conflicts
     static constexpr int X_CODES = FEW_ROWS * 128, X_BYTES = MODE == FEW ? FEW_TILES * (X_CODES + SB) : 0;   // FEW: codes of a k tile; all k tiles
-    static constexpr int OUT_BYTES = SPLIT ? 0 : (MODE == FEW ? 32 : 64) * PITCH;
+    static constexpr int OUT_BYTES = SPLIT ? 128 * (BN + 4) * 4 : (MODE == FEW ? 32 : 64) * PITCH;   // SPLIT: partial sums [run][channel][row of x, and a gap]
     static_assert(SF0 + STAGES * SF_COLS <= 512, "tensor memory");
     static constexpr size_t smem(int E, bool routed) { return (size_t)STAGES * STAGE + X_BYTES + OUT_BYTES + 256 + (routed ? 3 * (size_t)(E + 1) * 4 : 0); }
     static_assert(STAGES * STAGE + X_BYTES + OUT_BYTES + 256 + (MODE == FEW ? 0 : 12 * (MAX_EXPERTS + 1)) <= 232448, "shared memory");
@@ -115,6 +118,12 @@ __device__ __forceinline__ bool epilogue_any(bool v) {
     uint32_t r;
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)v) : "memory");
     return r != 0;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// sixteen bytes into the shared memory of a CTA of the cluster, counted there on `bar`
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
@@ -175,36 +184,89 @@ struct Tiles {
 };
 template <bool PAIR> __device__ __forceinline__ int columns_of(int rows) { return PAIR ? (rows + 31) & ~31 : (rows + 15) & ~15; }
 
+// SPLIT, the eight warps that write y: this CTA's partial sums to the CTAs that add them, then its own 128 / S channels of all runs, in their
+// order.  Sums arrive counted on a barrier, so nobody waits for the whole cluster in between.
+template <class SH>
+__device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, int lgS, int run, int k_tiles, int warp, int lane, uint8_t *part, uint64_t *sums, volatile int *dead) {
+    const int lgCW = 7 - lgS, CW = 1 << lgCW, pitch = ((t.rows + 15) & ~15) + 4;
+    const int quad = warp & 3, c = quad * 32 + lane, owner = c >> lgCW, tid = threadIdx.x - 128;
+    if (tid == 0) tc::mbar_arrive_expect_tx(sums, 128u * (uint32_t)((t.rows + 3) & ~3) * 4u);
+    tc::tc_fence_after();
+    __syncwarp();
+    cluster_wait();   // the others have started, and their barriers exist
+    const uint32_t to = tc::map_to_rank(part, owner) + (uint32_t)((run << lgCW) + (c & (CW - 1))) * pitch * 4, bar = tc::map_to_rank(sums, owner);
+    for (int c0 = (warp - 4) / 4 * 32; c0 < t.rows; c0 += 64) {
+        uint32_t v[32];
+        tc::tmem_ld32(c0 + ((uint32_t)(quad * 32) << 16), v);
+        if (SH::MMAS == 2 && k_tiles > 1) {   // the sums of the odd k tiles
+            uint32_t v1[32];
+            tc::tmem_ld32(SH::ACC_COLS + c0 + ((uint32_t)(quad * 32) << 16), v1);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(v1[i]));
+        } else {
+            tc::tmem_ld_wait();
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+            if (c0 + i < t.rows) send(to + (uint32_t)(c0 + i) * 4, bar, v[i], v[i + 1], v[i + 2], v[i + 3]);
+    }
+    __syncwarp();
+    cluster_arrive();
+    const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
+    if (!tc::mbar_wait(sums, 0, p.status, 58, tc::WAIT_LIMIT_CYCLES, dead)) { *dead = 1; return; }
+    const int mine = tid & (CW - 1);
+    const int64_t ch = (int64_t)t.nb * 128 + (run << lgCW) + mine;
+    uint16_t *out = p.y + (int64_t)t.yrow * p.N + ch;
+    for (int r = (tid >> lgCW) * 4; r < t.rows; r += (256 >> lgCW) * 4) {
+        const float *at = reinterpret_cast<const float *>(part) + mine * pitch + r;
+        float4 f = *reinterpret_cast<const float4 *>(at);
+        for (int s = 1; s < 1 << lgS; ++s) {
+            const float4 v = *reinterpret_cast<const float4 *>(at + ((s << lgCW) * pitch));
+            f.x += v.x; f.y += v.y; f.z += v.z; f.w += v.w;
+        }
+        if (ch < p.N) {
+            out[(int64_t)r * p.N] = round_out(f.x * alpha, p.f16);
+            if (r + 1 < t.rows) out[(int64_t)(r + 1) * p.N] = round_out(f.y * alpha, p.f16);
+            if (r + 2 < t.rows) out[(int64_t)(r + 2) * p.N] = round_out(f.z * alpha, p.f16);
+            if (r + 3 < t.rows) out[(int64_t)(r + 3) * p.N] = round_out(f.w * alpha, p.f16);
+        }
+    }
+}
+
 // Warps 0 and 2 bring tiles (bulk copies: 0 those of W, 2 those of x), warp 1 issues the MMAs (in the second CTA of a pair it tells the first
-// that its tiles are there), warp 3 reads the offsets of routed rows, warps 4 to 11 write y.
-// SPLIT: S CTAs (pairs) of a cluster share one output tile, each a run of its k tiles; the partial sums meet in the shared memory of the
-// cluster, where each of the S CTAs that hold the same 128 channels adds 128 / S of them in the order of the runs.  One tile a CTA
-// then; else CTAs (pairs) take tiles in turn.
+// that its tiles are there), warp 3 those of every second stage of small tiles, having read the offsets of routed rows, warps 4 to 11 write y.
+// SPLIT: 2^lgS CTAs of a cluster share one output tile, each a run of its k tiles; the partial sums meet in the shared memory of the
+// cluster, where each CTA adds 128 / S channels in the order of the runs.  One tile a CTA then; else CTAs (pairs) take tiles in turn.
 // FEW: warps 4 to 11 first quantise the rows for this CTA's k tiles, while the first weights are on their way.
 template <int FMT, int MODE, bool SPLIT>
-__global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int S, int64_t n_items) {
+__global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int lgS, int n_items) {
     using SH = Shape<FMT, MODE, SPLIT>;
     constexpr bool PAIR = SH::PAIR;
-    constexpr int ST = SH::STAGES, SB = SH::SB, ACCS = SH::ACCS, BN = SH::BN, CTAS = SH::CTAS, ACC_COLS = SH::ACC_COLS;
+    static_assert(!(PAIR && SPLIT), "pairs take whole tiles");
+    constexpr int ST = SH::STAGES, SB = SH::SB, ACCS = SH::ACCS, BN = SH::BN, CTAS = SH::CTAS, ACC_COLS = SH::ACC_COLS, MMAS = SH::MMAS;
     constexpr uint32_t TMEM = 0;   // a CTA takes all of tensor memory: its first column is column 0
     extern __shared__ __align__(1024) uint8_t ring[];   // the swizzle counts address bits from 1024 on
     uint8_t *x_codes = ring + ST * SH::STAGE, *x_scales = x_codes + FEW_TILES * SH::X_CODES;
     uint8_t *staged = x_codes + SH::X_BYTES;
     uint64_t *full = reinterpret_cast<uint64_t *>(staged + SH::OUT_BYTES), *empty = full + ST, *acc_full = empty + ST, *acc_empty = acc_full + ACCS;
-    uint64_t *drained = acc_empty + ACCS, *x_ready = drained + 1;
-    uint32_t *s_tmem = reinterpret_cast<uint32_t *>(x_ready + 1);
+    uint64_t *drained = acc_empty + ACCS, *x_ready = drained + MMAS, *sums = x_ready + 1;
+    uint32_t *s_tmem = reinterpret_cast<uint32_t *>(sums + 1);
     volatile int *dead = reinterpret_cast<volatile int *>(s_tmem + 1);
     int *s_off = reinterpret_cast<int *>(staged + SH::OUT_BYTES + 256), *s_blk = s_off + p.E + 1, *s_item = s_blk + p.E + 1;
-    static_assert((2 * ST + 2 * ACCS + 2) * 8 + 8 <= 256, "barriers");
+    static_assert((2 * ST + 2 * ACCS + MMAS + 2) * 8 + 8 <= 256, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cluster_rank = PAIR || SPLIT ? (int)tc::cluster_rank() : 0;
-    const int half = PAIR ? cluster_rank & 1 : 0, run = cluster_rank / CTAS;   // which 128 channels of the pair; which run of k
+    // From the block's number, not the cluster's registers, and by shifts: what branches and addresses of the issuing warp hang on is uniform.
+    const int lgC = PAIR ? 1 : SPLIT ? lgS : 0, cluster_rank = blockIdx.x & ((1 << lgC) - 1), unit = blockIdx.x >> lgC, units = gridDim.x >> lgC;
+    const int half = PAIR ? cluster_rank : 0, run = SPLIT ? cluster_rank : 0;   // which 128 channels of the pair; which run of k
+    const int k0 = SPLIT ? p.KT * run >> lgS : 0, k1 = SPLIT ? p.KT * (run + 1) >> lgS : p.KT;   // this CTA's k tiles
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < ST; ++i) { tc::mbar_init(&full[i], MODE == FEW ? 1 : PAIR && half == 0 ? 3 : 2); tc::mbar_init(&empty[i], 1); }   // a pair's first CTA also waits for the other's tiles
-        for (int i = 0; i < ACCS; ++i) { tc::mbar_init(&acc_full[i], 1); tc::mbar_init(&acc_empty[i], 8 * CTAS); }
-        tc::mbar_init(drained, 1);
+        for (int i = 0; i < ACCS; ++i) { tc::mbar_init(&acc_full[i], MMAS); tc::mbar_init(&acc_empty[i], 8 * CTAS); }
+        for (int i = 0; i < MMAS; ++i) tc::mbar_init(&drained[i], 1);
         tc::mbar_init(x_ready, 8);
+        tc::mbar_init(sums, 1);
         *dead = 0;
         tc::fence_barrier_init();
     }
@@ -212,33 +274,19 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         if (PAIR) tc::tmem_alloc_pair(s_tmem, 512);
         else { tc::tmem_alloc(s_tmem, 512); tc::tmem_relinquish(); }
     }
-    tc::wait_for_previous_kernel();
-    if (p.offset && warp == 3) {
-        scan_groups(p.offset, p.E, p.M, s_off, s_blk);
-        __syncwarp();
-        const int nbu = PAIR ? (p.NB + 1) >> 1 : p.NB;
-        int sum = 0;   // tiles in front of each group
-        for (int e0 = 0; e0 <= p.E; e0 += 32) {
-            const int e = e0 + lane;
-            int v = e > 0 && e <= p.E ? nbu * ((s_off[e] - s_off[e - 1] + p.bt - 1) / p.bt) : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int u = __shfl_up_sync(~0u, v, d);
-                if (lane >= d) v += u;
-            }
-            v += sum;
-            if (e <= p.E) s_item[e] = v;
-            sum = __shfl_sync(~0u, v, 31);
-        }
+    if (!p.offset && threadIdx.x == 0 && unit < n_items) {   // the first weights on their way to L2, which sees what the kernel in front may still write
+        const int nb = min(item_of<PAIR>(p, unit, nullptr, nullptr, nullptr).nb * CTAS + half, p.NB - 1);
+        for (int kt = k0; kt < k1 && kt < k0 + ST; ++kt) tc::prefetch_l2(p.w + ((int64_t)nb * p.KT + kt) * tile_bytes(FMT), SH::A_BYTES);
     }
+    tc::wait_for_previous_kernel();
+    if (p.offset && warp == 3) scan_groups(p.offset, p.E, p.M, s_off, s_blk, s_item, p.bt, PAIR ? (p.NB + 1) >> 1 : p.NB);
     tc::tc_fence_before();
     __syncthreads();
     if (PAIR) tc::cluster_sync();   // the partner's barriers exist before anything arrives on them
+    if (SPLIT) cluster_arrive();
     tc::tc_fence_after();
-    const int items = p.offset ? s_item[p.E] : (int)n_items;
-    const int unit = (int)(blockIdx.x / (CTAS * (SPLIT ? S : 1))), units = (int)(gridDim.x / (CTAS * (SPLIT ? S : 1)));
+    const int items = p.offset ? __reduce_max_sync(~0u, s_item[p.E]) : n_items;   // (a reduction's result is uniform)
     const int stride = SPLIT ? items : units;   // split: one tile
-    const int k0 = SPLIT ? (int)((int64_t)p.KT * run / S) : 0, k1 = SPLIT ? (int)((int64_t)p.KT * (run + 1) / S) : p.KT;   // this CTA's k tiles
 
     Tiles<PAIR> tiles{p, unit, stride, items, s_off, s_blk, s_item, {}};
     int it = 0;   // stages filled (warps 0 and 2) or used (warp 1) so far
@@ -275,63 +323,68 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         }
         if (!ok && lane == 0) *dead = 1;
         __syncwarp();
-    } else if (warp == 1) {
-        // The whole warp walks the loops and one lane issues: what the instructions take stays in uniform registers.
+    } else if (warp == 1 || (warp == 3 && MMAS == 2)) {
+        // The whole warp walks the loops and one lane issues: what the instructions take stays in uniform registers (a stage takes twice
+        // as long where a lane of its own does it all).
+        const int odd = warp >> 1;   // MMAS == 2: which of a tile's k tiles are this warp's
         uint32_t s = 0, phase = 0;
         bool ok = MODE != FEW || uniform_wait(x_ready, 0, p.status, 57, dead);
         for (int local = 0; ok && tiles.has(local); ++local) {
             const Item t = tiles.at(local);
-            const uint32_t n = columns_of<PAIR>(t.rows), sf_row = t.off / 32;
-            const int acc = local % ACCS;
-            const uint32_t d = TMEM + acc * ACC_COLS, desc = idesc_fp4<FMT, PAIR>(n, 0);
+            const uint32_t n = MODE == FEW ? FEW_ROWS : __reduce_max_sync(~0u, columns_of<PAIR>(t.rows)), sf_row = PAIR ? __reduce_max_sync(~0u, t.off / 32) : 0;
+            const int acc = local & (ACCS - 1);
+            const uint32_t d = TMEM + (acc * MMAS + odd) * ACC_COLS, desc = idesc_fp4<FMT, PAIR>(n, 0);
             if (half == 0 && local >= ACCS) ok = uniform_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 53, dead);
             tc::tc_fence_after();
-            for (int kt = k0; kt < k1 && ok; ++kt, ++it) {
-                ok = uniform_wait(&full[s], phase, p.status, 54, dead);
-                if (!ok) break;
-                if (PAIR && half == 1) {
-                    if (lane == 0) tc::mbar_arrive_cluster(tc::map_to_rank(&full[s], cluster_rank & ~1));
-                } else {
-                    tc::tc_fence_after();
-                    const uint32_t a = tc::smem_u32(ring) + s * SH::STAGE, sfa = TMEM + SH::SF0 + s * SH::SF_COLS, sfb = sfa + SH::ATOMS * 4, sfn = sfb + sf_row;
-                    const uint64_t da = tc::smem_desc_sw128(a), dsa = smem_desc_plain(a + CODE_BYTES);
-                    const uint64_t db = MODE == FEW ? tc::smem_desc_sw128(tc::smem_u32(x_codes) + (kt - k0) * SH::X_CODES) : da + SH::A_BYTES / 16;
-                    const uint64_t dsb = MODE == FEW ? smem_desc_plain(tc::smem_u32(x_scales) + (kt - k0) * SB) : dsa + (SB + SH::B_BYTES) / 16;
-                    const int steps = p.steps - 4 * kt;
-                    if (tc::elect_one()) {
+            for (int kt = k0; kt < k1 && ok; ++kt) {
+                if (MMAS == 1 || ((kt - k0) & 1) == odd) {
+                    ok = uniform_wait(&full[s], phase, p.status, 54, dead);
+                    if (!ok) break;
+                    if (PAIR && half == 1) {
+                        if (lane == 0) tc::mbar_arrive_cluster(tc::map_to_rank(&full[s], cluster_rank & ~1));
+                    } else {
+                        tc::tc_fence_after();
+                        const uint32_t a = tc::smem_u32(ring) + s * SH::STAGE, sfa = TMEM + SH::SF0 + s * SH::SF_COLS, sfb = sfa + SH::ATOMS * 4, sfn = sfb + sf_row;
+                        const uint64_t da = tc::smem_desc_sw128(a), dsa = smem_desc_plain(a + CODE_BYTES);
+                        const uint64_t db = MODE == FEW ? tc::smem_desc_sw128(tc::smem_u32(x_codes) + (kt - k0) * SH::X_CODES) : da + SH::A_BYTES / 16;
+                        const uint64_t dsb = MODE == FEW ? smem_desc_plain(tc::smem_u32(x_scales) + (kt - k0) * SB) : dsa + (SB + SH::B_BYTES) / 16;
+                        const int steps = p.steps - 4 * kt;
+                        if (tc::elect_one()) {
 #pragma unroll
-                        for (int j = 0; j < SH::ATOMS; ++j) {
-                            copy_scales<PAIR>(sfa + j * 4, dsa + j * 32);
+                            for (int j = 0; j < SH::ATOMS; ++j) {
+                                copy_scales<PAIR>(sfa + j * 4, dsa + j * 32);
 #pragma unroll
-                            for (int h = 0; h < SH::BLOCKS; ++h) copy_scales<PAIR>(sfb + (j * SH::BLOCKS + h) * 4, dsb + j * 32 + h * (SB / 16));
-                        }
+                                for (int h = 0; h < SH::BLOCKS; ++h) copy_scales<PAIR>(sfb + (j * SH::BLOCKS + h) * 4, dsb + j * 32 + h * (SB / 16));
+                            }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int atom = FMT == MX ? j / 2 : j;
-                            const uint32_t sf = FMT == MX ? (j & 1) * 2 : 0;
-                            if (j == 0 || j < steps)
-                                umma_fp4<FMT, PAIR>(d, da + 2 * j, db + 2 * j, desc | sf << 4 | sf << 29, sfa + atom * 4, sfn + atom * 4 * SH::BLOCKS, j > 0 || kt > k0);
+                            for (int j = 0; j < 4; ++j) {
+                                const int atom = FMT == MX ? j / 2 : j;
+                                const uint32_t sf = FMT == MX ? (j & 1) * 2 : 0;
+                                if (j == 0 || j < steps)
+                                    umma_fp4<FMT, PAIR>(d, da + 2 * j, db + 2 * j, desc | sf << 4 | sf << 29, sfa + atom * 4, sfn + atom * 4 * SH::BLOCKS, j > 0 || kt >= k0 + MMAS);
+                            }
+                            if (PAIR) commit_to_pair(&empty[s], cluster_rank);
+                            else tc::umma_commit(&empty[s]);
+                            if (kt >= k1 - MMAS) {
+                                if (PAIR) commit_to_pair(&acc_full[acc], cluster_rank);
+                                else tc::umma_commit(&acc_full[acc]);
+                            }
                         }
-                        if (PAIR) commit_to_pair(&empty[s], cluster_rank);
-                        else tc::umma_commit(&empty[s]);
-                        if (kt == k1 - 1) {
-                            if (PAIR) commit_to_pair(&acc_full[acc], cluster_rank);
-                            else tc::umma_commit(&acc_full[acc]);
-                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
                 if (++s == ST) { s = 0; phase ^= 1; }
             }
+            if (MMAS == 2 && ok && k1 - k0 == 1 && odd == 1 && lane == 0) tc::mbar_arrive(&acc_full[acc]);   // nothing to add
         }
         if (!ok && lane == 0) *dead = 1;
         if (!ok && half == 0) {   // what was issued completes before tensor memory is given back
             if (tc::elect_one()) {
-                if (PAIR) commit_to_pair(drained, cluster_rank);
-                else tc::umma_commit(drained);
+                if (PAIR) commit_to_pair(&drained[odd], cluster_rank);
+                else tc::umma_commit(&drained[odd]);
             }
             __syncwarp();
-            tc::mbar_wait(drained, 0, p.status, 55);
+            tc::mbar_wait(&drained[odd], 0, p.status, 55);
         }
         __syncwarp();
     } else if (warp >= 4) {
@@ -339,12 +392,13 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         // then 64 rows of y at a time go through shared memory, where the 8x8 matrices are turned round, and out as whole rows.
         if constexpr (MODE == FEW) {
             const int tid = threadIdx.x - 128, units = (k1 - k0) * p.M * 16, KU = (int)(p.K >> 4);
-            const float r = FMT == NV && p.x_scale ? __fdiv_rn(1.0f, *p.x_scale) : 1.0f;
+            const float g = FMT == NV && p.x_scale ? *p.x_scale : 1.0f;
             for (int i0 = 0; i0 < units; i0 += 256) {   // whole warps: they exchange scales
                 const int i = i0 + tid, u = i & 15, line = i >> 4, kt = line / p.M, row = line - kt * p.M, unit = (k0 + kt) * 16 + u;
                 const bool live = i < units, read = live && unit < KU;
                 const uint16_t *src = p.xr + row * p.ldx + (int64_t)unit * 16;
                 const uint4 a = read ? load16(src) : make_uint4(0, 0, 0, 0), b = read ? load16(src + 8) : make_uint4(0, 0, 0, 0);
+                const float r = __fdiv_rn(1.0f, g);
                 uint32_t scale;
                 const uint2 codes = p.f16 ? quantize_unit<FMT, DT_F16>(a, b, r, scale) : quantize_unit<FMT, DT_BF16>(a, b, r, scale);
                 if (unit >= KU) scale = 0;   // behind K
@@ -363,10 +417,17 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         const int quad = warp & 3, part = (warp - 4) >> 2;   // the 32 lanes of tensor memory that a warp may read; its half of 64 columns
         for (int local = 0; tiles.has(local); ++local) {
             const Item t = tiles.at(local);
-            const int acc = local % ACCS;
+            const int acc = local & (ACCS - 1);
             const bool ok = tc::mbar_wait(&acc_full[acc], (local / ACCS) & 1, p.status, 56, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
-            if (epilogue_any(!ok)) { *dead = 1; break; }
-            if constexpr (SPLIT) break;
+            if (epilogue_any(!ok)) {
+                *dead = 1;
+                if (SPLIT) { cluster_wait(); cluster_arrive(); }
+                break;
+            }
+            if constexpr (SPLIT) {
+                send_and_add<SH>(p, t, lgS, run, k1 - k0, warp, lane, staged, sums, dead);
+                break;
+            }
             tc::tc_fence_after();
             const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
             const int nb = t.nb * CTAS + half;
@@ -376,10 +437,22 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             for (int g = 0; g < GROUPS; ++g) {
                 if (g * 64 + part * 32 < t.rows) {
                     uint32_t lo[16], hi[16];
-                    const uint32_t from = TMEM + acc * ACC_COLS + g * 64 + part * 32 + ((uint32_t)(quad * 32) << 16);
+                    const uint32_t from = TMEM + acc * MMAS * ACC_COLS + g * 64 + part * 32 + ((uint32_t)(quad * 32) << 16);
                     tmem_ld_16x32(from, lo);
                     tmem_ld_16x32(from + (16u << 16), hi);
-                    tc::tmem_ld_wait();
+                    if (MMAS == 2 && k1 - k0 > 1) {   // the sums of the odd k tiles
+                        uint32_t lo1[16], hi1[16];
+                        tmem_ld_16x32(from + ACC_COLS, lo1);
+                        tmem_ld_16x32(from + ACC_COLS + (16u << 16), hi1);
+                        tc::tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            lo[i] = __float_as_uint(__uint_as_float(lo[i]) + __uint_as_float(lo1[i]));
+                            hi[i] = __float_as_uint(__uint_as_float(hi[i]) + __uint_as_float(hi1[i]));
+                        }
+                    } else {
+                        tc::tmem_ld_wait();
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         out16[g][4 * i] = pack_out(lo[4 * i], lo[4 * i + 1], alpha, p.f16);
@@ -423,56 +496,18 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         }
     }
 
-    if constexpr (SPLIT) {
-        // every CTA's MMAs are done (the warps that read tensor memory waited for them), so the rings are free for partial sums
-        const Item t = tiles.at(0);
-        const int CW = 128 / S, pitch = columns_of<PAIR>(t.rows) + 4;
-        __syncthreads();
-        tc::cluster_sync();
-        const bool alive = !*dead;
-        float *part = reinterpret_cast<float *>(ring);   // [run that sent it][channel of mine][row of x]
-        if (warp >= 4 && alive) {
-            tc::tc_fence_after();
-            const int quad = warp & 3, c = quad * 32 + lane, owner = c / CW;
-            const uint32_t to = tc::map_to_rank(part, owner * CTAS + half) + (uint32_t)(run * CW + c - owner * CW) * pitch * 4;
-            for (int c0 = (warp - 4) / 4 * 32; c0 < t.rows; c0 += 64) {
-                uint32_t v[32];
-                tc::tmem_ld32(TMEM + c0 + ((uint32_t)(quad * 32) << 16), v);
-                tc::tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 32; i += 4)
-                    if (c0 + i < t.rows)
-                        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(c0 + i) * 4), "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]) : "memory");
-            }
-        }
+    if (SPLIT && warp < 4) {   // the others have done so on their way
         __syncwarp();
-        tc::cluster_sync();
-        if (alive) {
-            const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
-            const int c = threadIdx.x % CW;   // CW a power of two
-            const int64_t ch = (int64_t)(t.nb * CTAS + half) * 128 + run * CW + c;
-            const float *mine = part + c * pitch;
-            uint16_t *out = p.y + (int64_t)t.yrow * p.N + ch;
-            for (int r = threadIdx.x / CW * 4; r < t.rows; r += 384 / CW * 4) {
-                float4 f = *reinterpret_cast<const float4 *>(mine + r);
-                for (int s = 1; s < S; ++s) {
-                    const float4 v = *reinterpret_cast<const float4 *>(mine + (int64_t)s * CW * pitch + r);
-                    f.x += v.x; f.y += v.y; f.z += v.z; f.w += v.w;
-                }
-                if (ch < p.N) {
-                    out[(int64_t)r * p.N] = round_out(f.x * alpha, p.f16);
-                    if (r + 1 < t.rows) out[(int64_t)(r + 1) * p.N] = round_out(f.y * alpha, p.f16);
-                    if (r + 2 < t.rows) out[(int64_t)(r + 2) * p.N] = round_out(f.z * alpha, p.f16);
-                    if (r + 3 < t.rows) out[(int64_t)(r + 3) * p.N] = round_out(f.w * alpha, p.f16);
-                }
-            }
-        }
+        cluster_wait();
+        cluster_arrive();
     }
     tc::tc_fence_before();
     __syncthreads();
     if (*dead && (warp == 0 || warp == 2))   // a wait gave up: copies in flight land before the shared memory goes away
         for (int i = it < ST ? 0 : it - ST; i < it; ++i) tc::mbar_wait(&full[i % ST], (i / ST) & 1, p.status, 52);
-    if (PAIR) { __syncwarp(); tc::cluster_sync(); }   // nothing of the pair is in flight towards a CTA that has left
+    __syncwarp();
+    if (PAIR) tc::cluster_sync();   // nothing of the pair is in flight towards a CTA that has left
+    if (SPLIT) cluster_wait();      // nor are partial sums
     if (warp == 1) {
         tc::tc_fence_after();
         if (PAIR) tc::tmem_dealloc_pair(TMEM, 512);
@@ -481,12 +516,12 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
 }
 
 template <int FMT, int MODE, bool SPLIT>
-static cudaError_t launch(const GemmArgs &p, int S, int64_t items, unsigned grid, cudaStream_t st) {
+static cudaError_t launch(const GemmArgs &p, int lgS, int64_t items, unsigned grid, cudaStream_t st) {
     using SH = Shape<FMT, MODE, SPLIT>;
     static std::atomic<uint64_t> done{0};
     const cudaError_t e = ensure_func_attr(fp4_gemm_kernel<FMT, MODE, SPLIT>, done, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SH::smem(MAX_EXPERTS, MODE != FEW));
     if (e != cudaSuccess) return e;
-    return launch_overlapped(fp4_gemm_kernel<FMT, MODE, SPLIT>, dim3(grid), 384u, SH::smem(p.E, p.offset != nullptr), st, SH::CTAS * (SPLIT ? S : 1), true, p, S, items);
+    return launch_overlapped(fp4_gemm_kernel<FMT, MODE, SPLIT>, dim3(grid), 384u, SH::smem(p.E, p.offset != nullptr), st, SH::CTAS << (SPLIT ? lgS : 0), true, p, lgS, (int)items);
 }
 
 }  // namespace fp4
@@ -495,10 +530,10 @@ using namespace fp4;
 
 // Runs of k that an output tile of few row blocks is cut into, while the GPU has places for them.  Eight CTAs to a cluster leave SMs
 // without a cluster that fits (4096 x 4096, one row: 14.6 us with eight, 5.9 with four).
-static int runs_of(int tiles, int KT, int places) {
-    int S = 1;
-    while (S < 4 && 2 * S <= KT && 2 * S * tiles <= places) S *= 2;
-    return S;
+static int lg_runs_of(int tiles, int KT, int places) {
+    int lg = 0;
+    while (lg < 2 && 2 << lg <= KT && (int64_t)(2 << lg) * tiles <= places) ++lg;
+    return lg;
 }
 static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scale, uint16_t *y, int64_t M, int64_t N, int64_t K, bool f16, int *status) {
     GemmArgs p{};
@@ -510,17 +545,18 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
 }
 
 bool fp4_few_ok(int64_t M, int64_t N, int64_t K) {
-    const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
-    return M <= FEW_ROWS && most <= FEW_TILES && M * most <= FEW_MOST;
+    if (M > FEW_ROWS) return false;
+    const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
+    return most <= FEW_TILES && M * most <= FEW_MOST;
 }
 cudaError_t launch_fp4_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, const float *x_scale, int fmt, uint16_t *y, int64_t M, int64_t N, int64_t K,
                            bool f16, int *status, cudaStream_t st) {
     GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
     p.xr = x; p.ldx = ldx; p.bt = FEW_ROWS; p.token_tiles = 1;
-    const int places = sm_count(), S = runs_of(p.NB, p.KT, places);
-    const unsigned grid = (unsigned)(S > 1 ? p.NB * S : p.NB < places ? p.NB : places);
-    if (fmt == MX) return S > 1 ? launch<MX, FEW, true>(p, S, p.NB, grid, st) : launch<MX, FEW, false>(p, 1, p.NB, grid, st);
-    return S > 1 ? launch<NV, FEW, true>(p, S, p.NB, grid, st) : launch<NV, FEW, false>(p, 1, p.NB, grid, st);
+    const int places = sm_count(), lg = lg_runs_of(p.NB, p.KT, places);
+    const unsigned grid = (unsigned)(lg ? p.NB << lg : p.NB < places ? p.NB : places);
+    if (fmt == MX) return lg ? launch<MX, FEW, true>(p, lg, p.NB, grid, st) : launch<MX, FEW, false>(p, 0, p.NB, grid, st);
+    return lg ? launch<NV, FEW, true>(p, lg, p.NB, grid, st) : launch<NV, FEW, false>(p, 0, p.NB, grid, st);
 }
 
 cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, int fmt, uint16_t *y, int64_t M,
@@ -528,17 +564,19 @@ cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, 
     GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
     p.x = (const uint8_t *)x; p.offset = offset; p.E = E;
     const int sms = sm_count();
-    int S = 1, pair = (offset ? M / E : M) > 256, bt = pair ? 256 : 128;
-    if (!offset && M <= 256) S = runs_of(p.NB * (int)((M + 127) / 128), p.KT, sms);
-    p.bt = bt;
-    p.token_tiles = (int)((M + bt - 1) / bt);
-    const int ctas = pair ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sms / ctas;
+    const int64_t rows = offset ? M / E : M;   // routed: on average, as the loads are not known here
+    const int mode = rows > 256 ? TWO : rows > 48 ? ONE : SMALL;
+    p.bt = mode == TWO ? 256 : mode == ONE ? 128 : 64;
+    p.token_tiles = (int)((M + p.bt - 1) / p.bt);
+    const int ctas = mode == TWO ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sms / ctas;
+    const int lg = offset || mode == TWO ? 0 : lg_runs_of(p.NB * p.token_tiles, p.KT, sms);
     const int64_t items = (int64_t)nbu * p.token_tiles;
-    const unsigned grid = (unsigned)(S > 1 ? items * S : offset ? places : items < places ? items : places) * ctas;
+    const unsigned grid = (unsigned)(lg ? items << lg : offset ? places : items < places ? items : places) * ctas;
     auto go = [&](auto f) {
         constexpr int F = decltype(f)::value;
-        if (S > 1) return pair ? launch<F, TWO, true>(p, S, items, grid, st) : launch<F, ONE, true>(p, S, items, grid, st);
-        return pair ? launch<F, TWO, false>(p, 1, items, grid, st) : launch<F, ONE, false>(p, 1, items, grid, st);
+        if (mode == TWO) return launch<F, TWO, false>(p, 0, items, grid, st);
+        if (mode == ONE) return lg ? launch<F, ONE, true>(p, lg, items, grid, st) : launch<F, ONE, false>(p, 0, items, grid, st);
+        return lg ? launch<F, SMALL, true>(p, lg, items, grid, st) : launch<F, SMALL, false>(p, 0, items, grid, st);
     };
     return fmt == MX ? go(std::integral_constant<int, MX>{}) : go(std::integral_constant<int, NV>{});
 }
