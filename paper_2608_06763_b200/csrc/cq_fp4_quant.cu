@@ -170,7 +170,30 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     const __half2 p = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
 }
-__device__ __noinline__ float gated_in_64_bits(float g, float u) { return (float)((double)g * (double)u / (1.0 + exp(-(double)g))); }
+__device__ __forceinline__ float gated_in_64_bits(float g, float u) { return (float)((double)g * (double)u / (1.0 + exp(-(double)g))); }
+// The units of the lanes that ask for it, one after another: a lane for each of the sixteen activations (a lane by itself would take
+// sixteen times as long, and the rest of its warp would wait).
+template <int DT>
+__device__ __forceinline__ void settle_in_64_bits(bool ask, const uint32_t *gw, const uint32_t *uw, uint32_t *act) {
+    const int lane = threadIdx.x & 31, mine = (lane & 15) >> 1;
+    for (uint32_t left = __ballot_sync(~0u, ask); left; left &= left - 1) {
+        const int from = __ffs(left) - 1;
+        uint32_t g = 0, u = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t a = __shfl_sync(~0u, gw[i], from), b = __shfl_sync(~0u, uw[i], from);
+            if (mine == i) { g = a; u = b; }
+        }
+        if (lane & 1) { g >>= 16; u >>= 16; }
+        const float y = gated_in_64_bits(value_of<DT>(&g, 0), value_of<DT>(&u, 0));
+        const uint32_t both = pack16<DT>(y, __shfl_down_sync(~0u, y, 1));   // in the even lanes
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t t = __shfl_sync(~0u, both, 2 * i);
+            if (lane == from) act[i] = t;
+        }
+    }
+}
 __device__ __forceinline__ float ulps_away(float v, int n) { return __uint_as_float(__float_as_uint(v) + n); }   // n > 0: away from zero
 // two activations
 __device__ __forceinline__ void gated_in_32_bits(float g0, float g1, float u0, float u1, float &y0, float &y1) {
@@ -254,12 +277,7 @@ __global__ void __launch_bounds__(256, 4) swiglu_quantize_kernel(const uint16_t 
 #pragma unroll
                 for (int k = 0; k < 16; ++k) { v0[k] = value_of<DT>(a0, k); v1[k] = value_of<DT>(a1, k); }
                 const uint2 c0 = round_codes(v0, f0), c1 = round_codes(v1, f1);
-                if (open && (far || s0 != s1 || c0.x != c1.x || c0.y != c1.y)) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (far || a0[k] != a1[k])
-                            act[k] = pack16<DT>(gated_in_64_bits(value_of<DT>(gw, 2 * k), value_of<DT>(uw, 2 * k)), gated_in_64_bits(value_of<DT>(gw, 2 * k + 1), value_of<DT>(uw, 2 * k + 1)));
-                }
+                settle_in_64_bits<DT>(open && (far || s0 != s1 || c0.x != c1.x || c0.y != c1.y), gw, uw, act);
                 top = top_of_block<FMT>(top_of_16bit<DT>(act));
             }
             float factor, v[16];
