@@ -269,6 +269,7 @@ int cq_encode(const float *W, int B, int G, int64_t N, int64_t K, int objective,
  * rows behind the last of a matrix or of a group are never written and reach no result.
  * E matrices of one shape (experts) lie one after another in one layout; their tensor scales are E floats.
  * dtype: CQ_BF16, CQ_F16, CQ_F32.  Rows of x are `ldx` elements apart, 16-byte aligned.
+ * A workspace (a layout that is written) serves one call at a time: calls that may overlap on the GPU take their own.
  * Errors as above; CQ_ERR_UNSUPPORTED: K not a multiple of the block, more than 512 groups, sizes above 2^30. */
 enum { CQ_MXFP4 = 0, CQ_NVFP4 = 1 };
 enum { CQ_BF16 = 0, CQ_F16 = 1, CQ_F32 = 2 };

@@ -67,7 +67,7 @@ int product(const void *w, const float *w_scale, const void *x, int64_t ldx, int
     if (!quantised) CQ_TRY(check_rows(x, dtype, ldx, K));
     if (misaligned(w) || misaligned(x) || misaligned(y) || misaligned(workspace)) return CQ_ERR_ALIGNMENT;
     const int64_t blocks = routed ? routed_blocks(E, M) : blocks_of(M);
-    if (blocks_of(N) * blocks > MOST) return CQ_ERR_UNSUPPORTED;
+    if (blocks_of(N) * blocks > MOST / 2) return CQ_ERR_UNSUPPORTED;   // two tiles of 64 rows to a row block, counted in 32 bits
     if (workspace_bytes < STATUS_BYTES + (quantised ? 0 : bytes_of(fmt, blocks, K))) return CQ_ERR_WORKSPACE;
     CQ_TRY(check_arch());
     cudaStream_t st = (cudaStream_t)stream;

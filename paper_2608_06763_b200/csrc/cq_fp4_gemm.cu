@@ -185,16 +185,22 @@ struct Tiles {
 template <bool PAIR> __device__ __forceinline__ int columns_of(int rows) { return PAIR ? (rows + 31) & ~31 : (rows + 15) & ~15; }
 
 // SPLIT, the eight warps that write y: this CTA's partial sums to the CTAs that add them, then its own 128 / S channels of all runs, in their
-// order.  Sums arrive counted on a barrier, so nobody waits for the whole cluster in between.
+// order.  Sums arrive counted on a barrier, so nobody waits for the whole cluster in between.  Few rows are sent from the registers;
+// more go through the ring, which nobody needs any more, and from there in one copy to each CTA (128 rows: 6000 cycles in pieces of
+// sixteen bytes, 2500 so).
 template <class SH>
-__device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, int lgS, int run, int k_tiles, int warp, int lane, uint8_t *part, uint64_t *sums, volatile int *dead) {
+__device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, int lgS, int run, int k_tiles, int warp, int lane, uint8_t *ring, uint8_t *part, uint64_t *sums,
+                                             volatile int *dead) {
+    constexpr bool COPY = SH::BN > 16;
     const int lgCW = 7 - lgS, CW = 1 << lgCW, pitch = ((t.rows + 15) & ~15) + 4;
     const int quad = warp & 3, c = quad * 32 + lane, owner = c >> lgCW, tid = threadIdx.x - 128;
-    if (tid == 0) tc::mbar_arrive_expect_tx(sums, 128u * (uint32_t)((t.rows + 3) & ~3) * 4u);
+    const uint32_t bytes_of_run = (uint32_t)(pitch << lgCW) * 4u;
+    if (tid == 0) tc::mbar_arrive_expect_tx(sums, COPY ? ((1u << lgS) - 1) * bytes_of_run : 128u * (uint32_t)((t.rows + 3) & ~3) * 4u);
     tc::tc_fence_after();
     __syncwarp();
-    cluster_wait();   // the others have started, and their barriers exist
-    const uint32_t to = tc::map_to_rank(part, owner) + (uint32_t)((run << lgCW) + (c & (CW - 1))) * pitch * 4, bar = tc::map_to_rank(sums, owner);
+    if (!COPY) cluster_wait();   // the others have started, and their barriers exist
+    const uint32_t to = COPY ? tc::smem_u32(ring) + (uint32_t)c * pitch * 4 : tc::map_to_rank(part, owner) + (uint32_t)((run << lgCW) + (c & (CW - 1))) * pitch * 4;
+    const uint32_t bar = COPY ? 0 : tc::map_to_rank(sums, owner);
     for (int c0 = (warp - 4) / 4 * 32; c0 < t.rows; c0 += 64) {
         uint32_t v[32];
         tc::tmem_ld32(c0 + ((uint32_t)(quad * 32) << 16), v);
@@ -209,27 +215,54 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
         }
 #pragma unroll
         for (int i = 0; i < 32; i += 4)
-            if (c0 + i < t.rows) send(to + (uint32_t)(c0 + i) * 4, bar, v[i], v[i + 1], v[i + 2], v[i + 3]);
+            if (c0 + i < t.rows) {
+                if (COPY) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(c0 + i) * 4), "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]) : "memory");
+                else send(to + (uint32_t)(c0 + i) * 4, bar, v[i], v[i + 1], v[i + 2], v[i + 3]);
+            }
     }
-    __syncwarp();
-    cluster_arrive();
+    if (COPY) {
+        tc::fence_proxy_async();
+        epilogue_sync();
+        cluster_wait();   // the others have started, and their barriers exist
+        if (tid < 1 << lgS && tid != run)
+            asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(tc::map_to_rank(part, tid) + run * bytes_of_run), "r"(tc::smem_u32(ring) + tid * bytes_of_run), "r"(bytes_of_run), "r"(tc::map_to_rank(sums, tid)) : "memory");
+        __syncwarp();
+    } else {
+        __syncwarp();
+        cluster_arrive();
+    }
     const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
-    if (!tc::mbar_wait(sums, 0, p.status, 58, tc::WAIT_LIMIT_CYCLES, dead)) { *dead = 1; return; }
-    const int mine = tid & (CW - 1);
+    const bool ok = tc::mbar_wait(sums, 0, p.status, 58, tc::WAIT_LIMIT_CYCLES, dead);
+    if (!ok) *dead = 1;
+    __syncwarp();
+    if (COPY) cluster_arrive();   // what was copied from here has been received when all have arrived
+    if (!ok) return;
+    // two channels of four rows a thread
+    const int mine = 2 * (tid & (CW / 2 - 1));
     const int64_t ch = (int64_t)t.nb * 128 + (run << lgCW) + mine;
     uint16_t *out = p.y + (int64_t)t.yrow * p.N + ch;
-    for (int r = (tid >> lgCW) * 4; r < t.rows; r += (256 >> lgCW) * 4) {
-        const float *at = reinterpret_cast<const float *>(part) + mine * pitch + r;
-        float4 f = *reinterpret_cast<const float4 *>(at);
-        for (int s = 1; s < 1 << lgS; ++s) {
-            const float4 v = *reinterpret_cast<const float4 *>(at + ((s << lgCW) * pitch));
-            f.x += v.x; f.y += v.y; f.z += v.z; f.w += v.w;
+    for (int r = (tid >> (lgCW - 1)) * 4; r < t.rows; r += (512 >> lgCW) * 4) {
+        float f[2][4];
+        for (int s = 0; s < 1 << lgS; ++s) {
+            const uint8_t *from = COPY && s == run ? ring + s * bytes_of_run : part + s * bytes_of_run;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float4 v = *reinterpret_cast<const float4 *>(from + ((mine + j) * pitch + r) * 4);
+                if (s == 0) { f[j][0] = v.x; f[j][1] = v.y; f[j][2] = v.z; f[j][3] = v.w; }
+                else { f[j][0] += v.x; f[j][1] += v.y; f[j][2] += v.z; f[j][3] += v.w; }
+            }
         }
-        if (ch < p.N) {
-            out[(int64_t)r * p.N] = round_out(f.x * alpha, p.f16);
-            if (r + 1 < t.rows) out[(int64_t)(r + 1) * p.N] = round_out(f.y * alpha, p.f16);
-            if (r + 2 < t.rows) out[(int64_t)(r + 2) * p.N] = round_out(f.z * alpha, p.f16);
-            if (r + 3 < t.rows) out[(int64_t)(r + 3) * p.N] = round_out(f.w * alpha, p.f16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (r + i >= t.rows) break;
+            const uint16_t a = round_out(f[0][i] * alpha, p.f16), b = round_out(f[1][i] * alpha, p.f16);
+            uint16_t *at = out + (int64_t)(r + i) * p.N;
+            if (p.wide && ch < p.N) *reinterpret_cast<uint32_t *>(at) = a | (uint32_t)b << 16;   // N even: both are inside
+            else {
+                if (ch < p.N) at[0] = a;
+                if (ch + 1 < p.N) at[1] = b;
+            }
         }
     }
 }
@@ -331,7 +364,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         bool ok = MODE != FEW || uniform_wait(x_ready, 0, p.status, 57, dead);
         for (int local = 0; ok && tiles.has(local); ++local) {
             const Item t = tiles.at(local);
-            const uint32_t n = MODE == FEW ? FEW_ROWS : __reduce_max_sync(~0u, columns_of<PAIR>(t.rows)), sf_row = PAIR ? __reduce_max_sync(~0u, t.off / 32) : 0;
+            const uint32_t n = MODE == FEW ? FEW_ROWS : __reduce_max_sync(~0u, columns_of<PAIR>(t.rows)), sf_row = PAIR || MODE == SMALL ? __reduce_max_sync(~0u, t.off / 32) : 0;   // a tile may start inside a row block
             const int acc = local & (ACCS - 1);
             const uint32_t d = TMEM + (acc * MMAS + odd) * ACC_COLS, desc = idesc_fp4<FMT, PAIR>(n, 0);
             if (half == 0 && local >= ACCS) ok = uniform_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 53, dead);
@@ -425,7 +458,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
                 break;
             }
             if constexpr (SPLIT) {
-                send_and_add<SH>(p, t, lgS, run, k1 - k0, warp, lane, staged, sums, dead);
+                send_and_add<SH>(p, t, lgS, run, k1 - k0, warp, lane, ring, staged, sums, dead);
                 break;
             }
             tc::tc_fence_after();
@@ -544,6 +577,42 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
     return p;
 }
 
+// What computes a product of more than sixteen rows: kind of tile, rows to a tile, runs of k (log2).  Costs in microseconds, from tiles forced in
+// turn.  A k tile of one CTA takes as long as an SM's port to L2 does for its bytes (113 bytes a nanosecond) but no less than its
+// MMAs take to issue; a pair's, 0.27 to 0.36.  Cutting k saves k tiles and costs a cluster's launch and the exchange.
+//   4096 x 14336, 200 rows: SMALL 16.6, ONE 20.3 (two runs 16.3), TWO 20.5 to 22.2;  4096 x 4096, 64 rows: SMALL 6.4 (two runs 7.4), ONE 7.7, TWO 8.7;
+//   128 rows: SMALL 6.5, ONE 8.4;  512 rows: ONE 9.1, TWO 10.4 to 11.5;  6144 x 4096, 1024 rows: ONE 19.0, TWO 16.0 with 192 rows to a tile, 17.8 with 256;
+//   2048 x 8192, 400 rows: ONE in two runs 12.8, whole 17.3, TWO 14.1;  28672 x 4096, 512 rows: ONE 45.6, TWO 33.6 to 38.4
+struct Plan { int mode, bt, lg; };
+static Plan dense_plan(int64_t M, int NB, int KT, int fmt) {
+    static const Plan kinds[] = {{SMALL, 64, 0}, {SMALL, 64, 1}, {ONE, 128, 0}, {ONE, 128, 1}, {TWO, 128, 0}, {TWO, 192, 0}, {TWO, 256, 0}};
+    const double a_kb = tile_bytes(fmt) / 1000.0, sb_kb = scale_bytes(fmt) / 1000.0;
+    const int sms = sm_count();
+    Plan best = kinds[2];
+    double least = 1e30;
+    for (const Plan &k : kinds) {
+        const int ctas = k.mode == TWO ? 2 : 1, S = 1 << k.lg, nbu = (NB + ctas - 1) / ctas, places = sms / ctas;
+        if (S > KT) continue;
+        const int64_t tiles = (M + k.bt - 1) / k.bt, items = nbu * tiles;
+        if (k.lg && items * S > places) continue;   // one round, or the runs of several tiles wait for one another's places
+        const double n = M < k.bt ? (double)M : (double)k.bt, rounds = (double)((items * S + places - 1) / places);
+        double per_kt, tail, base;
+        if (k.mode == TWO) { per_kt = 0.18 + 0.18 * n / 256; tail = 1.5 * n / 256; base = 3.2; }
+        else {
+            per_kt = (a_kb + sb_kb + 0.128 * n) / 113.0;
+            const double issue = k.mode == SMALL ? 0.15 : 0.27;
+            if (per_kt < issue) per_kt = issue;
+            tail = 0.5; base = 2.4 + (k.lg ? (k.mode == SMALL ? 3.0 : 4.5) : 0.0);
+        }
+        const double cost = base + rounds * ((KT + S - 1) / S * per_kt + tail);
+        if (cost < least) { least = cost; best = k; }
+    }
+    return best;
+}
+// Routed rows: the loads are on the GPU, so the mean decides.  Sixteen matrices of 2816 x 2048, us with SMALL / ONE / TWO: 24 rows on average
+// 12.8 / 13.5 / 14.6, 64: 14.6 / 14.6 / 17.1, 150: 20.5 / 19.2 / 20.6, 512: 53 / 40 / 33.
+static Plan routed_plan(int64_t mean) { return mean > 256 ? Plan{TWO, 256, 0} : mean > 48 ? Plan{ONE, 128, 0} : Plan{SMALL, 64, 0}; }
+
 bool fp4_few_ok(int64_t M, int64_t N, int64_t K) {
     if (M > FEW_ROWS) return false;
     const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
@@ -563,20 +632,17 @@ cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, 
                             int64_t N, int64_t K, bool f16, int *status, cudaStream_t st) {
     GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
     p.x = (const uint8_t *)x; p.offset = offset; p.E = E;
-    const int sms = sm_count();
-    const int64_t rows = offset ? M / E : M;   // routed: on average, as the loads are not known here
-    const int mode = rows > 256 ? TWO : rows > 48 ? ONE : SMALL;
-    p.bt = mode == TWO ? 256 : mode == ONE ? 128 : 64;
-    p.token_tiles = (int)((M + p.bt - 1) / p.bt);
-    const int ctas = mode == TWO ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sms / ctas;
-    const int lg = offset || mode == TWO ? 0 : lg_runs_of(p.NB * p.token_tiles, p.KT, sms);
+    const Plan q = offset ? routed_plan(M / E) : M <= FEW_ROWS ? Plan{SMALL, 64, lg_runs_of(p.NB, p.KT, sm_count())} : dense_plan(M, p.NB, p.KT, fmt);
+    p.bt = q.bt;
+    p.token_tiles = (int)((M + q.bt - 1) / q.bt);
+    const int ctas = q.mode == TWO ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sm_count() / ctas;
     const int64_t items = (int64_t)nbu * p.token_tiles;
-    const unsigned grid = (unsigned)(lg ? items << lg : offset ? places : items < places ? items : places) * ctas;
+    const unsigned grid = (unsigned)(q.lg ? items << q.lg : offset ? places : items < places ? items : places) * ctas;
     auto go = [&](auto f) {
         constexpr int F = decltype(f)::value;
-        if (mode == TWO) return launch<F, TWO, false>(p, 0, items, grid, st);
-        if (mode == ONE) return lg ? launch<F, ONE, true>(p, lg, items, grid, st) : launch<F, ONE, false>(p, 0, items, grid, st);
-        return lg ? launch<F, SMALL, true>(p, lg, items, grid, st) : launch<F, SMALL, false>(p, 0, items, grid, st);
+        if (q.mode == TWO) return launch<F, TWO, false>(p, 0, items, grid, st);
+        if (q.mode == ONE) return q.lg ? launch<F, ONE, true>(p, q.lg, items, grid, st) : launch<F, ONE, false>(p, 0, items, grid, st);
+        return q.lg ? launch<F, SMALL, true>(p, q.lg, items, grid, st) : launch<F, SMALL, false>(p, 0, items, grid, st);
     };
     return fmt == MX ? go(std::integral_constant<int, MX>{}) : go(std::integral_constant<int, NV>{});
 }

@@ -94,7 +94,7 @@ def _check_scale(scale, fmt: int, matrices: int = 1):
         return
     if fmt != CQ_NVFP4:
         raise CubicQuantError("MXFP4 has no tensor scale")
-    if scale.dtype != torch.float32 or scale.numel() != matrices or not scale.is_contiguous():
+    if not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or scale.numel() != matrices or not scale.is_contiguous():
         raise CubicQuantError(f"tensor_scale is {matrices} fp32 value(s) on the device")
 
 

@@ -174,7 +174,7 @@ def test_gemm_small(M, N, K, fmt):
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("fmt", ["mx", "nv"])
 @pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (2, 1001, 2816), (13, 6144, 4096), (17, 513, 5632), (40, 1024, 1024), (100, 2816, 2048), (200, 4096, 1408),
-                                   (300, 700, 4096), (513, 1024, 512), (1000, 2050, 288)])
+                                   (300, 700, 4096), (513, 1024, 512), (1000, 2050, 288), (65, 300, 1024), (449, 1100, 2048), (1024, 6144, 512)])
 def test_gemm(M, N, K, fmt, dtype):
     w, x, g, y, S = product_case(M, N, K, fmt, dtype)
     ws = cq.cq_fp4_workspace(w, M)
@@ -237,7 +237,7 @@ def routed_case(counts, N, K, fmt, dtype, seed=0, T=50):
 
 
 @pytest.mark.parametrize("fmt", ["mx", "nv"])
-@pytest.mark.parametrize("counts", [[1], [3, 0, 5, 1], [0, 0, 7], [128, 1, 129, 0, 300, 16], [1] * 40, [700, 2]])
+@pytest.mark.parametrize("counts", [[1], [3, 0, 5, 1], [0, 0, 7], [128, 1, 129, 0, 300, 16], [1] * 40, [700, 2], [100, 3, 0, 65, 1, 1, 1, 1, 129, 1]])
 def test_gemm_routed(counts, fmt):
     N, K = 260, 544
     w, x, token, off, g, y, S = routed_case(counts, N, K, fmt, "bf16")
@@ -351,3 +351,79 @@ def test_another_stream_and_refusals_on_the_gpu():
     with pytest.raises(cq.CubicQuantError):
         cq.cq_fp4_gemm(w, x, g, workspace=torch.zeros(512, dtype=torch.uint8, device="cuda"))
     assert cq.cq_fp4_gemm(w, x[:0], g).shape == (0, 1024)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K", [(3, 130, 288), (20, 300, 1056), (100, 200, 512), (300, 900, 800)])
+def test_what_lies_behind_the_last_row_reaches_nothing(M, N, K, fmt):
+    """Layouts and workspaces full of NaN scales beforehand: the same results, and not a byte of the rows behind the last written."""
+    w, x, g, y, S = product_case(M, N, K, fmt, "bf16")
+    want = cq.cq_fp4_gemm(w, x, g)
+    q = cq.cq_fp4_empty(FMT[fmt], N, K)
+    codes, scales = cq.cq_fp4_unpack(w)
+    q.layout.fill_(255)
+    from paper_2608_06763_b200.fp4 import _check, _lib, _stream
+    _check(_lib().cq_fp4_pack(codes.data_ptr(), scales.data_ptr(), FMT[fmt], 1, N, K, q.layout.data_ptr(), _stream()), "pack")
+    q.tensor_scale = w.tensor_scale
+    ws = cq.cq_fp4_workspace(w, M)
+    ws[512:].fill_(255)
+    got = cq.cq_fp4_gemm(q, x, g, workspace=ws)
+    assert torch.equal(got, want)
+    check_product(got, y, S, K)
+    xq = cq.cq_fp4_empty(FMT[fmt], M, K)
+    xq.layout.fill_(255)
+    cq.cq_fp4_quantize(x, FMT[fmt], g, out=xq)
+    assert torch.equal(cq.cq_fp4_gemm(q, xq), want)
+    KT, tile = (K + 255) // 256, 16384 + (1024 if fmt == "mx" else 2048)
+    last = xq.layout.view(-1, KT, tile)[-1]
+    used = (M - 1) % 128 + 1
+    assert torch.all(last[:, used * 128:16384] == 255)
+
+
+def test_two_streams_and_two_graphs_with_workspaces_of_their_own():
+    """Two products at once on two streams, and two captured graphs over one workspace replayed in turn."""
+    cases = [product_case(M, 2048, 1024, "nv", "bf16", seed=50 + M) for M in (40, 200)]
+    want = [cq.cq_fp4_gemm(w, x, g) for w, x, g, _, _ in cases]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in cases], []
+    for _ in range(20):
+        for st, (w, x, g, _, _) in zip(streams, cases):
+            with torch.cuda.stream(st):
+                got.append(cq.cq_fp4_gemm(w, x, g))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want[i % 2]) for i, a in enumerate(got))
+    ws = cq.cq_fp4_workspace(cases[1][0], 200)
+    graphs, outs = [], []
+    for w, x, g, _, _ in cases:
+        out = torch.empty((x.shape[0], 2048), dtype=x.dtype, device="cuda")
+        cq.cq_fp4_gemm(w, x, g, workspace=ws, out=out)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            cq.cq_fp4_gemm(w, x, g, workspace=ws, out=out)
+        graphs.append(graph)
+        outs.append(out)
+    for _ in range(10):
+        for graph, out, y in zip(graphs, outs, want):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(out, y)
+    assert cq.cq_gemm_status(ws) == 0
+
+
+def test_long_rows_and_a_layout_beyond_two_gigabytes():
+    """Offsets past 32 bits: the last rows of a matrix of 2.4 GB in the layout, and of 8.6 GB before it."""
+    M, K = 540000, 8192
+    x = torch.randn((256, K), generator=torch.Generator("cuda").manual_seed(3), device="cuda").bfloat16().repeat(M // 256 + 1, 1)[:M]
+    q = cq.cq_fp4_quantize(x, cq.CQ_MXFP4)
+    assert q.layout.numel() > 2 ** 31 and x.numel() > 2 ** 32
+    few = cq.cq_fp4_quantize(x[:256], cq.CQ_MXFP4)
+    v, ref_v = cq.cq_fp4_dequantize(q), cq.cq_fp4_dequantize(few)
+    for lo in (0, 262144, M // 256 * 256 - 256):
+        assert torch.equal(v[lo:lo + 256], ref_v)
+    assert torch.equal(v[M // 256 * 256:], ref_v[:M % 256])
+    small = cq.cq_fp4_quantize(torch.randn((40, K), device="cuda").bfloat16(), cq.CQ_MXFP4)
+    y = cq.cq_fp4_gemm(q, small)
+    a, b = as64(cq.cq_fp4_dequantize(small, torch.float32)), as64(cq.cq_fp4_dequantize(few, torch.float32))
+    for lo in (0, M // 256 * 256 - 256):
+        check_product(y[:, lo:lo + 256], a @ b.T, np.abs(a) @ np.abs(b).T, K)
