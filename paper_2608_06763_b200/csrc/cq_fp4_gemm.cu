@@ -311,13 +311,17 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         const int nb = min(item_of<PAIR>(p, unit, nullptr, nullptr, nullptr).nb * CTAS + half, p.NB - 1);
         for (int kt = k0; kt < k1 && kt < k0 + ST; ++kt) tc::prefetch_l2(p.w + ((int64_t)nb * p.KT + kt) * tile_bytes(FMT), SH::A_BYTES);
     }
-    tc::wait_for_previous_kernel();
-    if (p.offset && warp == 3) scan_groups(p.offset, p.E, p.M, s_off, s_blk, s_item, p.bt, PAIR ? (p.NB + 1) >> 1 : p.NB);
     tc::tc_fence_before();
     __syncthreads();
     if (PAIR) tc::cluster_sync();   // the partner's barriers exist before anything arrives on them
     if (SPLIT) cluster_arrive();
     tc::tc_fence_after();
+    // From here on the next kernel may start: this one holds its tensor memory, which a kernel that waits for this one might else take.
+    tc::wait_for_previous_kernel();
+    if (p.offset) {
+        if (warp == 3) scan_groups(p.offset, p.E, p.M, s_off, s_blk, s_item, p.bt, PAIR ? (p.NB + 1) >> 1 : p.NB);
+        __syncthreads();
+    }
     const int items = p.offset ? __reduce_max_sync(~0u, s_item[p.E]) : n_items;   // (a reduction's result is uniform)
     const int stride = SPLIT ? items : units;   // split: one tile
 
