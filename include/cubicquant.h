@@ -6,6 +6,8 @@
  * cubic (Section 2.2, Eq. cubic), in two activation modes (Section 5.3 model dtype,
  * Section 5.4 Dynamic A8).
  *
+ * Besides, 4-bit floating point with block scales (last section): quantisers and products for checkpoints in that format.
+ *
  * Conventions common to every call
  *   - All pointers are DEVICE pointers unless the name says "host".  The caller owns every
  *     buffer; the library allocates no device memory and never synchronises the device

@@ -2,7 +2,8 @@
 
 Every function here only marshals arguments (torch tensors -> device pointers, current CUDA
 stream) into the C ABI declared in include/cubicquant.h; all arithmetic runs in the CUDA
-kernels.  There is no CPU fallback: importing works without a GPU (so the build can be checked),
+kernels.  The cq_fp4_* calls are the operators on 4-bit floating point with block scales (fp4.py).
+There is no CPU fallback: importing works without a GPU (so the build can be checked),
 but every compute call needs a CUDA device and the built shared library.
 """
 from .binding import (CQ_DYN_A8, CQ_EFFORT, CQ_FIT_CONTINUOUS, CQ_FIT_JOINT, CQ_MODEL_DTYPE, CubicQuantError, PackedWeights, cq_canonical_code_bytes,

@@ -79,7 +79,7 @@ int product(const void *w, const float *w_scale, const void *x, int64_t ldx, int
         CQ_TRY(wrap(launch_fp4_quantize(x, dtype, ldx, rows, fmt, K, x_scale, ws + STATUS_BYTES, st)));
         x = ws + STATUS_BYTES;
     }
-    return wrap(launch_fp4_gemm(w, w_scale, x, x_scale, offset, (int)E, fmt, y, M, N, K, act_f16 != 0, (int *)ws, st));
+    return wrap(launch_fp4_gemm(w, w_scale, x, x_scale, offset, (int)E, fmt, y, M, N, K, act_f16 != 0, !quantised, (int *)ws, st));
 }
 
 }  // namespace

@@ -20,6 +20,7 @@ struct GemmArgs {
     int M;                   // rows of x
     int64_t N;
     bool f16, wide;          // wide: rows of y start on 16-byte boundaries
+    bool early;              // launched right behind the quantiser of x: everything else may be read before that has ended
     const uint16_t *xr;      // FEW: rows of x in the model dtype, ldx apart
     int64_t ldx, K;
 };
@@ -119,6 +120,8 @@ __device__ __forceinline__ bool epilogue_any(bool v) {
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)v) : "memory");
     return r != 0;
 }
+__device__ __forceinline__ void wait_for_quantiser() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // sixteen bytes into the shared memory of a CTA of the cluster, counted there on `bar`
@@ -271,6 +274,12 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
 // that its tiles are there), warp 3 those of every second stage of small tiles, having read the offsets of routed rows, warps 4 to 11 write y.
 // SPLIT: 2^lgS CTAs of a cluster share one output tile, each a run of its k tiles; the partial sums meet in the shared memory of the
 // cluster, where each CTA adds 128 / S channels in the order of the runs.  One tile a CTA then; else CTAs (pairs) take tiles in turn.
+// What bounds it.  256 x 256 tiles of pairs: a stage of 256 k is 512 cycles of the tensor core at its rate, and takes 640 with everything
+// around it (issuing 14 to 18 instructions a stage, a tile's accumulators read before the next tile starts); 57344 x 8192, 4096 rows 650 to 800 us, 4.8 to
+// 5.9 PFLOP/s, by what the power limit leaves of the clock; 8192 x 8192, 4096 rows 100 us in a burst with the tensor pipe 78 % active.  Copies come
+// as they are stored, a contiguous run each.  One CTA of 128 x 128 is bound by its SM's port to L2 (36.9 KB a stage, 600 cycles), small tiles by
+// memory: 28672 x 4096, 13 rows 13.1 us for 63 MB, of which some three are the launch, the first copies' way and the last tile's output, and
+// one and a half the second round of tiles, which 76 of 148 SMs have.
 // FEW: warps 4 to 11 first quantise the rows for this CTA's k tiles, while the first weights are on their way.
 template <int FMT, int MODE, bool SPLIT>
 __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int lgS, int n_items) {
@@ -307,7 +316,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         if (PAIR) tc::tmem_alloc_pair(s_tmem, 512);
         else { tc::tmem_alloc(s_tmem, 512); tc::tmem_relinquish(); }
     }
-    if (!p.offset && threadIdx.x == 0 && unit < n_items) {   // the first weights on their way to L2, which sees what the kernel in front may still write
+    if (!p.offset && !p.early && threadIdx.x == 0 && unit < n_items) {   // the first weights on their way to L2, which sees what the kernel in front may still write
         const int nb = min(item_of<PAIR>(p, unit, nullptr, nullptr, nullptr).nb * CTAS + half, p.NB - 1);
         for (int kt = k0; kt < k1 && kt < k0 + ST; ++kt) tc::prefetch_l2(p.w + ((int64_t)nb * p.KT + kt) * tile_bytes(FMT), SH::A_BYTES);
     }
@@ -317,7 +326,10 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
     if (SPLIT) cluster_arrive();
     tc::tc_fence_after();
     // From here on the next kernel may start: this one holds its tensor memory, which a kernel that waits for this one might else take.
-    tc::wait_for_previous_kernel();
+    // Behind the quantiser of this call only the layout that it writes has to be waited for (by the warp that reads it, and in every CTA): the
+    // quantiser lets this kernel start once all kernels in front of itself have ended, those that wrote weights, scales and offsets among them.
+    if (p.early) launch_dependents();
+    else tc::wait_for_previous_kernel();
     if (p.offset) {
         if (warp == 3) scan_groups(p.offset, p.E, p.M, s_off, s_blk, s_item, p.bt, PAIR ? (p.NB + 1) >> 1 : p.NB);
         __syncthreads();
@@ -333,6 +345,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         const int64_t block = (int64_t)p.KT * tile_bytes(FMT);   // from a row block to the next
         uint32_t s = 0, phase = 1;
         bool ok = true;
+        if (warp == 2 && p.early) wait_for_quantiser();
         for (int local = 0; ok && tiles.has(local); ++local) {
             const Item t = tiles.at(local);
             const int n = columns_of<PAIR>(t.rows), mine = n / CTAS, nb = min(t.nb * CTAS + half, p.NB - 1);   // an odd last pair reads a block twice
@@ -430,20 +443,35 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
         if constexpr (MODE == FEW) {
             const int tid = threadIdx.x - 128, units = (k1 - k0) * p.M * 16, KU = (int)(p.K >> 4);
             const float g = FMT == NV && p.x_scale ? *p.x_scale : 1.0f;
+            const float r = __fdiv_rn(1.0f, g);
+            struct Unit { int kt, row; bool live, inside; uint4 a, b; };
+            const int u = tid & 15;
+            auto load = [&](int i) {   // the i-th unit of sixteen k of all rows
+                Unit q;
+                const int line = i >> 4;
+                q.kt = line / p.M;
+                q.row = line - q.kt * p.M;
+                const int unit = (k0 + q.kt) * 16 + u;
+                q.live = i < units;
+                q.inside = unit < KU;
+                const uint16_t *src = p.xr + q.row * p.ldx + (int64_t)unit * 16;
+                const bool read = q.live && q.inside;
+                q.a = read ? load16(src) : make_uint4(0, 0, 0, 0);
+                q.b = read ? load16(src + 8) : make_uint4(0, 0, 0, 0);
+                return q;
+            };
+            Unit next = load(tid);
             for (int i0 = 0; i0 < units; i0 += 256) {   // whole warps: they exchange scales
-                const int i = i0 + tid, u = i & 15, line = i >> 4, kt = line / p.M, row = line - kt * p.M, unit = (k0 + kt) * 16 + u;
-                const bool live = i < units, read = live && unit < KU;
-                const uint16_t *src = p.xr + row * p.ldx + (int64_t)unit * 16;
-                const uint4 a = read ? load16(src) : make_uint4(0, 0, 0, 0), b = read ? load16(src + 8) : make_uint4(0, 0, 0, 0);
-                const float r = __fdiv_rn(1.0f, g);
+                const Unit q = next;
+                if (i0 + 256 < units) next = load(i0 + 256 + tid);
                 uint32_t scale;
-                const uint2 codes = p.f16 ? quantize_unit<FMT, DT_F16>(a, b, r, scale) : quantize_unit<FMT, DT_BF16>(a, b, r, scale);
-                if (unit >= KU) scale = 0;   // behind K
+                const uint2 codes = p.f16 ? quantize_unit<FMT, DT_F16>(q.a, q.b, r, scale) : quantize_unit<FMT, DT_BF16>(q.a, q.b, r, scale);
+                if (!q.inside) scale = 0;   // behind K
                 // a tile's scales and codes as in the layout, the codes of sixteen rows alone
                 const uint32_t word = gather_scales<FMT>(scale);
-                if (live) {
-                    *reinterpret_cast<uint2 *>(x_codes + kt * SH::X_CODES + code_offset(row, u * 8)) = codes;
-                    uint8_t *sc = x_scales + kt * SB + scale_offset(row, FMT == NV ? u : u >> 1) - CODE_BYTES;
+                if (q.live) {
+                    *reinterpret_cast<uint2 *>(x_codes + q.kt * SH::X_CODES + code_offset(q.row, u * 8)) = codes;
+                    uint8_t *sc = x_scales + q.kt * SB + scale_offset(q.row, FMT == NV ? u : u >> 1) - CODE_BYTES;
                     if ((lane & (FMT == NV ? 3 : 7)) == 0) *reinterpret_cast<uint32_t *>(sc) = word;
                 }
             }
@@ -633,8 +661,9 @@ cudaError_t launch_fp4_few(const void *w, const float *w_scale, const uint16_t *
 }
 
 cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, int fmt, uint16_t *y, int64_t M,
-                            int64_t N, int64_t K, bool f16, int *status, cudaStream_t st) {
+                            int64_t N, int64_t K, bool f16, bool early, int *status, cudaStream_t st) {
     GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
+    p.early = early;
     p.x = (const uint8_t *)x; p.offset = offset; p.E = E;
     const Plan q = offset ? routed_plan(M / E) : M <= FEW_ROWS ? Plan{SMALL, 64, lg_runs_of(p.NB, p.KT, sm_count())} : dense_plan(M, p.NB, p.KT, fmt);
     p.bt = q.bt;

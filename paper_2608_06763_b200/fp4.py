@@ -48,19 +48,14 @@ def _need(ok, what: str):
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _device() -> int:
-    """The current device; -2 where there is none, which no tensor is on."""
-    if torch.cuda.is_initialized():
-        return _current_device()
-    return torch.cuda.current_device() if torch.cuda.is_available() else -2
-
-
-def _here(*tensors) -> int:
+def _here(first, *others) -> int:
     """The stream to launch on.  Every tensor has to be on the current device: the call goes to that device's current stream."""
-    dev = _device()
-    for t in tensors:
+    dev = first.get_device()
+    if dev < 0 or dev != _current_device():
+        raise CubicQuantError(f"a tensor on {first.device}, which is not the current device: switch with torch.cuda.device")
+    for t in others:
         if t is not None and t.get_device() != dev:
-            raise CubicQuantError(f"a tensor on {t.device} with device {dev} current: switch with torch.cuda.device")
+            raise CubicQuantError(f"tensors on {first.device} and {t.device}")
     return binding._raw_stream(dev) if binding._raw_stream is not None else _stream()
 
 
@@ -94,7 +89,7 @@ def _check_scale(scale, fmt: int, matrices: int = 1):
         return
     if fmt != CQ_NVFP4:
         raise CubicQuantError("MXFP4 has no tensor scale")
-    if not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or scale.numel() != matrices or not scale.is_contiguous():
+    if not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or scale.numel() != matrices or (matrices > 1 and not scale.is_contiguous()):
         raise CubicQuantError(f"tensor_scale is {matrices} fp32 value(s) on the device")
 
 
