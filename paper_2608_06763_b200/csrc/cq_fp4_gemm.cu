@@ -99,6 +99,9 @@ struct Shape {
     static constexpr int PITCH = 272;                            // bytes of a row of the staged output: 128 channels and a gap against bank conflicts
     static constexpr int X_CODES = FEW_ROWS * 128, X_BYTES = MODE == FEW ? FEW_TILES * (X_CODES + SB) : 0;   // FEW: codes of a k tile; all k tiles
     static constexpr int OUT_BYTES = SPLIT ? 128 * (BN + 4) * 4 : (MODE == FEW ? 32 : 64) * PITCH;   // SPLIT: partial sums [run][channel][row of x, and a gap]
+    // A stage of the ring always has the same one of them: a warp that passed over a stage in one round cannot tell from the parity of its
+    // barrier, in the next, whether that round has come.
+    static_assert(STAGES % MMAS == 0, "a stage belongs to one issuing warp");
     static_assert(SF0 + STAGES * SF_COLS <= 512, "tensor memory");
     static constexpr size_t smem(int E, bool routed) { return (size_t)STAGES * STAGE + X_BYTES + OUT_BYTES + 256 + (routed ? 3 * (size_t)(E + 1) * 4 : 0); }
     static_assert(STAGES * STAGE + X_BYTES + OUT_BYTES + 256 + (MODE == FEW ? 0 : 12 * (MAX_EXPERTS + 1)) <= 232448, "shared memory");
@@ -207,7 +210,7 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
     for (int c0 = (warp - 4) / 4 * 32; c0 < t.rows; c0 += 64) {
         uint32_t v[32];
         tc::tmem_ld32(c0 + ((uint32_t)(quad * 32) << 16), v);
-        if (SH::MMAS == 2 && k_tiles > 1) {   // the sums of the odd k tiles
+        if (SH::MMAS == 2 && k_tiles > 1) {   // the sums of the other k tiles
             uint32_t v1[32];
             tc::tmem_ld32(SH::ACC_COLS + c0 + ((uint32_t)(quad * 32) << 16), v1);
             tc::tmem_ld_wait();
@@ -376,7 +379,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
     } else if (warp == 1 || (warp == 3 && MMAS == 2)) {
         // The whole warp walks the loops and one lane issues: what the instructions take stays in uniform registers (a stage takes twice
         // as long where a lane of its own does it all).
-        const int odd = warp >> 1;   // MMAS == 2: which of a tile's k tiles are this warp's
+        const uint32_t odd = warp >> 1;   // MMAS == 2: which stages are this warp's, every second k tile of an output tile
         uint32_t s = 0, phase = 0;
         bool ok = MODE != FEW || uniform_wait(x_ready, 0, p.status, 57, dead);
         for (int local = 0; ok && tiles.has(local); ++local) {
@@ -386,8 +389,10 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             const uint32_t d = TMEM + (acc * MMAS + odd) * ACC_COLS, desc = idesc_fp4<FMT, PAIR>(n, 0);
             if (half == 0 && local >= ACCS) ok = uniform_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 53, dead);
             tc::tc_fence_after();
+            bool idle = true;
             for (int kt = k0; kt < k1 && ok; ++kt) {
-                if (MMAS == 1 || ((kt - k0) & 1) == odd) {
+                if (MMAS == 1 || (s & 1) == odd) {
+                    idle = false;
                     ok = uniform_wait(&full[s], phase, p.status, 54, dead);
                     if (!ok) break;
                     if (PAIR && half == 1) {
@@ -425,7 +430,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
                 }
                 if (++s == ST) { s = 0; phase ^= 1; }
             }
-            if (MMAS == 2 && ok && k1 - k0 == 1 && odd == 1 && lane == 0) tc::mbar_arrive(&acc_full[acc]);   // nothing to add
+            if (MMAS == 2 && ok && idle && lane == 0) tc::mbar_arrive(&acc_full[acc]);   // one k tile, and it was the other warp's
         }
         if (!ok && lane == 0) *dead = 1;
         if (!ok && half == 0) {   // what was issued completes before tensor memory is given back
@@ -502,10 +507,11 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             for (int g = 0; g < GROUPS; ++g) {
                 if (g * 64 + part * 32 < t.rows) {
                     uint32_t lo[16], hi[16];
-                    const uint32_t from = TMEM + acc * MMAS * ACC_COLS + g * 64 + part * 32 + ((uint32_t)(quad * 32) << 16);
+                    // one k tile: it is in the accumulators of the warp whose stage it came in
+                    const uint32_t from = TMEM + (acc * MMAS + (MMAS == 2 && k1 - k0 == 1 ? local & 1 : 0)) * ACC_COLS + g * 64 + part * 32 + ((uint32_t)(quad * 32) << 16);
                     tmem_ld_16x32(from, lo);
                     tmem_ld_16x32(from + (16u << 16), hi);
-                    if (MMAS == 2 && k1 - k0 > 1) {   // the sums of the odd k tiles
+                    if (MMAS == 2 && k1 - k0 > 1) {   // the sums of the other k tiles
                         uint32_t lo1[16], hi1[16];
                         tmem_ld_16x32(from + ACC_COLS, lo1);
                         tmem_ld_16x32(from + ACC_COLS + (16u << 16), hi1);

@@ -427,3 +427,21 @@ def test_long_rows_and_a_layout_beyond_two_gigabytes():
     a, b = as64(cq.cq_fp4_dequantize(small, torch.float32)), as64(cq.cq_fp4_dequantize(few, torch.float32))
     for lo in (0, M // 256 * 256 - 256):
         check_product(y[:, lo:lo + 256], a @ b.T, np.abs(a) @ np.abs(b).T, K)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 24000, 200), (5, 24000, 700), (2, 20100, 1312), (40, 20100, 1312), (60, 24000, 144)])
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_odd_numbers_of_k_tiles_over_many_output_tiles(M, N, K, fmt):
+    """Several output tiles to a CTA, an odd number of stages each, so that the ring's stages fall to other k tiles from one to the next:
+    called often enough for the two issuing warps to drift apart, always the same bits."""
+    K = K // 32 * 32
+    w, x, g, y, S = product_case(M, N, K, fmt, "bf16")
+    ws = cq.cq_fp4_workspace(w, M)
+    want = cq.cq_fp4_gemm(w, x, g, workspace=ws)
+    check_product(want, y, S, K)
+    out = torch.empty_like(want)
+    for i in range(200):
+        cq.cq_fp4_gemm(w, x, g, workspace=ws, out=out)
+        if i % 20 == 0:
+            assert torch.equal(out, want)
+    assert torch.equal(out, want) and cq.cq_gemm_status(ws) == 0
