@@ -28,7 +28,9 @@ struct GemmArgs {
 // What a CTA computes.  ONE: 128 channels x up to 128 rows of x; TWO: a pair of CTAs 256 channels x up to 256 rows; FEW: 128 channels x up to 16
 // rows, which it quantises itself and keeps in shared memory; SMALL: 128 channels x up to 64 rows.
 enum { ONE = 0, TWO = 1, FEW = 2, SMALL = 3 };
-constexpr int FEW_ROWS = 16, FEW_TILES = 16, FEW_MOST = 64;   // rows, and k tiles of them, that fit beside the ring
+// rows, and k tiles of them, that fit beside the ring; and their product up to which a CTA's own quantising (0.5 us for sixteen of it) costs no
+// more than a launch for it.  us, by itself / in front: 16: 6.3 / 7.7; 32: 6.9 / 7.8; 52: 8.1 / 8.0; 64: 14.9 / 15.1; 128: 18.4 / 15.2.
+constexpr int FEW_ROWS = 16, FEW_TILES = 16, FEW_MOST = 64;
 
 // D[tmem] (+)= A B, codes by shared-memory descriptors, scales in tensor memory.  PAIR: by the tensor cores of two SMs, each with 128 of
 // the 256 rows of A and half of the columns of B in its shared memory.
