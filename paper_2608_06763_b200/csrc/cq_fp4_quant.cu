@@ -164,9 +164,10 @@ __global__ void __launch_bounds__(256) quantize_kernel(const void *x, int64_t ld
 // sum 1, the reciprocal 2, the last product 1: ten.  Where no value lies within BAND = 12 units of the last place (each at least such a unit)
 // of a border, the roundings stand.  In a unit of sixteen where one does (one in 170 in bfloat16, one in 22 in binary16) the
 // candidates on both sides are quantised, and only where a scale or a code differs is the activation formed in 64 bits.  Gates beyond 60
-// either way go there at once (exp(60) leaves room in 32 bits for the denominator and its reciprocal).
-// 25 instructions an activation, in pairs where the GPU has paired fp32 operations; the issue slots are 72 % used.  4096 x 14336 to MXFP4 60 us
-// (4.4 TB/s); with expf and no pairs 102, with the 64-bit evaluation by single lanes 72.  13 x 14336 3.9 us.
+// either way go there at once (exp(60) leaves room in 32 bits for the denominator and its reciprocal), and so does a unit with an
+// activation that is not finite: gate * up is exact within the range of fp32 alone, and leaves it where silu(gate) * up need not.
+// 25 instructions an activation, in pairs where the GPU has paired fp32 operations; the issue slots are 72 % used.  4096 x 14336 to MXFP4 60.7 us
+// (4.4 TB/s); with expf and no pairs 102, with the 64-bit evaluation by single lanes 72.  13 x 14336 3.6 us.  Looking for infinities is 0.8 of the 60.7.
 constexpr int BAND = 12;
 template <int DT>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
@@ -265,9 +266,10 @@ __global__ void __launch_bounds__(256, 4) swiglu_quantize_kernel(const uint16_t 
                 if (DT == DT_F16) small = fminf(small, fminf(y[k] == 0.0f ? 1.0f : fabsf(y[k]), y[k + 1] == 0.0f ? 1.0f : fabsf(y[k + 1])));   // subnormal halves have their borders elsewhere
             }
             constexpr uint32_t WIDE = 2 * BAND * (DT == DT_BF16 ? 1 : 8);
-            const bool far = top_of_16bit<DT>(gw) > 0x42700000u;   // 60
+            const uint32_t largest = top_of_16bit<DT>(act);
+            const bool far = top_of_16bit<DT>(gw) > 0x42700000u || largest >= 0x7F800000u;   // 60; infinities and NaN
             const bool open = (near & 0xFFFFu) <= WIDE || (near >> 16) <= WIDE || far || (DT == DT_F16 && small < 6.103515625e-05f);
-            uint32_t top = top_of_block<FMT>(top_of_16bit<DT>(act));
+            uint32_t top = top_of_block<FMT>(largest);
             if (__any_sync(~0u, open)) {
                 uint32_t a0[8], a1[8];   // a unit without open values has one candidate
 #pragma unroll

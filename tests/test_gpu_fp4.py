@@ -144,6 +144,26 @@ def test_swiglu_far_gates_and_subnormal_activations(fmt):
         check_bytes(q, *ref.quantize(as64(act), fmt))
 
 
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_swiglu_products_of_gate_and_up_beyond_fp32(fmt):
+    """gate * up leaves fp32 where silu(gate) * up does not: finite values, and an infinity only where the activation itself is one."""
+    I, M = 64, 40
+    r = np.random.default_rng(21)
+    gate = r.uniform(-60, 60, (M, I)) * r.choice([1.0, 0.05], (M, I))
+    up = 10.0 ** r.uniform(36.5, 38.5, (M, I)) * r.choice([-1.0, 1.0], (M, I))
+    gate[0, :3], up[0, :3] = (-2.0, -50.0, 1.5), (3e38, 1e37, 2.4e38)
+    gate[1:20] = -np.abs(gate[1:20])              # whole blocks of finite activations
+    up[20:30, ::2] = 1.0                           # among ordinary ones
+    h = torch.from_numpy(np.concatenate([gate, up], axis=1)).float().to(torch.bfloat16)
+    v = as64(h)
+    act = torch.from_numpy(ref.gated(v[:, :I], v[:, I:])).to(torch.bfloat16)
+    assert torch.isfinite(act[1:20]).all() and not torch.isfinite(act).all()
+    assert (np.abs(v[:, :I] * v[:, I:]) > torch.finfo(torch.float32).max).any(axis=1)[1:20].all()
+    g = 1e34
+    q = cq.cq_fp4_swiglu_quantize(h.cuda(), FMT[fmt], g_of(fmt, g))
+    check_bytes(q, *ref.quantize(as64(act), fmt, g))
+
+
 def product_case(M, N, K, fmt, dtype, seed=0):
     gw, gx = (1.0, 1.0) if fmt == "mx" else (0.0007, 0.021)
     w, x = rows(N, K, "f32", seed, 0.3) * 0.05, rows(M, K, dtype, seed + 1, 0.3)
