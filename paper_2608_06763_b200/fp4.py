@@ -223,16 +223,20 @@ def cq_fp4_swiglu_quantize(h: torch.Tensor, fmt: int, tensor_scale: torch.Tensor
 
 
 def cq_fp4_dequantize(q: Fp4Tensor, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
-    """The values that q stands for, [M, K] or [E, M, K]; rows of no group are left as they were (new ones: zeros)."""
+    """The values that q stands for, [M, K] or [E, M, K]; rows of no group are left as they were (new ones: zeros).  Routed rows: of
+    a handle that a quantiser has filled, which carries their offsets."""
+    if q.groups:
+        _check_offset(q.expert_offset, q.groups)
     shape = (q.matrices, q.M, q.K) if q.matrices > 1 else (q.M, q.K)
     if out is None:
         out = (torch.zeros if q.groups else torch.empty)(shape, dtype=dtype, device=q.layout.device)
     code, at = _DTYPE.get(out.dtype), out.data_ptr()
     if code is None or out.shape != shape or at % 16 or not out.is_contiguous():
         raise CubicQuantError(f"out is a contiguous tensor of shape {shape}")
-    stream = _here(q.layout, q.tensor_scale, q.expert_offset, out)
+    offset = q.expert_offset if q.groups else None
+    stream = _here(q.layout, q.tensor_scale, offset, out)
     if q.M:
-        status = (_L or _lib()).cq_fp4_dequantize(q.layout.data_ptr(), q.fmt, q.groups or q.matrices, q.M, q.K, _at(q.expert_offset), _at(q.tensor_scale), at, code, stream)
+        status = (_L or _lib()).cq_fp4_dequantize(q.layout.data_ptr(), q.fmt, q.groups or q.matrices, q.M, q.K, _at(offset), _at(q.tensor_scale), at, code, stream)
         if status != 0:
             _check(status, "cq_fp4_dequantize")
     return out

@@ -135,3 +135,16 @@ def test_python_refuses():
                 lambda: cq.cq_fp4_gemm_routed(w4, x, None, off), lambda: cq.cq_fp4_gemm_routed(w4, routed, None, off), lambda: cq.cq_fp4_unpack(routed)):
         with pytest.raises(E):
             bad()
+
+
+def test_values_of_routed_rows_need_their_offsets():
+    """A handle that no quantiser has filled has no offsets; without them the rows would be taken for whole matrices, one for each group."""
+    layout = torch.zeros(3 * 18432, dtype=torch.uint8)
+    for offset in (None, torch.zeros(3, dtype=torch.int32), torch.zeros(5, dtype=torch.int32), torch.zeros(4, dtype=torch.int64), [0, 1, 2, 3]):
+        q = cq.Fp4Tensor(layout, cq.CQ_NVFP4, 1, 3, 256, None, 3, offset)
+        for out in (None, torch.zeros((3, 256), dtype=torch.bfloat16)):
+            with pytest.raises(cq.CubicQuantError, match="expert_offset"):
+                cq.cq_fp4_dequantize(q, out=out)
+    q = cq.cq_fp4_empty(cq.CQ_NVFP4, 3, 256, groups=3, device="cpu")
+    with pytest.raises(cq.CubicQuantError, match="expert_offset"):
+        cq.cq_fp4_dequantize(q)
