@@ -191,11 +191,10 @@ def cq_fp4_quantize(x: torch.Tensor, fmt: int, tensor_scale: torch.Tensor | None
         stream = _here(x, tensor_scale, route_token, expert_offset, None if out is None else out.layout)
         R, groups = route_token.numel(), expert_offset.numel() - 1
         q = _into(out, fmt, R, K, 1, groups, device=x.device)
-        q.expert_offset = expert_offset
         if R:
             _check((_L or _lib()).cq_fp4_quantize_routed(at, dtype, ld, M, route_token.data_ptr(), expert_offset.data_ptr(), groups, R, fmt, K, _at(tensor_scale),
                                                          q.layout.data_ptr(), stream), "cq_fp4_quantize")
-    q.tensor_scale = tensor_scale
+    q.tensor_scale, q.expert_offset = tensor_scale, expert_offset
     return q
 
 
@@ -214,11 +213,11 @@ def cq_fp4_swiglu_quantize(h: torch.Tensor, fmt: int, tensor_scale: torch.Tensor
         groups = expert_offset.numel() - 1
     stream = _here(h, tensor_scale, expert_offset, None if out is None else out.layout)
     q = _into(out, fmt, M, K, 1, groups, device=h.device)
-    q.tensor_scale, q.expert_offset = tensor_scale, expert_offset
     if M:
         status = (_L or _lib()).cq_fp4_swiglu_quantize(at, dtype, ld, fmt, M, K, _at(expert_offset), groups or 0, _at(tensor_scale), q.layout.data_ptr(), stream)
         if status != 0:
             _check(status, "cq_fp4_swiglu_quantize")
+    q.tensor_scale, q.expert_offset = tensor_scale, expert_offset
     return q
 
 

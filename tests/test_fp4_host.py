@@ -148,3 +148,26 @@ def test_values_of_routed_rows_need_their_offsets():
     q = cq.cq_fp4_empty(cq.CQ_NVFP4, 3, 256, groups=3, device="cpu")
     with pytest.raises(cq.CubicQuantError, match="expert_offset"):
         cq.cq_fp4_dequantize(q)
+
+
+@pytest.mark.parametrize("routed", [False, True])
+def test_a_refused_quantiser_leaves_the_given_handle_as_it_was(monkeypatch, routed):
+    """What a handle says of its rows changes with the rows, not before the call that writes them may still refuse."""
+    from paper_2608_06763_b200 import fp4
+
+    class Refusing:
+        def __getattr__(self, name):
+            return lambda *a: -2
+
+    monkeypatch.setattr(fp4, "_here", lambda *a: None)
+    monkeypatch.setattr(fp4, "_L", Refusing())
+    layout = torch.zeros(3 * 18432, dtype=torch.uint8)
+    scale, offset = torch.ones(1), torch.zeros(4, dtype=torch.int32)
+    token = torch.zeros(3, dtype=torch.int32)
+    x, h = torch.zeros((3, 256), dtype=torch.bfloat16), torch.zeros((3, 512), dtype=torch.bfloat16)
+    for call in (lambda q: cq.cq_fp4_quantize(x, cq.CQ_NVFP4, torch.full((1,), 2.0), *((token, offset.clone()) if routed else (None, None)), out=q),
+                 lambda q: cq.cq_fp4_swiglu_quantize(h, cq.CQ_NVFP4, torch.full((1,), 2.0), offset.clone() if routed else None, out=q)):
+        q = cq.Fp4Tensor(layout, cq.CQ_NVFP4, 1, 3, 256, scale, 3 if routed else 0, offset if routed else None)
+        with pytest.raises(cq.CubicQuantError):
+            call(q)
+        assert q.tensor_scale is scale and q.expert_offset is (offset if routed else None)
