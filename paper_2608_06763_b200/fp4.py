@@ -252,7 +252,7 @@ def _output(w, M, dtype, workspace, out, own_workspace):
     if out is None:
         out = torch.empty((M, w.M), dtype=dtype, device=w.layout.device)
     code, at = _DTYPE.get(out.dtype), out.data_ptr()
-    if out.dtype != dtype or code == 2 or out.shape != (M, w.M) or at % 16 or not out.is_contiguous():
+    if out.dtype != dtype or code is None or code == 2 or out.shape != (M, w.M) or at % 16 or not out.is_contiguous():
         raise CubicQuantError(f"out is a contiguous [{M}, {w.M}] tensor of 16-byte alignment in the dtype of x, bfloat16 or float16")
     if workspace is None:
         workspace = cq_fp4_workspace(w, M) if own_workspace else torch.zeros(512, dtype=torch.uint8, device=w.layout.device)

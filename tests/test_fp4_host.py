@@ -171,3 +171,16 @@ def test_a_refused_quantiser_leaves_the_given_handle_as_it_was(monkeypatch, rout
         with pytest.raises(cq.CubicQuantError):
             call(q)
         assert q.tensor_scale is scale and q.expert_offset is (offset if routed else None)
+
+
+@pytest.mark.parametrize("dtype", [torch.float64, torch.int32, torch.uint8, torch.float32])
+def test_products_of_quantised_rows_refuse_an_out_of_another_type(dtype):
+    layout = torch.zeros(18432, dtype=torch.uint8)
+    w = cq.Fp4Tensor(layout, cq.CQ_NVFP4, 1, 128, 256)
+    x = cq.Fp4Tensor(layout, cq.CQ_NVFP4, 1, 4, 256)
+    off = torch.zeros(2, dtype=torch.int32)
+    routed = cq.Fp4Tensor(layout, cq.CQ_NVFP4, 1, 4, 256, None, 1, off)
+    out = torch.zeros((4, 128), dtype=dtype)
+    for bad in (lambda: cq.cq_fp4_gemm(w, x, out=out), lambda: cq.cq_fp4_gemm_routed(w, routed, None, off, out=out)):
+        with pytest.raises(cq.CubicQuantError, match="out is"):
+            bad()
