@@ -317,6 +317,11 @@ int cq_fp4_linear_routed(const void *w, const float *w_scale, const uint16_t *x,
                          const int32_t *expert_offset, int64_t E, int fmt, uint16_t *y, int act_f16, int64_t R, int64_t N, int64_t K, void *workspace,
                          size_t workspace_bytes, void *stream);
 
+/* How a product of M rows is cut on the current device (host-side query, launches nothing).  E = 0: cq_fp4_linear, or with `quantised`
+ * cq_fp4_gemm; E > 0: the routed ones with E matrices.  plan must hold four values: channels and rows of x to an output tile (256 channels: a pair
+ * of CTAs), the runs of K that share such a tile (1: none), and 1 when the product quantises x itself, without a launch in front. */
+int cq_debug_fp4_plan(int fmt, int64_t E, int64_t M, int64_t N, int64_t K, int quantised, int64_t *plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,7 @@ from .binding import (CQ_DYN_A8, CQ_EFFORT, CQ_FIT_CONTINUOUS, CQ_FIT_JOINT, CQ_
                       cq_effective_bits, cq_encode, cq_encode_assign, cq_encode_losses, cq_encode_scale, cq_gemm, cq_gemm_host, cq_gemm_routed, cq_gemm_status, cq_gemv_static, cq_layout_bytes, cq_mlp_swiglu, cq_pack_codes, cq_quantize_a8,
                       cq_repack, cq_status_string, cq_unpack, cq_workspace_bytes, cq_workspace_init, lib,
                       library_path)
-from .fp4 import (CQ_MXFP4, CQ_NVFP4, Fp4Tensor, cq_fp4_dequantize, cq_fp4_empty, cq_fp4_gemm, cq_fp4_gemm_routed, cq_fp4_pack, cq_fp4_quantize,
+from .fp4 import (CQ_MXFP4, CQ_NVFP4, Fp4Tensor, cq_debug_fp4_plan, cq_fp4_dequantize, cq_fp4_empty, cq_fp4_gemm, cq_fp4_gemm_routed, cq_fp4_pack, cq_fp4_quantize,
                   cq_fp4_swiglu_quantize, cq_fp4_unpack, cq_fp4_workspace)
 
 __all__ = [n for n in dir() if n.startswith(("cq_", "CQ_"))] + ["PackedWeights", "Fp4Tensor", "CubicQuantError", "lib",

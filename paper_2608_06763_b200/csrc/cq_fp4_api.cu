@@ -53,22 +53,25 @@ int check_arch() {   // as for every product: tcgen05 needs a device of compute 
     return major == 10 ? CQ_OK : CQ_ERR_ARCH;
 }
 
+int64_t product_blocks(int64_t E, bool routed, int64_t M) { return routed ? routed_blocks(E, M) : blocks_of(M); }
+int check_product(int fmt, int64_t E, bool routed, int64_t M, int64_t N, int64_t K) {
+    CQ_TRY(check_shape(fmt, E, N, K));
+    CQ_TRY(check_shape(fmt, 1, M, K));
+    if (routed) CQ_TRY(check_groups(E, M));
+    return blocks_of(N) * product_blocks(E, routed, M) > MOST / 2 ? CQ_ERR_UNSUPPORTED : CQ_OK;   // two tiles of 64 rows to a row block, counted in 32 bits
+}
 // x: the layout of quantised rows (ldx < 0), or rows in the model dtype, quantised into the workspace first
 int product(const void *w, const float *w_scale, const void *x, int64_t ldx, int64_t T, const int32_t *route_token, const float *x_scale, const int32_t *offset, bool routed,
             int64_t E, int fmt, uint16_t *y, int act_f16, int64_t M, int64_t N, int64_t K, void *workspace, size_t workspace_bytes, void *stream) {
     const bool quantised = ldx < 0;
     if (!w || !x || !y || !workspace || (routed && !offset) || (routed && !quantised && (!route_token || T <= 0))) return CQ_ERR_INVALID_ARG;
-    CQ_TRY(check_shape(fmt, E, N, K));
-    CQ_TRY(check_shape(fmt, 1, M, K));
-    if (routed) CQ_TRY(check_groups(E, M));
+    CQ_TRY(check_product(fmt, E, routed, M, N, K));
     CQ_TRY(check_scale(fmt, w_scale));
     CQ_TRY(check_scale(fmt, x_scale));
     const int dtype = act_f16 ? CQ_F16 : CQ_BF16;
     if (!quantised) CQ_TRY(check_rows(x, dtype, ldx, K));
     if (misaligned(w) || misaligned(x) || misaligned(y) || misaligned(workspace)) return CQ_ERR_ALIGNMENT;
-    const int64_t blocks = routed ? routed_blocks(E, M) : blocks_of(M);
-    if (blocks_of(N) * blocks > MOST / 2) return CQ_ERR_UNSUPPORTED;   // two tiles of 64 rows to a row block, counted in 32 bits
-    if (workspace_bytes < STATUS_BYTES + (quantised ? 0 : bytes_of(fmt, blocks, K))) return CQ_ERR_WORKSPACE;
+    if (workspace_bytes < STATUS_BYTES + (quantised ? 0 : bytes_of(fmt, product_blocks(E, routed, M), K))) return CQ_ERR_WORKSPACE;
     CQ_TRY(check_arch());
     cudaStream_t st = (cudaStream_t)stream;
     uint8_t *ws = (uint8_t *)workspace;
@@ -172,6 +175,16 @@ int cq_fp4_linear_routed(const void *w, const float *w_scale, const uint16_t *x,
                          size_t workspace_bytes, void *stream) {
     if (ldx < 0) return CQ_ERR_INVALID_ARG;
     return product(w, w_scale, x, ldx, T, route_token, x_scale, expert_offset, true, E, fmt, y, act_f16, R, N, K, workspace, workspace_bytes, stream);
+}
+
+int cq_debug_fp4_plan(int fmt, int64_t E, int64_t M, int64_t N, int64_t K, int quantised, int64_t *plan) {
+    if (!plan || E < 0) return CQ_ERR_INVALID_ARG;
+    const bool routed = E > 0;
+    CQ_TRY(check_product(fmt, routed ? E : 1, routed, M, N, K));
+    const bool own = !quantised && !routed && fp4_few_ok(M, N, K);
+    const Fp4Plan p = fp4_plan(E, routed, M, N, K, fmt, own);
+    plan[0] = p.channels; plan[1] = p.rows; plan[2] = p.runs; plan[3] = own;
+    return CQ_OK;
 }
 
 }  // extern "C"

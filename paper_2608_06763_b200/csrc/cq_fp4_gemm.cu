@@ -658,6 +658,17 @@ bool fp4_few_ok(int64_t M, int64_t N, int64_t K) {
     const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
     return most <= FEW_TILES && M * most <= FEW_MOST;
 }
+// what launch_fp4_few (own) or launch_fp4_gemm takes for M rows; routed: of E matrices
+static Plan plan_of(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, int fmt) {
+    const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB);
+    if (routed) return routed_plan(M / E);
+    return M <= FEW_ROWS ? Plan{SMALL, 64, lg_runs_of(NB, KT, sm_count())} : dense_plan(M, NB, KT, fmt);
+}
+Fp4Plan fp4_plan(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, int fmt, bool own) {
+    if (own) return Fp4Plan{128, FEW_ROWS, 1 << lg_runs_of((int)((N + 127) / 128), (int)((K + KB - 1) / KB), sm_count())};
+    const Plan q = plan_of(E, routed, M, N, K, fmt);
+    return Fp4Plan{q.mode == TWO ? 256 : 128, q.bt, 1 << q.lg};
+}
 cudaError_t launch_fp4_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, const float *x_scale, int fmt, uint16_t *y, int64_t M, int64_t N, int64_t K,
                            bool f16, int *status, cudaStream_t st) {
     GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
@@ -673,7 +684,7 @@ cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, 
     GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
     p.early = early;
     p.x = (const uint8_t *)x; p.offset = offset; p.E = E;
-    const Plan q = offset ? routed_plan(M / E) : M <= FEW_ROWS ? Plan{SMALL, 64, lg_runs_of(p.NB, p.KT, sm_count())} : dense_plan(M, p.NB, p.KT, fmt);
+    const Plan q = plan_of(E, offset != nullptr, M, N, K, fmt);
     p.bt = q.bt;
     p.token_tiles = (int)((M + q.bt - 1) / q.bt);
     const int ctas = q.mode == TWO ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sm_count() / ctas;

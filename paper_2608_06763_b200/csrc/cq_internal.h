@@ -160,6 +160,9 @@ cudaError_t launch_fp4_exchange(uint8_t *codes, uint8_t *scales, const Fp4Rows &
 bool fp4_few_ok(int64_t M, int64_t N, int64_t K);
 cudaError_t launch_fp4_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, const float *x_scale, int fmt, uint16_t *y, int64_t M, int64_t N, int64_t K,
                            bool f16, int *status, cudaStream_t st);
+// how the product is cut: channels and rows of x to an output tile, runs of K that share one; own: launch_fp4_few, else launch_fp4_gemm
+struct Fp4Plan { int channels, rows, runs; };
+Fp4Plan fp4_plan(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, int fmt, bool own);
 // y[M][N] = x W^T of two layouts; offset != null: E groups of rows, group e times matrix e; early: the kernel in front is launch_fp4_quantize of x
 cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, int fmt, uint16_t *y, int64_t M,
                             int64_t N, int64_t K, bool f16, bool early, int *status, cudaStream_t st);

@@ -36,6 +36,7 @@ def _lib():
                            ("linear_routed", [vp, vp, vp, i64, i64, vp, vp, vp, i64, i, vp, i, i64, i64, i64, vp, sz, vp])):
             fn = getattr(L, "cq_fp4_" + name)
             fn.restype, fn.argtypes = i, args
+        L.cq_debug_fp4_plan.restype, L.cq_debug_fp4_plan.argtypes = i, [i, i64, i64, i64, i64, i, vp]
         _L = L
     return _L
 
@@ -332,3 +333,10 @@ def cq_fp4_gemm_routed(w: Fp4Tensor, x, route_token: torch.Tensor | None, expert
         if status != 0:
             _check(status, "cq_fp4_gemm_routed")
     return out
+
+
+def cq_debug_fp4_plan(fmt: int, M: int, N: int, K: int, matrices: int = 0, quantised: bool = False) -> dict:
+    """How cq_fp4_gemm (matrices = 0) or cq_fp4_gemm_routed cuts a product of M rows on the current device."""
+    out = (C.c_int64 * 4)()
+    _check(_lib().cq_debug_fp4_plan(fmt, matrices, M, N, K, 1 if quantised else 0, out), "cq_debug_fp4_plan")
+    return {"channels": out[0], "rows": out[1], "runs": out[2], "quantises": bool(out[3])}

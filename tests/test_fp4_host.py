@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2608_06763_b200 as cq
+from fp4_shapes import PRODUCTS, ROUTED
 from oracle import fp4 as ref
 from paper_2608_06763_b200.fp4 import _lib
 
@@ -184,3 +185,37 @@ def test_products_of_quantised_rows_refuse_an_out_of_another_type(dtype):
     for bad in (lambda: cq.cq_fp4_gemm(w, x, out=out), lambda: cq.cq_fp4_gemm_routed(w, routed, None, off, out=out)):
         with pytest.raises(cq.CubicQuantError, match="out is"):
             bad()
+
+
+def _cut(fmt, M, N, K, **how):
+    return tuple(cq.cq_debug_fp4_plan(fmt, M, N, K, **how).values())
+
+
+def test_tested_products_reach_every_kind_of_tile():
+    """What the sizes of the GPU tests are for: no kind that a product of any size takes is left out."""
+    rng = np.random.default_rng(4)
+    for fmt in (0, 1):
+        for plan, M, N, K in PRODUCTS:
+            assert _cut(fmt, M, N, K) == plan, (fmt, M, N, K)
+        kinds = {(p, N % 8 == 0) for p, _, N, _ in PRODUCTS}
+        for _ in range(6000):
+            M, N, K = int(2 ** rng.uniform(0, 12.5)), int(2 ** rng.uniform(0, 16)), 32 * int(2 ** rng.uniform(0, 10))
+            p = _cut(fmt, M, N, K)
+            assert (p, N % 8 == 0) in kinds, (fmt, M, N, K, p)
+            if not p[3]:
+                assert _cut(fmt, M, N, K, quantised=True) == p
+            else:
+                assert _cut(fmt, M, N, K, quantised=True) == (128, 64, p[2], False)
+        for plan, counts, N, K in ROUTED:
+            assert _cut(fmt, sum(counts), N, K, matrices=len(counts)) == plan + (1, False)
+        routed = {p for p, _, _, _ in ROUTED}
+        assert all(_cut(fmt, R, 512, 512, matrices=E)[:2] in routed for E in (1, 3, 16, 512) for R in (1, 60, 800, 5000, 200000))
+
+
+def test_debug_plan_refuses():
+    L, plan = _lib(), (ctypes.c_int64 * 4)()
+    assert L.cq_debug_fp4_plan(1, 0, 4, 128, 256, 0, plan) == 0
+    assert L.cq_debug_fp4_plan(1, 0, 4, 128, 256, 0, None) == -1 and L.cq_debug_fp4_plan(2, 0, 4, 128, 256, 0, plan) == -1
+    assert L.cq_debug_fp4_plan(1, -1, 4, 128, 256, 0, plan) == -1 and L.cq_debug_fp4_plan(1, 0, 0, 128, 256, 0, plan) == -1
+    assert L.cq_debug_fp4_plan(1, 0, 4, 128, 264, 0, plan) == -2 and L.cq_debug_fp4_plan(1, 513, 4, 128, 256, 0, plan) == -2
+    assert L.cq_debug_fp4_plan(1, 0, 1 << 30, 1 << 30, 256, 0, plan) == -2

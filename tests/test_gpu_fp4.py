@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paper_2608_06763_b200 as cq
+from fp4_shapes import PRODUCTS, ROUTED
 from oracle import fp4 as ref
 
 pytestmark = pytest.mark.gpu
@@ -465,3 +466,32 @@ def test_odd_numbers_of_k_tiles_over_many_output_tiles(M, N, K, fmt):
         if i % 20 == 0:
             assert torch.equal(out, want)
     assert torch.equal(out, want) and cq.cq_gemm_status(ws) == 0
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("plan,M,N,K", PRODUCTS)
+def test_every_kind_of_tile(plan, M, N, K, fmt):
+    """bfloat16 and binary16 in turn; from rows in the model dtype and from quantised ones, which have the same bits."""
+    assert tuple(cq.cq_debug_fp4_plan(FMT[fmt], M, N, K).values()) == plan
+    w, x, g, y, S = product_case(M, N, K, fmt, "bf16" if (M + (fmt == "nv")) % 2 else "f16", seed=M)
+    ws = cq.cq_fp4_workspace(w, M)
+    got = cq.cq_fp4_gemm(w, x, g, workspace=ws)
+    check_product(got, y, S, K)
+    q = cq.cq_fp4_quantize(x, FMT[fmt], g)
+    out = torch.full_like(got, 7.0)
+    assert torch.equal(cq.cq_fp4_gemm(w, q, workspace=ws, out=out), got)
+    assert cq.cq_gemm_status(ws) == 0
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("plan,counts,N,K", ROUTED)
+def test_every_kind_of_routed_tile(plan, counts, N, K, fmt):
+    R = sum(counts)
+    assert tuple(cq.cq_debug_fp4_plan(FMT[fmt], R, N, K, matrices=len(counts)).values()) == plan + (1, False)
+    w, x, token, off, g, y, S = routed_case(counts, N, K, fmt, "bf16" if fmt == "nv" else "f16", seed=N, T=150)
+    ws = cq.cq_fp4_workspace(w, R)
+    got = cq.cq_fp4_gemm_routed(w, x, token, off, g, workspace=ws)
+    check_product(got, y, S, K)
+    q = cq.cq_fp4_quantize(x, FMT[fmt], g, route_token=token, expert_offset=off)
+    assert torch.equal(cq.cq_fp4_gemm_routed(w, q, None, off, workspace=ws, out=torch.full_like(got, 7.0)), got)
+    assert cq.cq_gemm_status(ws) == 0
