@@ -495,3 +495,65 @@ def test_every_kind_of_routed_tile(plan, counts, N, K, fmt):
     q = cq.cq_fp4_quantize(x, FMT[fmt], g, route_token=token, expert_offset=off)
     assert torch.equal(cq.cq_fp4_gemm_routed(w, q, None, off, workspace=ws, out=torch.full_like(got, 7.0)), got)
     assert cq.cq_gemm_status(ws) == 0
+
+
+def repaired(offset, R):
+    """Offsets as the calls take them: the largest so far, within [0, R]."""
+    return np.maximum.accumulate(np.clip(offset, 0, R))
+
+
+ASTRAY = {
+    "descends": [0, 10, 5, 28], "behind the rows": [0, 10, 22, 99], "negative": [-3, 10, 22, 28], "starts late": [4, 10, 12, 28], "starts behind": [41, 0, 0, 0],
+    "all at once": [9, -5, 200, 3],
+    # over the 32 offsets that one step of the scan takes, and over 64 of them
+    "descends at 31": list(range(32)) + [3, 4] + [35] * 6, "descends at 32": list(range(33)) + [7] * 4 + [38], "falls behind 31": [5] * 31 + [39] + list(range(10)),
+    "long": [3] + [2 * i if i % 5 else -i for i in range(1, 20)] + [38] * 30 + [0] * 15 + [40] * 10, "thirty-two": list(range(0, 33)), "thirty-one": list(range(0, 32)),
+}
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("name", ASTRAY)
+def test_offsets_that_go_astray(name, fmt):
+    """Every row against the matrix that it belongs to by the rule in the header; rows of no group are left as they were: by product, quantiser,
+    gated activation and inverse."""
+    offset, R, N, K, I = ASTRAY[name], 40, 136, 256, 64
+    E = len(offset) - 1
+    r = np.random.default_rng(E)
+    gw = np.linspace(0.0005, 0.002, E).astype(np.float32)
+    gx = 0.03 if fmt == "nv" else 1.0
+    W = [ref.quantize(r.standard_normal((N, K)) * 0.05, fmt, float(gw[e])) for e in range(E)]
+    w = cq.cq_fp4_pack(torch.from_numpy(np.stack([ref.pack(c) for c, _ in W])).cuda(), torch.from_numpy(np.stack([b for _, b in W])).cuda(), FMT[fmt],
+                       None if fmt == "mx" else torch.from_numpy(gw).cuda())
+    x, token = rows(50, K, "bf16", 7, 0.3), r.integers(0, 50, R).astype(np.int32)
+    off = torch.tensor(offset, dtype=torch.int32, device="cuda")
+    true = repaired(offset, R)
+    mine = np.zeros(R, bool)
+    mine[true[0]:true[-1]] = True
+    xc, xb = ref.quantize(as64(x), fmt, gx)
+    y, S = np.zeros((R, N)), np.zeros((R, N))
+    for e in range(E):
+        part = slice(true[e], true[e + 1])
+        if true[e] < true[e + 1]:
+            y[part], S[part] = ref.product(xc[token[part]], xb[token[part]], *W[e], fmt, gx, float(gw[e]) if fmt == "nv" else 1.0)
+    ws = cq.cq_fp4_workspace(w, R)
+    out = torch.full((R, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    q = cq.cq_fp4_quantize(x.cuda(), FMT[fmt], g_of(fmt, gx), route_token=torch.from_numpy(token).cuda(), expert_offset=off)
+    for call in (lambda: cq.cq_fp4_gemm_routed(w, x.cuda(), torch.from_numpy(token).cuda(), off, g_of(fmt, gx), workspace=ws, out=out),
+                 lambda: cq.cq_fp4_gemm_routed(w, q, None, off, workspace=ws, out=out)):
+        out.fill_(7.0)
+        call()
+        if mine.any():
+            check_product(out[torch.from_numpy(mine).cuda()], y[mine], S[mine], K)
+        assert torch.all(out[torch.from_numpy(~mine).cuda()] == 7.0)
+    assert cq.cq_gemm_status(ws) == 0
+    back = cq.cq_fp4_dequantize(q, out=torch.full((R, K), 7.0, device="cuda"))
+    want = np.where(mine[:, None], ref.values(xc, xb, fmt, gx).astype(np.float32)[token].astype(np.float64), 7.0)
+    assert np.array_equal(as64(back), want)
+    h = rows(R, 2 * I, "bf16", 8, 0.3)
+    v = as64(h)
+    act = torch.from_numpy(ref.gated(v[:, :I], v[:, I:])).to(torch.bfloat16)
+    g2 = 0.11 if fmt == "nv" else 1.0
+    a = cq.cq_fp4_swiglu_quantize(h.cuda(), FMT[fmt], g_of(fmt, g2), expert_offset=off)
+    back = cq.cq_fp4_dequantize(a, out=torch.full((R, I), 7.0, device="cuda"))
+    want = np.where(mine[:, None], ref.values(*ref.quantize(as64(act), fmt, g2), fmt, g2).astype(np.float32).astype(np.float64), 7.0)
+    assert np.array_equal(as64(back), want)
