@@ -51,7 +51,7 @@ __device__ __forceinline__ void scan_groups(const int32_t *offset, int E, int R,
         int o = max(e <= E ? min(max(offset[e], 0), R) : 0, top);
         int before = __shfl_up_sync(~0u, o, 1);
         if (lane == 0) before = e0 == 0 ? o : top;
-        if (__any_sync(~0u, e <= E ? o < before : o != top)) {   // not ascending, or the last 32 of them
+        if (__any_sync(~0u, e <= E && o < before)) {   // not ascending
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int v = __shfl_up_sync(~0u, o, d);
@@ -60,6 +60,7 @@ __device__ __forceinline__ void scan_groups(const int32_t *offset, int E, int R,
             before = __shfl_up_sync(~0u, o, 1);
             if (lane == 0) before = e0 == 0 ? o : top;
         }
+        // behind E the counts mean nothing, and nobody reads them
         int b = (o - before + ROWS - 1) / ROWS, n = s_item ? (o - before + bt - 1) / bt : 0;   // row blocks and tiles of the group that ends here
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {

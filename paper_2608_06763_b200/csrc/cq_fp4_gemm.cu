@@ -58,11 +58,11 @@ __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
 __device__ __forceinline__ uint64_t smem_desc_plain(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)8 << 16) | ((uint64_t)8 << 32) | ((uint64_t)1 << 46);
 }
-// Instruction descriptor: e2m1 both, scale type (bit 23: e8m0), M = 128 (a pair 256), N by the tile.  sf: which scales of a 32-bit column an
-// MXFP4 step takes (0: the first two, 2: the last two).
+// Instruction descriptor: e2m1 both, scale type (bit 23: e8m0), M = 128 (a pair 256), N by the tile.  Bits 4 and 29 up, added where it is
+// used: which scales of a 32-bit column an MXFP4 step takes (0: the first two, 2: the last two).
 template <int FMT, bool PAIR>
-__device__ __forceinline__ uint32_t idesc_fp4(uint32_t n, uint32_t sf) {
-    return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (FMT == MX ? 1u << 23 : 0u) | ((PAIR ? 2u : 1u) << 27) | (sf << 4) | (sf << 29);
+__device__ __forceinline__ uint32_t idesc_fp4(uint32_t n) {
+    return (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (FMT == MX ? 1u << 23 : 0u) | ((PAIR ? 2u : 1u) << 27);
 }
 
 // accumulators to registers in the order of 8x8 matrices: lane l has row l / 4 (+ 8), columns 8 i + 2 (l % 4) and the next
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             const Item t = tiles.at(local);
             const uint32_t n = MODE == FEW ? FEW_ROWS : __reduce_max_sync(~0u, columns_of<PAIR>(t.rows)), sf_row = PAIR || MODE == SMALL ? __reduce_max_sync(~0u, t.off / 32) : 0;   // a tile may start inside a row block
             const int acc = local & (ACCS - 1);
-            const uint32_t d = TMEM + (acc * MMAS + odd) * ACC_COLS, desc = idesc_fp4<FMT, PAIR>(n, 0);
+            const uint32_t d = TMEM + (acc * MMAS + odd) * ACC_COLS, desc = idesc_fp4<FMT, PAIR>(n);
             if (half == 0 && local >= ACCS) ok = uniform_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 53, dead);
             tc::tc_fence_after();
             bool idle = true;

@@ -14,14 +14,8 @@ struct Rows {
     int E;                        // groups, or matrices of `per` rows each
     int64_t per, rows, T;         // rows of one matrix; all rows; rows that x has
 };
-// the row among the padded rows of the layout, or -1
-__device__ __forceinline__ int64_t padded_row(const Rows &q, int64_t r, const int *s_off, const int *s_blk) {
-    if (r >= q.rows) return -1;
-    if (q.offset) {
-        if (r >= s_off[q.E]) return -1;
-        const int e = find_group(s_off, q.E, (int)r);
-        return (int64_t)s_blk[e] * ROWS + ((int)r - s_off[e]);
-    }
+// the row among the padded rows of the layout of dense rows
+__device__ __forceinline__ int64_t padded_row(const Rows &q, int64_t r) {
     if (q.E == 1) return r;
     const int64_t e = r / q.per;
     return e * ((q.per + ROWS - 1) / ROWS * ROWS) + (r - e * q.per);
@@ -351,7 +345,7 @@ __global__ void __launch_bounds__(256) exchange_kernel(uint8_t *codes, uint8_t *
     for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (int64_t)gridDim.x * 256) {
         const int64_t row = idx / KU;
         const int unit = (int)(idx - row * KU), u = unit & 15;
-        const int64_t k = (int64_t)unit * 16, prow = padded_row(q, row, nullptr, nullptr);
+        const int64_t k = (int64_t)unit * 16, prow = padded_row(q, row);
         const int r = (int)(prow & (ROWS - 1));
         uint8_t *tile = layout + ((prow >> 7) * KT + (unit >> 4)) * (int64_t)tile_bytes(FMT);
         uint2 *at = reinterpret_cast<uint2 *>(tile + code_offset(r, u * 8));
