@@ -557,3 +557,39 @@ def test_offsets_that_go_astray(name, fmt):
     back = cq.cq_fp4_dequantize(a, out=torch.full((R, I), 7.0, device="cuda"))
     want = np.where(mine[:, None], ref.values(*ref.quantize(as64(act), fmt, g2), fmt, g2).astype(np.float32).astype(np.float64), 7.0)
     assert np.array_equal(as64(back), want)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,dtype", [(1, "bf16"), (5, "f16"), (200, "bf16")])
+def test_mlp_as_it_is_used(M, dtype, fmt):
+    """gate | up, gated activation, down of a dense layer from a captured graph, one workspace for both products."""
+    H, I = 512, 1376
+    g1, g2 = (1.0, 1.0) if fmt == "mx" else (0.03, 0.09)
+    r = np.random.default_rng(31)
+    up, down = ref.quantize(r.standard_normal((2 * I, H)) * 0.06, fmt, 0.001), ref.quantize(r.standard_normal((H, I)) * 0.06, fmt, 0.001)
+    load = lambda c, b: cq.cq_fp4_pack(torch.from_numpy(ref.pack(c)).cuda(), torch.from_numpy(b).cuda(), FMT[fmt], g_of(fmt, 0.001))  # noqa: E731
+    wu, wd = load(*up), load(*down)
+    x = torch.zeros((M, H), dtype=DTYPE[dtype], device="cuda")
+    ws = cq.cq_fp4_workspace(wu, M)
+    h, a, y = torch.zeros((M, 2 * I), dtype=x.dtype, device="cuda"), cq.cq_fp4_empty(FMT[fmt], M, I), torch.zeros((M, H), dtype=x.dtype, device="cuda")
+    s1, s2 = g_of(fmt, g1), g_of(fmt, g2)
+
+    def mlp():
+        cq.cq_fp4_gemm(wu, x, s1, workspace=ws, out=h)
+        cq.cq_fp4_gemm(wd, cq.cq_fp4_swiglu_quantize(h, FMT[fmt], s2, out=a), workspace=ws, out=y)
+
+    mlp()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mlp()
+    for seed in range(3):
+        xs = rows(M, H, dtype, 200 + seed, 0.3)
+        x.copy_(xs)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_product(h, *ref.product(*ref.quantize(as64(xs), fmt, g1), *up, fmt, g1, 0.001), H)
+        hv = as64(h)   # from here on by what the first product returned
+        act = torch.from_numpy(ref.gated(hv[:, :I], hv[:, I:])).to(x.dtype)
+        check_product(y, *ref.product(*ref.quantize(as64(act), fmt, g2), *down, fmt, g2, 0.001), I)
+    assert cq.cq_gemm_status(ws) == 0
