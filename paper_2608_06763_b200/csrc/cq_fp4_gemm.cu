@@ -28,9 +28,14 @@ struct GemmArgs {
 // What a CTA computes.  ONE: 128 channels x up to 128 rows of x; TWO: a pair of CTAs 256 channels x up to 256 rows; FEW: 128 channels x up to 16
 // rows, which it quantises itself and keeps in shared memory; SMALL: 128 channels x up to 64 rows.
 enum { ONE = 0, TWO = 1, FEW = 2, SMALL = 3 };
-// rows, and k tiles of them, that fit beside the ring; and their product up to which a CTA's own quantising (0.5 us for sixteen of it) costs no
-// more than a launch for it.  us, by itself / in front: 16: 6.3 / 7.7; 32: 6.9 / 7.8; 52: 8.1 / 8.0; 64: 14.9 / 15.1; 128: 18.4 / 15.2.
-constexpr int FEW_ROWS = 16, FEW_TILES = 16, FEW_MOST = 64;
+// rows, and k tiles of them, that fit beside the ring
+constexpr int FEW_ROWS = 16, FEW_TILES = 16;
+// A CTA quantises rows x k tiles, sixteen of their product at a time (0.5 us), while its weights come; in front of it that is a launch.  Where the
+// first costs no more.  us, by itself / in front, MXFP4: 32: 6.4 / 6.8 (8 rows, 4096 x 4096), 13.4 / 15.4 (2 rows, 28672 x 4096); 48: 6.9 / 6.9 (12 rows,
+// 4096 x 4096), 6.6 / 6.8 (12, 8192 x 2048), 14.3 / 15.5 (3, 28672 x 4096); 52 to 64 with many rows: 7.4 / 7.0 (13 and 16, 4096 x 4096), 7.1 / 6.8
+// (13 and 16, 8192 x 2048); with many k tiles, which take longer themselves: 10.8 / 11.5 (4, 4096 x 14336), 14.9 / 15.4 (4, 28672 x 4096), 7.1 / 7.6 (8,
+// 2048 x 8192), 7.4 / 7.4 (8, 6144 x 4096); beyond 64: 11.3 / 11.2 (5, 4096 x 14336), 15.5 / 15.6 (5, 28672 x 4096), 12.1 / 11.5 (6, 4096 x 14336).
+constexpr int few_most(int rows) { return rows <= 8 ? 64 : 48; }
 
 // D[tmem] (+)= A B, codes by shared-memory descriptors, scales in tensor memory.  PAIR: by the tensor cores of two SMs, each with 128 of
 // the 256 rows of A and half of the columns of B in its shared memory.
@@ -656,7 +661,7 @@ static Plan routed_plan(int64_t mean) { return mean > 256 ? Plan{TWO, 256, 0} : 
 bool fp4_few_ok(int64_t M, int64_t N, int64_t K) {
     if (M > FEW_ROWS) return false;
     const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
-    return most <= FEW_TILES && M * most <= FEW_MOST;
+    return most <= FEW_TILES && M * most <= few_most((int)M);
 }
 // what launch_fp4_few (own) or launch_fp4_gemm takes for M rows; routed: of E matrices
 static Plan plan_of(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, int fmt) {

@@ -219,3 +219,11 @@ def test_debug_plan_refuses():
     assert L.cq_debug_fp4_plan(1, -1, 4, 128, 256, 0, plan) == -1 and L.cq_debug_fp4_plan(1, 0, 0, 128, 256, 0, plan) == -1
     assert L.cq_debug_fp4_plan(1, 0, 4, 128, 264, 0, plan) == -2 and L.cq_debug_fp4_plan(1, 513, 4, 128, 256, 0, plan) == -2
     assert L.cq_debug_fp4_plan(1, 0, 1 << 30, 1 << 30, 256, 0, plan) == -2
+
+
+def test_products_quantise_themselves_where_that_was_measured_faster():
+    own = lambda M, N, K: [cq.cq_debug_fp4_plan(fmt, M, N, K)["quantises"] for fmt in (0, 1)]  # noqa: E731
+    for M, N, K in ((12, 4096, 4096), (16, 1024, 2048), (4, 28672, 4096), (4, 4096, 14336), (8, 2048, 8192), (12, 8192, 2048), (6, 6144, 4096)):
+        assert own(M, N, K) == [True, True], (M, N, K)
+    for M, N, K in ((13, 4096, 4096), (16, 4096, 4096), (13, 8192, 2048), (16, 8192, 2048), (5, 28672, 4096), (6, 4096, 14336), (11, 2048, 8192)):
+        assert own(M, N, K) == [False, False], (M, N, K)
