@@ -593,3 +593,96 @@ def test_mlp_as_it_is_used(M, dtype, fmt):
         act = torch.from_numpy(ref.gated(hv[:, :I], hv[:, I:])).to(x.dtype)
         check_product(y, *ref.product(*ref.quantize(as64(act), fmt, g2), *down, fmt, g2, 0.001), I)
     assert cq.cq_gemm_status(ws) == 0
+
+
+def test_quantize_all_f16_values():
+    p = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.float16)
+    x = torch.zeros((65536, 32), dtype=torch.float16)
+    x[:, 3] = p
+    x[:, 4] = p.flip(0)
+    x[:, 20] = p.roll(77)
+    for fmt in ("mx", "nv"):
+        q = cq.cq_fp4_quantize(x.cuda(), FMT[fmt])
+        check_bytes(q, *ref.quantize(as64(x), fmt))
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K", [(1, 300, 512), (9, 300, 512), (16, 600, 8192), (70, 300, 512), (300, 9843, 864)])
+def test_rows_apart(M, N, K, fmt):
+    """x as columns of a wider matrix, a single row at any distance, the factor with and without an axis: the bits of a copy."""
+    w, x, g, y, S = product_case(M, N, K, fmt, "bf16")
+    want = cq.cq_fp4_gemm(w, x, g)
+    check_product(want, y, S, K)
+    wide = torch.full((M, K + 96), float("nan"), dtype=x.dtype, device="cuda")
+    wide[:, 64:64 + K] = x
+    part = wide[:, 64:64 + K]
+    assert part.stride(0) == K + 96
+    assert torch.equal(cq.cq_fp4_gemm(w, part, None if g is None else g.reshape(1)), want)
+    token, off = torch.arange(M, dtype=torch.int32, device="cuda"), torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    routed = cq.cq_fp4_gemm_routed(w, part, token, off, g)
+    check_product(routed, y, S, K)
+    assert torch.equal(cq.cq_fp4_gemm_routed(w, x, token, off, g), routed)
+    if M == 1:
+        odd = torch.zeros((3, K + 8), dtype=x.dtype, device="cuda")
+        odd[1, :K] = x[0]
+        assert torch.equal(cq.cq_fp4_gemm(w, odd[1:2, :K].as_strided((1, K), (3, 1), odd[1].storage_offset()), g), want)
+    I = K // 64 * 32
+    h = torch.full((M, 2 * I + 32), float("nan"), dtype=x.dtype, device="cuda")
+    h[:, 16:16 + 2 * I] = x[:, :2 * I]
+    a, b = cq.cq_fp4_swiglu_quantize(h[:, 16:16 + 2 * I], FMT[fmt], g), cq.cq_fp4_swiglu_quantize(x[:, :2 * I], FMT[fmt], g)
+    assert all(torch.equal(s, t) for s, t in zip(cq.cq_fp4_unpack(a), cq.cq_fp4_unpack(b)))
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_as_many_groups_as_there_may_be(fmt):
+    r = np.random.default_rng(12)
+    counts = r.integers(0, 4, 512)
+    counts[[0, 31, 32, 511]] = 0, 140, 1, 2
+    w, x, token, off, g, y, S = routed_case(counts.tolist(), 40, 96, fmt, "bf16")
+    ws = cq.cq_fp4_workspace(w, int(counts.sum()))
+    check_product(cq.cq_fp4_gemm_routed(w, x, token, off, g, workspace=ws), y, S, 96)
+    assert cq.cq_gemm_status(ws) == 0
+    with pytest.raises(cq.CubicQuantError):
+        cq.cq_fp4_quantize(x, FMT[fmt], g, route_token=token, expert_offset=torch.zeros(514, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("M,N,K", [(4, 300, 512), (100, 300, 512)])
+def test_rows_of_zeros_under_their_own_factor(M, N, K):
+    """max|x| / 2688 of a matrix of zeros is zero: so are its values and its products."""
+    w, x, _, _, _ = product_case(M, N, K, "nv", "bf16")
+    x.zero_()
+    g = x.abs().amax().float() / 2688
+    assert torch.all(cq.cq_fp4_gemm(w, x, g) == 0)
+    assert torch.all(cq.cq_fp4_dequantize(cq.cq_fp4_quantize(x, cq.CQ_NVFP4, g)) == 0)
+
+
+@pytest.mark.parametrize("M", [4, 100])
+def test_captured_without_a_workspace_and_between_streams(M):
+    """What a call allocates for itself lives as long as the graph; operands that another stream makes are waited for by an event alone."""
+    w, x, g, y, S = product_case(M, 1024, 2048, "nv", "bf16")
+    want = cq.cq_fp4_gemm(w, x, g)
+    static = torch.zeros_like(x)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = cq.cq_fp4_gemm(w, static, g)
+    static.copy_(x)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want)
+    side = torch.cuda.Stream()
+    for _ in range(20):
+        late = torch.full_like(x, float("nan"))
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(200000)
+            late.copy_(x)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(cq.cq_fp4_gemm(w, late, g), want)
+        q = cq.cq_fp4_quantize(late, cq.CQ_NVFP4, g)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = cq.cq_fp4_gemm(w, q)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, want)
