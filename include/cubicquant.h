@@ -261,7 +261,7 @@ int cq_encode(const float *W, int B, int G, int64_t N, int64_t K, int objective,
  * consecutive k; weights AND activations are in it, and the tensor cores multiply them as they are.
  *   CQ_MXFP4  blocks of 32, scale byte b: 2^(b - 127), 255 is NaN.  Quantiser: b - 127 = floor(log2 max|x|) - 2, at least -127; the codes
  *             are x / scale to the nearest, ties to the even code, at most 6.
- *   CQ_NVFP4  blocks of 16, scale byte in e4m3 (127 is NaN), and one fp32 factor g > 0 for the whole matrix, given as
+ *   CQ_NVFP4  blocks of 16, scale byte in e4m3 (0 .. 126, and 127 for NaN; there is no sign, and a checkpoint has no other byte), and one fp32 factor g > 0 (0: values of finite blocks are zeros) for the whole matrix, given as
  *             `tensor_scale`: a DEVICE pointer to it (NULL: 1), read when the kernel runs.  Quantiser, in fp32 with IEEE roundings:
  *             r = 1 / g; scale = (max|x| r) / 6, at least 2^-9 and at most 448, to the nearest e4m3; i = r / scale; codes x i as above.
  *             (g = max|x| / 2688 over the matrix uses the whole range.)  The value of a code is code * (scale * g).
@@ -293,7 +293,8 @@ int cq_fp4_quantize(const void *x, int dtype, int64_t ldx, int fmt, int64_t E, i
 /* Routed rows: row r of the layout is row route_token[r] of x [T][K] (zeros for a token outside [0, T)), and belongs to the group e
  * with expert_offset[e] <= r < expert_offset[e + 1].  Both arrays are int32 on the DEVICE, R and E + 1 of them: no host
  * needs to know the loads, and a captured call follows them.  Offsets start at 0 and ascend, the last at most R; what does not is taken as
- * the largest offset so far, at most R.  Rows from the last offset on belong to nobody and are left alone.  tensor_scale: one factor. */
+ * the largest offset so far, at most R.  Rows in front of the first offset and from the last one on belong to nobody and are left alone.
+ * tensor_scale: one factor. */
 int cq_fp4_quantize_routed(const void *x, int dtype, int64_t ldx, int64_t T, const int32_t *route_token, const int32_t *expert_offset, int64_t E, int64_t R, int fmt,
                            int64_t K, const float *tensor_scale, void *layout, void *stream);
 /* h [M][2 I] (gate | up) -> silu(gate) * up, correctly rounded to the model dtype (from fp32), and at once quantised: what stands between

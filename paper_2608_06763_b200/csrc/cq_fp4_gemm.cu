@@ -285,7 +285,7 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
 // SPLIT: 2^lgS CTAs of a cluster share one output tile, each a run of its k tiles; the partial sums meet in the shared memory of the
 // cluster, where each CTA adds 128 / S channels in the order of the runs.  One tile a CTA then; else CTAs (pairs) take tiles in turn.
 // What bounds it.  256 x 256 tiles of pairs: a stage of 256 k is 512 cycles of the tensor core at its rate, and takes 640 with everything
-// around it (issuing 14 to 18 instructions a stage, a tile's accumulators read before the next tile starts); 57344 x 8192, 4096 rows 650 to 800 us, 4.8 to
+// around it (issuing 14 to 18 instructions a stage, a tile's accumulators read before the next tile starts); 57344 x 8192, 4096 rows 650 to 820 us, 4.7 to
 // 5.9 PFLOP/s, by what the power limit leaves of the clock; 8192 x 8192, 4096 rows 100 us in a burst with the tensor pipe 78 % active.  Copies come
 // as they are stored, a contiguous run each.  One CTA of 128 x 128 is bound by its SM's port to L2 (36.9 KB a stage, 600 cycles), small tiles by
 // memory: 28672 x 4096, 13 rows 13.1 us for 63 MB, of which some three are the launch, the first copies' way and the last tile's output, and
@@ -624,7 +624,9 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
 
 // What computes a product of more than sixteen rows: kind of tile, rows to a tile, runs of k (log2).  Costs in microseconds, from tiles forced in
 // turn.  A k tile of one CTA takes as long as an SM's port to L2 does for its bytes (113 bytes a nanosecond) but no less than its
-// MMAs take to issue; a pair's, 0.27 to 0.36.  Cutting k saves k tiles and costs a cluster's launch and the exchange.
+// MMAs take to issue; a pair's, 0.27 to 0.36.  Cutting k saves k tiles and costs a cluster's launch and the exchange.  Measured with quantised rows, two,
+// four and six rounds of pairs with 256 rows, K 1024 to 8192: 0.34 (MXFP4) to 0.355 (NVFP4) a k tile and 1.25 a tile on top (its only
+// accumulators are emptied before the next tile's first MMA): at K = 2048 31 % of a tile.
 //   4096 x 14336, 200 rows: SMALL 16.6, ONE 20.3 (two runs 16.3), TWO 20.5 to 22.2;  4096 x 4096, 64 rows: SMALL 6.4 (two runs 7.4), ONE 7.7, TWO 8.7;
 //   128 rows: SMALL 6.5, ONE 8.4;  512 rows: ONE 9.1, TWO 10.4 to 11.5;  6144 x 4096, 1024 rows: ONE 19.0, TWO 16.0 with 192 rows to a tile, 17.8 with 256;
 //   2048 x 8192, 400 rows: ONE in two runs 12.8, whole 17.3, TWO 14.1;  28672 x 4096, 512 rows: ONE 45.6, TWO 33.6 to 38.4

@@ -77,8 +77,8 @@ __device__ __forceinline__ void fill_factors(float *s_factor, float r) {
 
 // ---------------------------------------------------------------- the quantiser
 // Bound by memory and, for 16-bit values, by instructions alike: 2 (4) bytes read and 0.53 or 0.56 written a value, eleven instructions.  Measured:
-// 14336 x 4096 fp32 to MXFP4 44.5 us (6.0 TB/s, 0.91 of the copy rate), 4096 x 8192 bf16 to NVFP4 17.5 us (4.9 TB/s; issue slots 64 % used),
-// a row of 4096 2.7 us, most of it the way to memory and back.  A loop over single units with more threads at a time was 10 % slower.
+// 14336 x 4096 fp32 to MXFP4 44.6 us (6.0 TB/s, 0.91 of the copy rate), 4096 x 8192 bf16 to NVFP4 19.3 us (4.5 TB/s; issue slots 64 % used), to MXFP4
+// 18.6 us, a row of 4096 2.6 us, most of it the way to memory and back.  A loop over single units with more threads at a time was 10 % slower.
 template <int FMT, int DT>
 __global__ void __launch_bounds__(256) quantize_kernel(const void *x, int64_t ldx, Rows q, int64_t K, int KT, const float *tensor_scale, uint8_t *layout) {
     extern __shared__ int s_tab[];

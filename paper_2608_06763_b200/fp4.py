@@ -66,7 +66,8 @@ def _at(t):
 
 @dataclass
 class Fp4Tensor:
-    """Rows in the 4-bit device layout: `matrices` of M x K one after another, or (groups) M routed rows of K."""
+    """Rows in the 4-bit device layout: `matrices` of M x K one after another, or (groups) M routed rows of K.  Made by cq_fp4_empty,
+    cq_fp4_pack and the quantisers; calls take what it says of its layout as they find it."""
     layout: torch.Tensor
     fmt: int
     matrices: int
@@ -243,7 +244,8 @@ def cq_fp4_dequantize(q: Fp4Tensor, dtype: torch.dtype = torch.bfloat16, out: to
 
 
 def cq_fp4_workspace(w: Fp4Tensor, M: int) -> torch.Tensor:
-    """A zeroed workspace for products of up to M rows (routes) with w."""
+    """A zeroed workspace for products of up to M rows (routes) with w.  A program that keeps one saves each call its own, and can ask
+    cq_gemm_status of it whether a wait on the device gave up."""
     n = _lib().cq_fp4_routed_workspace_bytes(w.fmt, w.matrices, max(M, 1), w.K)
     return torch.zeros(max(n, 512), dtype=torch.uint8, device=w.layout.device)
 
