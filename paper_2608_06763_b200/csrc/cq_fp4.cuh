@@ -15,19 +15,16 @@
 // blocks of its own.  Codes and scales behind K are written as zeros; rows behind the last are never written, and
 // what they hold reaches no result (a row of an operand meets only its own row or column of the product).
 #pragma once
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <cuda_runtime.h>
-#include <stdint.h>
+#include "cq_rows.cuh"
 
 namespace cq {
 namespace fp4 {
 
+using namespace rows;
+
 constexpr int MX = 0, NV = 1;                 // CQ_MXFP4, CQ_NVFP4
-constexpr int DT_BF16 = 0, DT_F16 = 1, DT_F32 = 2;   // CQ_BF16, CQ_F16, CQ_F32
-constexpr int ROWS = 128, KB = 256;           // a tile
+constexpr int KB = 256;                       // a tile has ROWS rows and so many k
 constexpr int CODE_BYTES = ROWS * KB / 2;
-constexpr int MAX_EXPERTS = 512;              // the offsets' tables in shared memory
 
 __host__ __device__ constexpr int block_of(int fmt) { return fmt == MX ? 32 : 16; }
 __host__ __device__ constexpr int scale_bytes(int fmt) { return ROWS * KB / block_of(fmt); }
@@ -37,57 +34,6 @@ __host__ __device__ constexpr int tile_bytes(int fmt) { return CODE_BYTES + scal
 __host__ __device__ inline int code_offset(int r, int b) { return r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15); }
 // byte of a tile that holds scale j of row r, counted along k inside the tile
 __host__ __device__ inline int scale_offset(int r, int j) { return CODE_BYTES + (j >> 2) * 512 + (r & 31) * 16 + (r >> 5) * 4 + (j & 3); }
-
-// ---- groups of routed rows ------------------------------------------------------------------
-// offset[e] .. offset[e + 1] are the rows of group e, as the router left them on the GPU.  What does not ascend, or leaves
-// [0, R], is brought back into it: the largest value so far, at most R.  One warp writes the offsets and the first row
-// block of each group (E + 1 values each), and, for a product, its first tile (bt rows of x to a tile, `times` of them); the
-// block synchronises before it reads them.
-__device__ __forceinline__ void scan_groups(const int32_t *offset, int E, int R, int *s_off, int *s_blk, int *s_item = nullptr, int bt = 1, int times = 0) {
-    const int lane = threadIdx.x & 31;
-    int top = 0, blk = 0, item = 0;   // of what lies in front
-    for (int e0 = 0; e0 <= E; e0 += 32) {
-        const int e = e0 + lane;
-        int o = max(e <= E ? min(max(offset[e], 0), R) : 0, top);
-        int before = __shfl_up_sync(~0u, o, 1);
-        if (lane == 0) before = e0 == 0 ? o : top;
-        if (__any_sync(~0u, e <= E && o < before)) {   // not ascending
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int v = __shfl_up_sync(~0u, o, d);
-                if (lane >= d) o = max(o, v);
-            }
-            before = __shfl_up_sync(~0u, o, 1);
-            if (lane == 0) before = e0 == 0 ? o : top;
-        }
-        // behind E the counts mean nothing, and nobody reads them
-        int b = (o - before + ROWS - 1) / ROWS, n = s_item ? (o - before + bt - 1) / bt : 0;   // row blocks and tiles of the group that ends here
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int v = __shfl_up_sync(~0u, b, d), u = __shfl_up_sync(~0u, n, d);
-            if (lane >= d) { b += v; n += u; }
-        }
-        b += blk;
-        n += item;
-        if (e <= E) {
-            s_off[e] = o;
-            s_blk[e] = b;
-            if (s_item) s_item[e] = n * times;
-        }
-        top = __shfl_sync(~0u, o, 31);
-        blk = __shfl_sync(~0u, b, 31);
-        item = __shfl_sync(~0u, n, 31);
-    }
-}
-// the group that a row or a tile belongs to: the last e with table[e] <= v (v < table[E])
-__device__ __forceinline__ int find_group(const int *table, int E, int v) {
-    int lo = 0, hi = E;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (table[mid] <= v) lo = mid; else hi = mid;
-    }
-    return lo;
-}
 
 // ---- conversions ----------------------------------------------------------------------------
 // eight values to eight codes, the first in the lowest four bits; nearest, ties to the even code, saturating at 6
@@ -143,37 +89,6 @@ __device__ __forceinline__ uint32_t block_scale(uint32_t top, float r, const flo
     const uint32_t b = top >= 0x7F800000u ? 127u : to_e4m3(s);
     factor = factors ? factors[b] : b == 127u ? 0.0f : __fdiv_rn(r, from_e4m3(b));
     return b;
-}
-
-// ---------------------------------------------------------------- two fp32 operations an instruction, each rounded by itself
-using Pair = unsigned long long;
-__device__ __forceinline__ Pair pair_of(float a, float b) { Pair r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void unpair(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-
-// ---------------------------------------------------------------- sixteen values of a row
-__device__ __forceinline__ uint4 load16(const void *p) { return *reinterpret_cast<const uint4 *>(p); }
-template <int DT>
-__device__ __forceinline__ float value_of(const uint32_t *w, int i) {
-    const uint32_t h = (i & 1) ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu;
-    return DT == DT_BF16 ? __uint_as_float(h << 16) : __half2float(__ushort_as_half((unsigned short)h));
-}
-// bits of the largest magnitude of sixteen 16-bit values; NaN counts as the largest
-template <int DT>
-__device__ __forceinline__ uint32_t top_of_16bit(const uint32_t *w) {
-    if (DT == DT_BF16) {
-        __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[0]));
-#pragma unroll
-        for (int i = 1; i < 8; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i])));
-        const uint32_t b = *reinterpret_cast<uint32_t *>(&m) & 0x7FFF7FFFu;
-        return max(b << 16, b & 0xFFFF0000u);
-    }
-    __half2 m = __habs2(*reinterpret_cast<const __half2 *>(&w[0]));
-#pragma unroll
-    for (int i = 1; i < 8; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __half2 *>(&w[i])));
-    return max(__float_as_uint(__low2float(m)) & 0x7FFFFFFFu, __float_as_uint(__high2float(m)) & 0x7FFFFFFFu);
 }
 
 template <int FMT>
