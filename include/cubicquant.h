@@ -6,7 +6,8 @@
  * cubic (Section 2.2, Eq. cubic), in two activation modes (Section 5.3 model dtype,
  * Section 5.4 Dynamic A8).
  *
- * Besides, 4-bit floating point with block scales (last section): quantisers and products for checkpoints in that format.
+ * Besides, 4-bit floating point with block scales and 8-bit integers with a scale for each row: quantisers and products for checkpoints in
+ * those formats; and routing to experts (last sections).
  *
  * Conventions common to every call
  *   - All pointers are DEVICE pointers unless the name says "host".  The caller owns every
@@ -322,6 +323,90 @@ int cq_fp4_linear_routed(const void *w, const float *w_scale, const uint16_t *x,
  * cq_fp4_gemm; E > 0: the routed ones with E matrices.  plan must hold four values: channels and rows of x to an output tile (256 channels: a pair
  * of CTAs), the runs of K that share such a tile (1: none), and 1 when the product quantises x itself, without a launch in front. */
 int cq_debug_fp4_plan(int fmt, int64_t E, int64_t M, int64_t N, int64_t K, int quantised, int64_t *plan);
+
+/* ---- Routing to experts (no counterpart in the paper, which leaves it outside) ------------------------------
+ * What stands in front of a routed product and behind it: the choice of experts from a router's logits, with the route map that the
+ * routed products take, and the weighted sum of a token's routes. */
+enum { CQ_SOFTMAX = 0, CQ_SIGMOID = 1 };
+
+/* logits [T][E] of `dtype` (CQ_BF16, CQ_F16, CQ_F32), rows ldl elements apart, any alignment.
+ *   score s[e]: the softmax of a row, or the sigmoid of each logit; choice score c[e] = s[e] + bias[e] (fp32 [E], or NULL: 0).
+ *   groups > 1: experts fall into groups of E / groups neighbours; the score of a group is the sum of its group_best (1 or 2) largest choice
+ *     scores; experts of the groups_kept best groups alone may be chosen, of equals those of lower index.
+ *   The `top` experts of largest c in descending order; of those whose c is equal in 64 bits the larger logit, then the lower index comes first.
+ *   A logit of -inf or NaN, or a bias of -inf or NaN, excludes its expert; +inf is the largest number.
+ * expert [T][top]: the choices; -1 where fewer than `top` experts may be chosen (a row of -inf: padding; it has no routes).
+ * weight [T][top] fp32: s of the choices (without the bias), renormalise: over their sum; times scale; 0 where there is no choice.
+ * The map, R = T top:
+ *   expert_offset [E + 1]: routes of expert e are rows [expert_offset[e], expert_offset[e + 1]); the last one is the number of routes, at most R
+ *   route_token [R]: the tokens of the routes, grouped by expert, ascending within each; -1 from the last offset on
+ *   route_row [T][top]: the row of each choice among the routes; -1 for none
+ * The outputs do not depend on timing.  One launch up to 64 tokens, two beyond.
+ * Errors: CQ_ERR_INVALID_ARG (also: E not a multiple of groups, top beyond the experts of the kept groups), CQ_ERR_UNSUPPORTED (E > 512,
+ * groups > 32, top > 32, T top > 2^30). */
+size_t cq_route_workspace_bytes(int64_t T, int64_t E);
+int cq_route(const void *logits, int dtype, int64_t ldl, int64_t T, int64_t E, int top, int score, const float *bias, int groups, int groups_kept, int group_best, int renormalise,
+             float scale, int32_t *expert, float *weight, int32_t *route_token, int32_t *expert_offset, int32_t *route_row, void *workspace, size_t workspace_bytes, void *stream);
+
+/* y[t] = add[t] + sum over j of weight[t][j] y_routes[route_row[t][j]], in fp32 and in the order of j, rounded once.  y_routes [R][N], add [T][N] (NULL:
+ * none; may be y) and y [T][N] in bfloat16 or (act_f16) binary16, rows ldr, lda, ldy elements apart.  A row outside [0, R) is no
+ * route; nothing is read of it. */
+int cq_combine(const uint16_t *y_routes, int64_t ldr, int64_t R, const float *weight, const int32_t *route_row, int64_t T, int top, int64_t N, const uint16_t *add, int64_t lda,
+               uint16_t *y, int64_t ldy, int act_f16, void *stream);
+
+/* ---- 8-bit integers with a scale for each row (no counterpart in the paper) ---------------------------------
+ * A third stored format, for checkpoints of int8 codes with one fp32 scale for each output channel, and the operators that a linear layer, an MLP and
+ * routed experts need of it; activations are in it too, a scale for each token.  Sums of products of codes are exact integers.
+ *   Quantiser, of a row: d = max(max|x|, 1e-10) / 127, codes x / d (both IEEE fp32) to the nearest integer, halves away from zero: that of
+ *   cq_quantize_a8.  A row with an infinity or a NaN gets the scale NaN and codes 0; the products it enters are NaN.
+ * Canonical form: codes int8 [M][K], scale float [M].  Codes may be -128 (the quantiser makes none).  K is a multiple of 16, at most 2^17.
+ * The device layout is private (cq_i8_pack, cq_i8_unpack; quantisers write it directly); scales lie beside it, M of them, E M for the E
+ * matrices of one shape that lie one after another, R for routed rows.  Rows behind the last of a matrix or of a group are never
+ * written and reach no result.  Everything else, dtype, ldx, routed rows and their offsets, workspaces, errors, as in the section on 4-bit floating point.
+ * CQ_ERR_UNSUPPORTED: K not a multiple of 16 or beyond 2^17, more than 512 groups, sizes above 2^30. */
+size_t cq_i8_layout_bytes(int64_t E, int64_t M, int64_t K);
+size_t cq_i8_routed_layout_bytes(int64_t E, int64_t R, int64_t K);
+/* Of cq_i8_linear and cq_i8_linear_routed (the products of quantised rows need 512).  Zero it once with cq_workspace_init; cq_gemm_status
+ * reports a bounded wait that gave up in any call since then. */
+size_t cq_i8_workspace_bytes(int64_t M, int64_t K);
+size_t cq_i8_routed_workspace_bytes(int64_t E, int64_t R, int64_t K);
+
+/* Canonical codes to layout, and back (a bijection). */
+int cq_i8_pack(const int8_t *codes, int64_t E, int64_t M, int64_t K, void *layout, void *stream);
+int cq_i8_unpack(const void *layout, int64_t E, int64_t M, int64_t K, int8_t *codes, void *stream);
+
+/* The quantiser: E matrices of M rows; routed rows (offsets as for cq_fp4_quantize_routed; scales of rows of no group are left alone); and of silu(gate) * up,
+ * correctly rounded to the model dtype (from fp32), of rows of h [M][2 I] (gate | up). */
+int cq_i8_quantize(const void *x, int dtype, int64_t ldx, int64_t E, int64_t M, int64_t K, void *layout, float *scale, void *stream);
+int cq_i8_quantize_routed(const void *x, int dtype, int64_t ldx, int64_t T, const int32_t *route_token, const int32_t *expert_offset, int64_t E, int64_t R, int64_t K, void *layout,
+                          float *scale, void *stream);
+int cq_i8_swiglu_quantize(const void *h, int dtype, int64_t ldh, int64_t M, int64_t I, const int32_t *expert_offset, int64_t E, void *layout, float *scale, void *stream);
+/* code * scale, y [E M][K] (routed: [M][K], rows of no group left alone), rounded once to `dtype`. */
+int cq_i8_dequantize(const void *layout, const float *scale, int64_t E, int64_t M, int64_t K, const int32_t *expert_offset, void *y, int dtype, void *stream);
+
+/* y[M][N] = x W^T; w: layout and scales of the N x K matrix, x: layout and scales of M rows.  (float)sum * (w_scale * x_scale) in fp32, rounded
+ * to bfloat16 or (act_f16) binary16. */
+int cq_i8_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, uint16_t *y, int act_f16, int64_t M, int64_t N, int64_t K, void *workspace,
+               size_t workspace_bytes, void *stream);
+/* The same from rows in the model dtype (that of y), quantised on the way. */
+int cq_i8_linear(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, uint16_t *y, int act_f16, int64_t M, int64_t N, int64_t K, void *workspace, size_t workspace_bytes,
+                 void *stream);
+/* Routed: w holds E matrices, w_scale E N scales; rows of group e of x, y[R][N] meet matrix e.  Rows of y of no group are left as they were. */
+int cq_i8_gemm_routed(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *expert_offset, int64_t E, uint16_t *y, int act_f16, int64_t R, int64_t N,
+                      int64_t K, void *workspace, size_t workspace_bytes, void *stream);
+int cq_i8_linear_routed(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, int64_t T, const int32_t *route_token, const int32_t *expert_offset, int64_t E, uint16_t *y,
+                        int act_f16, int64_t R, int64_t N, int64_t K, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The experts of a layer in one call, behind cq_route: rows of x [T][H] quantised by route, gate | up (E matrices 2 I x H), gated activation, down (E matrices
+ * H x I), combined into y [T][H] (add: as for cq_combine).  Equal to cq_i8_linear_routed, cq_i8_swiglu_quantize, cq_i8_gemm_routed and cq_combine one after
+ * another.  workspace: cq_i8_moe_workspace_bytes() bytes, zeroed once. */
+size_t cq_i8_moe_workspace_bytes(int64_t E, int64_t T, int top, int64_t H, int64_t I);
+int cq_i8_moe(const void *gate_up, const float *gate_up_scale, const void *down, const float *down_scale, int64_t E, const uint16_t *x, int64_t ldx, int64_t T, int top,
+              const int32_t *route_token, const int32_t *expert_offset, const int32_t *route_row, const float *weight, const uint16_t *add, int64_t lda, uint16_t *y, int64_t ldy,
+              int act_f16, int64_t H, int64_t I, void *workspace, size_t workspace_bytes, void *stream);
+
+/* How a product of M rows is cut on the current device: as cq_debug_fp4_plan, for cq_i8_linear, (quantised) cq_i8_gemm and, E > 0, the routed ones. */
+int cq_debug_i8_plan(int64_t E, int64_t M, int64_t N, int64_t K, int quantised, int64_t *plan);
 
 #ifdef __cplusplus
 }

@@ -167,4 +167,37 @@ Fp4Plan fp4_plan(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, int fm
 cudaError_t launch_fp4_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, int fmt, uint16_t *y, int64_t M,
                             int64_t N, int64_t K, bool f16, bool early, int *status, cudaStream_t st);
 
+// Routing to experts (cq_route.cu): T rows of E logits, `top` choices each; dtype, score and the rest as cq_route takes them.
+struct RouteCall {
+    const void *logits;
+    int dtype;
+    int64_t ldl, T;
+    int E, groups, kept, best, top;
+    const float *bias;
+    bool sigmoid, renormalise;
+    float scale;
+    int32_t *expert, *row, *token, *offset;
+    float *weight;
+    int32_t *counts;   // route_count_bytes(T, E)
+};
+size_t route_count_bytes(int64_t T, int64_t E);
+cudaError_t launch_route(const RouteCall &c, cudaStream_t st);
+cudaError_t launch_combine(const uint16_t *routes, int64_t ldr, int64_t R, const float *weight, const int32_t *row, int64_t T, int top, int64_t N, const uint16_t *add,
+                           int64_t lda, uint16_t *y, int64_t ldy, bool f16, cudaStream_t st);
+
+// 8-bit integers with a scale for each row (cq_i8_quant.cu, cq_i8_gemm.cu); rows as for Fp4Rows.
+struct I8Rows { const int32_t *route_token, *offset; int E; int64_t per, rows, T; };
+cudaError_t launch_i8_quantize(const void *x, int dtype, int64_t ldx, const I8Rows &rows, int64_t K, float *scale, void *layout, cudaStream_t st);
+cudaError_t launch_i8_swiglu_quantize(const void *h, int dtype, int64_t ldh, const I8Rows &rows, int64_t I, float *scale, void *layout, cudaStream_t st);
+cudaError_t launch_i8_dequantize(const void *layout, const I8Rows &rows, int64_t K, const float *scale, void *y, int dtype, cudaStream_t st);
+cudaError_t launch_i8_exchange(uint8_t *codes, const I8Rows &rows, int64_t K, void *layout, bool in, cudaStream_t st);
+// few rows in the model dtype, quantised by the product itself; for the sizes that i8_few_ok allows
+bool i8_few_ok(int64_t M, int64_t N, int64_t K);
+cudaError_t launch_i8_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, uint16_t *y, int64_t M, int64_t N, int64_t K, bool f16, int *status, cudaStream_t st);
+struct I8Plan { int channels, rows, runs; };
+I8Plan i8_plan(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, bool own);
+// y[M][N] = x W^T of two layouts; offset != null: E groups of rows, group e times matrix e; early: the kernel in front is the quantiser of x
+cudaError_t launch_i8_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, uint16_t *y, int64_t M, int64_t N, int64_t K,
+                           bool f16, bool early, int *status, cudaStream_t st);
+
 }  // namespace cq
