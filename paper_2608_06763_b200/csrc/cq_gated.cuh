@@ -53,14 +53,19 @@ __device__ __forceinline__ void gated_in_32_bits(float g0, float g1, float u0, f
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(d1));
     unpair(mul2(mul2(g, pair_of(u0, u1)), pair_of(e0, e1)), y0, y1);
 }
-// The least distance, as (bits - border + BAND) in the bits that rounding to the model dtype drops (binary16: in their eighths), of two values
-// and of those before; borders lie in the middle of these bits.
+// The bits that rounding two values to the model dtype drops (binary16: in their eighths), and how they become a distance: bits + ABOVE is
+// bits - border + BAND, at most 2 BAND (in such units) next to a border; borders lie in the middle of these bits.
+template <int DT> constexpr uint32_t ABOVE = (0x8000u + BAND * (DT == DT_BF16 ? 1u : 8u)) & 0xFFFFu;
 template <int DT>
-__device__ __forceinline__ uint32_t nearer(uint32_t near, float y0, float y1) {
+__device__ __forceinline__ uint32_t dropped(float y0, float y1) {
     const uint32_t low = __byte_perm(__float_as_uint(y0), __float_as_uint(y1), 0x5410);
-    constexpr uint32_t SHIFT = DT == DT_BF16 ? 1 : 8, ADD = (0x8000u + BAND * SHIFT) & 0xFFFFu;
-    return __viaddmin_u16x2(DT == DT_BF16 ? low : (low & 0x1FFF1FFFu) * 8u, ADD << 16 | ADD, near);
+    return DT == DT_BF16 ? low : (low & 0x1FFF1FFFu) * 8u;
 }
+// the least distance of what was dropped of two values and of those before
+template <int DT>
+__device__ __forceinline__ uint32_t nearer(uint32_t near, uint32_t bits) { return __viaddmin_u16x2(bits, ABOVE<DT> << 16 | ABOVE<DT>, near); }
+template <int DT>
+__device__ __forceinline__ uint32_t nearer(uint32_t near, float y0, float y1) { return nearer<DT>(near, dropped<DT>(y0, y1)); }
 
 }  // namespace rows
 }  // namespace cq

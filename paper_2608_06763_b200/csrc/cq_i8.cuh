@@ -26,12 +26,21 @@ __host__ __device__ inline int piece_offset(int r, int u) { return r * 128 + ((u
 __device__ __forceinline__ float row_scale(uint32_t top) {
     return top >= 0x7F800000u ? __uint_as_float(0x7FFFFFFFu) : __fdiv_rn(fmaxf(__uint_as_float(top), 1e-10f), 127.0f);
 }
-// Sixteen codes: x / d (a quotient rounded to fp32) to the nearest integer, halves away from zero; a row without a finite scale: zeros.
+// Codes: x / d (a quotient rounded to fp32) to the nearest integer, halves away from zero; a row without a finite scale: zeros.
 // The product with r = 1 / d is off by less than 127 * 3 * 2^-24 of the quotient, so where no product lies within BORDER of a half, its nearest
-// integer is that of the quotient; elsewhere (a unit in 800) the quotients are formed.  Adding 1.5 * 2^23 rounds to an integer and leaves it
-// in the low bits.
+// integer is that of the quotient.  Adding 1.5 * 2^23 rounds to an integer and leaves it in the low bits.  Elsewhere (a unit in 800) the quotient is
+// compared with the half h that it lies next to: rounded to fp32 it reaches h if |x| / d >= h - e, e half the distance of h from the fp32 number
+// below (a tie goes to h, the even one of the two).  |x| - h d is exact in fp32 (a multiple of half a unit of d, less than 2^18 of them) and so is d e.
 constexpr float BORDER = 4e-5f;
 static_assert(127.0f * 3.0f / 16777216.0f < BORDER, "the product's error");
+// the code of one value v >= 0
+__device__ __forceinline__ int code_of(float v, float d, float r) {
+    const float q = v * r, n = rintf(q), off = q - n;
+    if (fabsf(off) <= 0.5f - BORDER) return (int)n;
+    const float h = n + copysignf(0.5f, off), e = 0.5f * (h - __uint_as_float(__float_as_uint(h) - 1u));
+    return (int)h + (fmaf(-h, d, v) >= -(d * e));
+}
+// sixteen codes
 __device__ __forceinline__ uint4 codes_of(const float *v, float d, float r) {
     constexpr float MAGIC = 12582912.0f;
     const Pair rr = pair_of(r, r), up = pair_of(MAGIC, MAGIC), down = pair_of(-MAGIC, -MAGIC), minus = pair_of(-1.0f, -1.0f);
@@ -50,8 +59,8 @@ __device__ __forceinline__ uint4 codes_of(const float *v, float d, float r) {
     if (far > 0.5f - BORDER) {
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-            const float q = v[k] * r;
-            if (fabsf(q - rintf(q)) > 0.5f - BORDER) b[k] = (uint32_t)(int)fminf(fmaxf(roundf(__fdiv_rn(v[k], d)), -127.0f), 127.0f);
+            const int m = code_of(fabsf(v[k]), d, r);
+            b[k] = (uint32_t)(v[k] < 0.0f ? -m : m);
         }
     }
     uint32_t out[4];

@@ -8,14 +8,15 @@
 namespace cq {
 namespace i8 {
 
-// A row belongs to a team of threads, 32 to 512 of them, each with units of sixteen neighbouring k; a block has one team or several.
-constexpr int HELD = 4;   // units of a row that a thread keeps in registers until the row's scale is known
+// A row belongs to a team of threads, 32 to 512 of them, which take units of sixteen neighbouring k in turn; a block has one team or several.
+// What a thread has read (formed) stays in shared memory until the row's scale is known; of a row beyond that room the rest is formed again.
+constexpr int ROOM = 40 << 10;   // bytes of shared memory for that
 struct Rows {
     const int32_t *route_token;   // routed: the row of x that row r takes (null: r itself)
     const int32_t *offset;        // routed: first rows of the groups, on the device (null: rows are dense)
     int E;                        // groups, or matrices of `per` rows each
     int64_t per, rows, T;         // rows of one matrix; all rows; rows that x has
-    int team;                     // threads to a row
+    int team, held;               // threads to a row; units of a row that are kept, a multiple of `team`
 };
 struct Place { int64_t src, at; bool live, read; };   // row of x; row among the padded rows of the layout; whether it is one; whether x has it
 __device__ __forceinline__ void scan_if_routed(const Rows &q, int *s_off, int *s_blk) {
@@ -47,120 +48,183 @@ __device__ __forceinline__ uint32_t team_max(uint32_t v, int team, uint32_t *red
     v = __reduce_max_sync(~0u, v);
     if (team == 32) return v;
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int first = threadIdx.x / team * (team / 32), lane = threadIdx.x & 31;
-    return __reduce_max_sync(~0u, lane < team / 32 ? red[first + lane] : 0u);
+    const int mine = threadIdx.x / team, lane = threadIdx.x & 31;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(team) : "memory");
+    return __reduce_max_sync(~0u, lane < team / 32 ? red[mine * (team / 32) + lane] : 0u);
 }
-
 // ---------------------------------------------------------------- where sixteen values of a row come from
+// Units of a row in shared memory: 16-byte pieces of one unit `step` apart, so that a warp's accesses have no conflicts.
+struct Store {
+    uint4 *at;
+    int step;
+    __device__ __forceinline__ uint4 &piece(int slot, int k) const { return at[k * step + slot]; }
+};
 // rows of x as they are
 template <int DT>
 struct Plain {
-    static constexpr int WORDS = DT == DT_F32 ? 16 : 8;
+    static constexpr int PIECES = DT == DT_F32 ? 4 : 2, AHEAD = DT == DT_F32 ? 2 : 4;   // units whose loads are on their way together
     const void *x;
     int64_t ldx;
-    __device__ __forceinline__ uint32_t get(int64_t row, int64_t unit, bool read, uint32_t *w) const {
+    struct Raw { uint4 q[PIECES]; };
+    __device__ __forceinline__ Raw load(int64_t row, int64_t unit, bool read) const {
         const uint8_t *p = reinterpret_cast<const uint8_t *>(x) + (row * ldx + unit * 16) * (DT == DT_F32 ? 4 : 2);
+        Raw r;
 #pragma unroll
-        for (int k = 0; k < WORDS / 4; ++k) {
-            const uint4 q = read ? load16(p + 16 * k) : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < PIECES; ++k) r.q[k] = read ? load16(p + 16 * k) : make_uint4(0, 0, 0, 0);
+        return r;
+    }
+    // to a slot of the store; the largest magnitude.  The whole warp.
+    __device__ __forceinline__ void keep(const Raw &r, int64_t, int64_t, bool, const Store &s, int slot, uint32_t &largest) const {
+        uint32_t w[4 * PIECES], top = 0;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            s.piece(slot, k) = r.q[k];
+            w[4 * k] = r.q[k].x; w[4 * k + 1] = r.q[k].y; w[4 * k + 2] = r.q[k].z; w[4 * k + 3] = r.q[k].w;
+        }
+        if constexpr (DT != DT_F32) {
+            top = top_of_16bit<DT>(w);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4 * PIECES; ++k) top = max(top, w[k] & 0x7FFFFFFFu);
+        }
+        largest = max(largest, top);
+    }
+    __device__ __forceinline__ uint4 codes(const Store &s, int slot, float d, float r) const {
+        uint32_t w[4 * PIECES];
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            const uint4 q = s.piece(slot, k);
             w[4 * k] = q.x; w[4 * k + 1] = q.y; w[4 * k + 2] = q.z; w[4 * k + 3] = q.w;
         }
-        uint32_t top = 0;
-        if (DT == DT_F32) {
-#pragma unroll
-            for (int k = 0; k < WORDS; ++k) top = max(top, w[k] & 0x7FFFFFFFu);
+        if constexpr (DT != DT_F32) {
+            return codes_of_16bit<DT>(w, d, r);
         } else {
-            top = top_of_16bit<DT>(w);
-        }
-        return top;
-    }
-    __device__ __forceinline__ uint4 codes(const uint32_t *w, float d, float r) const {
-        if (DT != DT_F32) return codes_of_16bit<DT == DT_F32 ? DT_BF16 : DT>(w, d, r);
-        float v[16];
+            float v[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(w[k % WORDS]);
-        return codes_of(v, d, r);
+            for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(w[k]);
+            return codes_of(v, d, r);
+        }
     }
 };
-// silu(gate) * up of rows of h (gate | up), rounded to their type (cq_gated.cuh); what 32 bits leave open is formed in 64
+// silu(gate) * up of rows of h (gate | up), rounded to their type (cq_gated.cuh).  Values whose rounding 32 bits leave open are formed in 64, each
+// lane one of its own at a time: in binary16 three warps of four have one in every step, but few lanes.  (Kept with a bit that says so, and formed only
+// where the row's largest or a code hangs on them: one in fifty does, but telling them costs more than forming them, 126 us instead of 112.)
 template <int DT>
 struct Gated {
-    static constexpr int WORDS = 8;
+    static constexpr int AHEAD = 1, PIECES = 2;
     const uint16_t *h;
     int64_t ldh, I;
-    __device__ __forceinline__ uint32_t get(int64_t row, int64_t unit, bool read, uint32_t *act) const {
+    struct Raw { uint4 g[2], u[2]; };
+    __device__ __forceinline__ Raw load(int64_t row, int64_t unit, bool read) const {
         const uint16_t *pg = h + row * ldh + unit * 16, *pu = pg + I;
-        uint32_t gw[8] = {}, uw[8] = {};
-        if (read) {
+        Raw r;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint4 a = load16(pg + 8 * k), b = load16(pu + 8 * k);
-                gw[4 * k] = a.x; gw[4 * k + 1] = a.y; gw[4 * k + 2] = a.z; gw[4 * k + 3] = a.w;
-                uw[4 * k] = b.x; uw[4 * k + 1] = b.y; uw[4 * k + 2] = b.z; uw[4 * k + 3] = b.w;
-            }
+        for (int k = 0; k < 2; ++k) {
+            r.g[k] = read ? load16(pg + 8 * k) : make_uint4(0, 0, 0, 0);
+            r.u[k] = read ? load16(pu + 8 * k) : make_uint4(0, 0, 0, 0);
         }
-        uint32_t near = ~0u;
-        float small = 1.0f;
+        return r;
+    }
+    // value k of a unit in 64 bits
+    __device__ __forceinline__ void settle(int64_t row, int64_t unit, int k, const Store &s, int slot) const {
+        const uint16_t *pg = h + row * ldh + unit * 16 + k;
+        const uint32_t g = pg[0], u = pg[I];
+        const float y = gated_in_64_bits(value_of<DT>(&g, 0), value_of<DT>(&u, 0));
+        reinterpret_cast<uint16_t *>(&s.piece(slot, k >> 3))[k & 7] = (uint16_t)pack16<DT>(y, 0.0f);
+    }
+    __device__ __forceinline__ uint32_t top_of(const Store &s, int slot) const {
+        const uint4 a = s.piece(slot, 0), b = s.piece(slot, 1);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        return top_of_16bit<DT>(w);
+    }
+    __device__ __forceinline__ void keep(const Raw &r, int64_t row, int64_t unit, bool read, const Store &s, int slot, uint32_t &largest) const {
+        const uint32_t gw[8] = {r.g[0].x, r.g[0].y, r.g[0].z, r.g[0].w, r.g[1].x, r.g[1].y, r.g[1].z, r.g[1].w};
+        const uint32_t uw[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[1].x, r.u[1].y, r.u[1].z, r.u[1].w};
+        uint32_t act[8], low[8], near = ~0u, least = ~0u;
+        constexpr uint32_t LEAST = 0x0400u, ENDLESS = DT == DT_BF16 ? 0x7F80u : 0x7C00u, FAR = DT == DT_BF16 ? 0x4270u : 0x5380u;   // the least normal half, infinity, 60
 #pragma unroll
         for (int k = 0; k < 16; k += 2) {
             float y0, y1;
             gated_in_32_bits(value_of<DT>(gw, k), value_of<DT>(gw, k + 1), value_of<DT>(uw, k), value_of<DT>(uw, k + 1), y0, y1);
-            near = nearer<DT>(near, y0, y1);
+            low[k / 2] = dropped<DT>(y0, y1);
+            near = nearer<DT>(near, low[k / 2]);
             act[k / 2] = pack16<DT>(y0, y1);
-            if (DT == DT_F16) small = fminf(small, fminf(y0 == 0.0f ? 1.0f : fabsf(y0), y1 == 0.0f ? 1.0f : fabsf(y1)));   // subnormal halves have their borders elsewhere
+            if (DT == DT_F16) least = __viaddmin_u32(__float_as_uint(y0) & 0x7FFFFFFFu, ~0u, __viaddmin_u32(__float_as_uint(y1) & 0x7FFFFFFFu, ~0u, least));   // less one: 0 is exact, and becomes the largest
         }
-        constexpr uint32_t BAND_BITS = 2 * BAND * (DT == DT_BF16 ? 1 : 8);
-        const uint32_t largest = top_of_16bit<DT>(act);
-        const bool far = top_of_16bit<DT>(gw) > 0x42700000u || largest >= 0x7F800000u;   // 60; infinities and NaN
-        const bool open = read && ((near & 0xFFFFu) <= BAND_BITS || (near >> 16) <= BAND_BITS || far || (DT == DT_F16 && small < 6.103515625e-05f));
-        if (!__any_sync(~0u, open)) return largest;
-        settle_in_64_bits<DT>(open, gw, uw, act);
-        return top_of_16bit<DT>(act);
+        constexpr uint32_t WIDE = 2 * BAND * (DT == DT_BF16 ? 1 : 8);
+        uint32_t top = top_of_16bit<DT>(act);
+        // far gates, what is not finite, and subnormal halves, which have their borders elsewhere
+        const bool odd = read && (top_of_16bit<DT>(gw) > 0x42700000u || top >= 0x7F800000u || (DT == DT_F16 && least < 0x38800000u - 1));   // 2^-14
+        const bool open = read && ((near & 0xFFFFu) <= WIDE || (near >> 16) <= WIDE);
+        s.piece(slot, 0) = make_uint4(act[0], act[1], act[2], act[3]);
+        s.piece(slot, 1) = make_uint4(act[4], act[5], act[6], act[7]);
+        if (open || odd) {
+            uint32_t mask = 0;   // value 2 k at bit k, value 2 k + 1 at bit 16 + k
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {   // the top bit of a half is set where its distance is at most WIDE
+                const uint32_t far = __viaddmin_u16x2(low[k], ABOVE<DT> << 16 | ABOVE<DT>, (WIDE + 1) << 16 | (WIDE + 1));
+                mask |= (((0x7FFFu + WIDE + 1) << 16 | (0x7FFFu + WIDE + 1)) - far & 0x80008000u) >> (15 - k);
+            }
+            if (odd) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const uint32_t a = (k & 1 ? act[k / 2] >> 16 : act[k / 2]) & 0x7FFFu, g = (k & 1 ? gw[k / 2] >> 16 : gw[k / 2]) & 0x7FFFu;
+                    if (g > FAR || a >= ENDLESS || (DT == DT_F16 && a < LEAST)) mask |= 1u << (k / 2 + 16 * (k & 1));
+                }
+            }
+            for (; mask; mask &= mask - 1) {
+                const int b = __ffs(mask) - 1;
+                settle(row, unit, 2 * (b & 15) + (b >> 4), s, slot);
+            }
+            top = top_of(s, slot);
+        }
+        largest = max(largest, top);
     }
-    __device__ __forceinline__ uint4 codes(const uint32_t *w, float d, float r) const { return codes_of_16bit<DT>(w, d, r); }
+    __device__ __forceinline__ uint4 codes(const Store &s, int slot, float d, float r) const {
+        const uint4 a = s.piece(slot, 0), b = s.piece(slot, 1);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        return codes_of_16bit<DT>(w, d, r);
+    }
 };
 
 // ---------------------------------------------------------------- the quantisers
-template <class From, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) quantize_kernel(const From from, Rows q, int64_t K, int KT, float *scale, uint8_t *layout) {
-    extern __shared__ int s_tab[];
-    __shared__ uint32_t red[2][THREADS / 32];
+template <class From>
+__global__ void __launch_bounds__(512, 2) quantize_kernel(const From from, Rows q, int64_t K, int KT, float *scale, uint8_t *layout) {
+    extern __shared__ uint4 s_store[];
+    __shared__ uint32_t red[2][16];
     tc::wait_for_previous_kernel();
-    int *s_off = s_tab, *s_blk = s_tab + q.E + 1;
+    const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, mine = threadIdx.x / q.team, KU = (int)(K >> 4), units = KT * 8;
+    const int slots = q.held < KU ? q.held + q.team : q.held;   // a row that is longer has a slot for each thread besides
+    const Store s{s_store + mine * From::PIECES * slots, slots};
+    int *s_off = reinterpret_cast<int *>(s_store + teams * From::PIECES * slots), *s_blk = s_off + q.E + 1;
     scan_if_routed(q, s_off, s_blk);
-    const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, KU = (int)(K >> 4), units = KT * 8;
     int turn = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * teams; r0 < q.rows; r0 += (int64_t)gridDim.x * teams, turn ^= 1) {
-        const int64_t r = r0 + threadIdx.x / q.team;
+    for (int64_t r = (int64_t)blockIdx.x * teams + mine; r - mine < q.rows; r += (int64_t)gridDim.x * teams, turn ^= 1) {
         const Place p = place_of(q, r, s_off, s_blk);
-        uint32_t w[HELD][From::WORDS], top = 0;
+        uint32_t top = 0;
+        for (int u0 = in; u0 - in < KU; u0 += From::AHEAD * q.team) {   // whole warps
+            typename From::Raw raw[From::AHEAD];
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const int u = in + i * q.team;
-            if (i == 0 || i * q.team < KU) top = max(top, from.get(p.src, u, p.read && u < KU, w[i]));   // whole warps
-        }
-        for (int u = in + HELD * q.team; u - in < KU; u += q.team) {
-            uint32_t more[From::WORDS];
-            top = max(top, from.get(p.src, u, p.read && u < KU, more));
+            for (int i = 0; i < From::AHEAD; ++i) raw[i] = from.load(p.src, u0 + i * q.team, p.read && u0 + i * q.team < KU);
+#pragma unroll
+            for (int i = 0; i < From::AHEAD; ++i) {
+                const int u = u0 + i * q.team;
+                if (u - in >= KU) break;
+                from.keep(raw[i], p.src, u, p.read && u < KU, s, u < q.held ? u : q.held + in, top);
+            }
         }
         const float d = row_scale(team_max(top, q.team, red[turn])), inverse = __fdiv_rn(1.0f, d);
         if (p.live && in == 0) scale[r] = d;
         uint8_t *line = layout + (p.at >> 7) * KT * (int64_t)TILE_BYTES;
         const int rr = (int)(p.at & (ROWS - 1));
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const int u = in + i * q.team;
-            if (u < units && p.live) {
-                const uint4 c = u < KU ? from.codes(w[i], d, inverse) : make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(line + (int64_t)(u >> 3) * TILE_BYTES + piece_offset(rr, u & 7)) = c;
+#pragma unroll 1
+        for (int u = in; u - in < units; u += q.team) {
+            const int slot = u < q.held ? u : q.held + in;
+            if (u >= q.held && u - in < KU) {   // formed again
+                from.keep(from.load(p.src, u, p.read && u < KU), p.src, u, p.read && u < KU, s, slot, top);
             }
-        }
-        for (int u = in + HELD * q.team; u - in < units; u += q.team) {   // of a long row: formed again
-            uint32_t more[From::WORDS];
-            from.get(p.src, u, p.read && u < KU, more);
             if (u < units && p.live) {
-                const uint4 c = u < KU ? from.codes(more, d, inverse) : make_uint4(0, 0, 0, 0);
+                const uint4 c = u < KU ? from.codes(s, slot, d, inverse) : make_uint4(0, 0, 0, 0);
                 *reinterpret_cast<uint4 *>(line + (int64_t)(u >> 3) * TILE_BYTES + piece_offset(rr, u & 7)) = c;
             }
         }
@@ -168,14 +232,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) quantize_kern
 }
 
 // ---------------------------------------------------------------- back to values
-// code * scale, rounded once to the type asked for.  A thread takes eight values, so that a warp's stores are one run of memory.
+// code * scale, rounded once to the type asked for.  A thread reads sixteen codes; in 16 bits neighbouring threads exchange halves, so that each
+// of a warp's two stores fills whole sectors.
 template <int DT>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t *layout, Rows q, int64_t K, int KT, const float *scale, void *y) {
     extern __shared__ int s_tab[];
     tc::wait_for_previous_kernel();
     int *s_off = s_tab, *s_blk = s_tab + q.E + 1;
     scan_if_routed(q, s_off, s_blk);
-    const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, units = (int)(K >> 3);
+    const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, units = (int)(K >> 4), odd = threadIdx.x & 1;
     for (int64_t r = (int64_t)blockIdx.x * teams + threadIdx.x / q.team; r < q.rows; r += (int64_t)gridDim.x * teams) {
         const Place p = place_of(q, r, s_off, s_blk);
         if (!p.live) continue;
@@ -183,19 +248,30 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t *layout, 
         const uint8_t *line = layout + (p.at >> 7) * KT * (int64_t)TILE_BYTES;
         const int rr = (int)(p.at & (ROWS - 1));
 #pragma unroll 4
-        for (int u = in; u < units; u += q.team) {
-            const uint2 c = *reinterpret_cast<const uint2 *>(line + (int64_t)(u >> 4) * TILE_BYTES + piece_offset(rr, (u >> 1) & 7) + (u & 1) * 8);
-            float v[8];
+        for (int u = in; u - in < units; u += q.team) {   // whole warps
+            uint4 c = make_uint4(0, 0, 0, 0);
+            if (u < units) c = load16(line + (int64_t)(u >> 3) * TILE_BYTES + piece_offset(rr, u & 7));
+            uint32_t w[4] = {c.x, c.y, c.z, c.w};
+            if (DT != DT_F32) {   // the even thread has the first halves of both units then, the odd one the second halves
+                const uint32_t x = __shfl_xor_sync(~0u, odd ? c.x : c.z, 1), y = __shfl_xor_sync(~0u, odd ? c.y : c.w, 1);
+                w[0] = odd ? x : c.x; w[1] = odd ? y : c.y;
+                w[2] = odd ? c.z : x; w[3] = odd ? c.w : y;
+            }
+            float v[16];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = (float)(int8_t)((k < 4 ? c.x : c.y) >> (8 * (k & 3)) & 0xFFu) * s;
-            const int64_t at = r * K + (int64_t)u * 8;
+            for (int k = 0; k < 16; ++k) v[k] = (float)(int8_t)(w[k >> 2] >> (8 * (k & 3)) & 0xFFu) * s;
             if (DT == DT_F32) {
-                float4 *o = reinterpret_cast<float4 *>(reinterpret_cast<float *>(y) + at);
-                o[0] = make_float4(v[0], v[1], v[2], v[3]);
-                o[1] = make_float4(v[4], v[5], v[6], v[7]);
+                float4 *o = reinterpret_cast<float4 *>(reinterpret_cast<float *>(y) + r * K + (int64_t)u * 16);
+                if (u < units) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                }
             } else {
                 constexpr int D = DT == DT_F32 ? DT_BF16 : DT;
-                *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(y) + at) = make_uint4(pack16<D>(v[0], v[1]), pack16<D>(v[2], v[3]), pack16<D>(v[4], v[5]), pack16<D>(v[6], v[7]));
+                const int even = u & ~1;
+                uint4 *o = reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(y) + r * K + (int64_t)even * 16) + odd;
+                if (even < units) o[0] = make_uint4(pack16<D>(v[0], v[1]), pack16<D>(v[2], v[3]), pack16<D>(v[4], v[5]), pack16<D>(v[6], v[7]));
+                if (even + 1 < units) o[2] = make_uint4(pack16<D>(v[8], v[9]), pack16<D>(v[10], v[11]), pack16<D>(v[12], v[13]), pack16<D>(v[14], v[15]));
             }
         }
     }
@@ -217,27 +293,29 @@ __global__ void __launch_bounds__(256) exchange_kernel(uint8_t *codes, Rows q, i
 }
 
 // ---------------------------------------------------------------- launchers
-static Rows rows_of(const I8Rows &s, int team) { return Rows{s.route_token, s.offset, s.E, s.per, s.rows, s.T, team}; }
+static Rows rows_of(const I8Rows &s, int team, int held) { return Rows{s.route_token, s.offset, s.E, s.per, s.rows, s.T, team, held}; }
 static int kt_of(int64_t K) { return (int)((K + KB - 1) / KB); }
 static size_t table_bytes(const I8Rows &s) { return s.offset ? 2 * (size_t)(s.E + 1) * sizeof(int) : 0; }
 // Threads to a row: one unit each where there are few rows and latency counts, else four.
 static int team_of(int64_t rows, int units, int most) {
-    const int want = rows <= 2 * sm_count() ? units : (units + HELD - 1) / HELD;
+    const int want = rows <= 2 * sm_count() ? units : (units + 3) / 4;
     int team = 32;
     while (team < want && team < most) team *= 2;
     return team;
 }
+// per_sm: blocks of an SM at most, which take rows in turn (routed rows, whose tables each block fills first); 0: as many as there are rows for
 static unsigned grid_of(int64_t rows, int teams, int per_sm) {
-    const int64_t blocks = (rows + teams - 1) / teams, most = (int64_t)per_sm * sm_count();
+    const int64_t blocks = (rows + teams - 1) / teams, most = per_sm ? (int64_t)per_sm * sm_count() : blocks;
     return (unsigned)(blocks < most ? blocks : most);
 }
 template <class From>
 static cudaError_t quantize(const From &from, const I8Rows &s, int64_t K, float *scale, void *layout, cudaStream_t st) {
-    const int KT = kt_of(K), team = team_of(s.rows, KT * 8, s.rows <= 2 * sm_count() ? 512 : 256), threads = team < 256 ? 256 : team;
-    auto go = [&](auto kern) {
-        return launch_overlapped(kern, dim3(grid_of(s.rows, threads / team, 4)), (unsigned)threads, table_bytes(s), st, 1, true, from, rows_of(s, team), K, KT, scale, (uint8_t *)layout);
-    };
-    return threads == 256 ? go(quantize_kernel<From, 256>) : go(quantize_kernel<From, 512>);
+    const int KT = kt_of(K), KU = (int)(K >> 4), team = team_of(s.rows, KU, s.rows <= 2 * sm_count() ? 512 : 256), threads = team < 256 ? 256 : team, teams = threads / team;
+    const int all = (KU + team - 1) / team * team, room = ROOM / (teams * From::PIECES * 16) / team * team;
+    const int held = all <= room ? all : room - team;
+    const size_t smem = (size_t)teams * From::PIECES * 16 * (held < all ? held + team : held) + table_bytes(s);
+    return launch_overlapped(quantize_kernel<From>, dim3(grid_of(s.rows, teams, s.offset ? 2048 / threads : 0)), (unsigned)threads, smem, st, 1, true, from, rows_of(s, team, held), K, KT, scale,
+                             (uint8_t *)layout);
 }
 
 }  // namespace i8
@@ -254,17 +332,17 @@ cudaError_t launch_i8_swiglu_quantize(const void *h, int dtype, int64_t ldh, con
     return quantize(Gated<DT_F16>{(const uint16_t *)h, ldh, I}, s, I, scale, layout, st);
 }
 cudaError_t launch_i8_dequantize(const void *layout, const I8Rows &s, int64_t K, const float *scale, void *y, int dtype, cudaStream_t st) {
-    const int KT = kt_of(K), team = team_of(s.rows, (int)(K >> 3), 256);
+    const int KT = kt_of(K), team = team_of(s.rows, (int)(K >> 4), 256);
     auto go = [&](auto kern) {
-        return launch_overlapped(kern, dim3(grid_of(s.rows, 256 / team, 8)), 256u, table_bytes(s), st, 1, true, (const uint8_t *)layout, rows_of(s, team), K, KT, scale, y);
+        return launch_overlapped(kern, dim3(grid_of(s.rows, 256 / team, s.offset ? 8 : 0)), 256u, table_bytes(s), st, 1, true, (const uint8_t *)layout, rows_of(s, team, 0), K, KT, scale, y);
     };
     return dtype == DT_BF16 ? go(dequantize_kernel<DT_BF16>) : dtype == DT_F16 ? go(dequantize_kernel<DT_F16>) : go(dequantize_kernel<DT_F32>);
 }
 cudaError_t launch_i8_exchange(uint8_t *codes, const I8Rows &s, int64_t K, void *layout, bool in, cudaStream_t st) {
     const int KT = kt_of(K);
     const unsigned grid = grid_of((s.rows * KT * 8 + 255) / 256, 1, 8);
-    if (in) exchange_kernel<true><<<grid, 256, 0, st>>>(codes, rows_of(s, 32), K, KT, (uint8_t *)layout);
-    else exchange_kernel<false><<<grid, 256, 0, st>>>(codes, rows_of(s, 32), K, KT, (uint8_t *)layout);
+    if (in) exchange_kernel<true><<<grid, 256, 0, st>>>(codes, rows_of(s, 32, 0), K, KT, (uint8_t *)layout);
+    else exchange_kernel<false><<<grid, 256, 0, st>>>(codes, rows_of(s, 32, 0), K, KT, (uint8_t *)layout);
     return cudaGetLastError();
 }
 

@@ -2,6 +2,7 @@
 // sum of a token's routes.  What lies between them are the products of routed rows.
 #include <math_constants.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "cq_internal.h"
@@ -18,12 +19,13 @@ struct Args {
     int64_t ldl;
     const float *bias;               // for the choice alone, or null
     int T, E, groups, per, kept, best, top;   // per: experts of a group; best: choice scores that make its score
-    int lanes, each;                 // lanes to a group, experts to a lane
+    int lg_lanes, each;              // lanes to a group (log2), experts to a lane
     bool sigmoid, renormalise;
     float scale;
     int32_t *expert, *row, *token, *offset;
     float *weight;
-    int32_t *counts;                 // [blocks][E]: routes of each block's tokens
+    int32_t *counts;                 // [blocks][pitch]: routes of each block's tokens
+    int pitch;                       // E, to a multiple of four
     int per_block;                   // tokens of a block
 };
 
@@ -50,6 +52,14 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
     return v;
 }
+__device__ __forceinline__ int sum_up(int v) {   // of this lane and those in front
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(~0u, v, o);
+        if ((int)(threadIdx.x & 31) >= o) v += u;
+    }
+    return v;
+}
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
@@ -64,81 +74,57 @@ __device__ __forceinline__ float one_logit(const void *logits, int64_t at) {
     return v;
 }
 // NaN becomes -inf (not to be chosen), +inf the largest number, -0 becomes 0 (equal logits have equal bits)
-__device__ __forceinline__ float clean(float v) { return v > -CUDART_INF_F ? fminf(v, 3.402823466e38f) + 0.0f : -CUDART_INF_F; }
+__device__ __forceinline__ float clean(float v) { return fminf(fmaxf(v, -CUDART_INF_F), 3.402823466e38f) + 0.0f; }
 
-// A warp has a token, a lane `each` neighbouring experts of one group: group lane / lanes, from (lane % lanes) * each on.
+// A warp has a token, a lane `each` neighbouring experts of one group.
 struct Mine { int first, count; };   // expert, how many
 __device__ __forceinline__ Mine mine_of(const Args &p, int lane) {
-    const int g = lane / p.lanes, in = (lane - g * p.lanes) * p.each;
-    return {g * p.per + in, g < p.groups ? max(0, min(p.each, p.per - in)) : 0};
+    const int g = lane >> p.lg_lanes, in = (lane & ((1 << p.lg_lanes) - 1)) * p.each, count = g < p.groups ? max(0, min(p.each, p.per - in)) : 0;
+    return {count ? g * p.per + in : 0, count};
 }
 
-// Which groups stay: a lane's group by its score (-inf: it has no expert to choose); `open` where the least that stays and the best that does not
-// are closer than `margin`.
-template <class F>
-__device__ __forceinline__ bool group_stays(const Args &p, int lane, F total, F margin, bool &open) {
-    const int own = lane / p.lanes;
-    int ahead = 0;
-    for (int g = 0; g < p.groups; ++g) {
-        const F t = __shfl_sync(~0u, total, g * p.lanes);
-        ahead += t > total || (t == total && g < own);
-    }
-    const bool any = own < p.groups && total > -CUDART_INF_F, stays = any && ahead < p.kept;
-    F least = stays ? total : (F)CUDART_INF_F, most = any && !stays ? total : (F)-CUDART_INF_F;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        least = min(least, __shfl_xor_sync(~0u, least, o));
-        most = max(most, __shfl_xor_sync(~0u, most, o));
-    }
-    open = most > -CUDART_INF_F && !(least - most > margin);
-    return stays;
-}
 // the best two of a group, from those of its lanes
 template <class F>
-__device__ __forceinline__ F group_total(const Args &p, F first, F second) {
-    for (int o = 1; o < p.lanes; o <<= 1) {
+__device__ __forceinline__ void best_two_of_group(const Args &p, F &first, F &second) {
+    for (int o = 1; o < 1 << p.lg_lanes; o <<= 1) {
         const F a = __shfl_xor_sync(~0u, first, o), b = __shfl_xor_sync(~0u, second, o);
         second = max(min(first, a), max(second, b));
         first = max(first, a);
     }
-    return p.best == 2 && second > -CUDART_INF_F ? first + second : first;
 }
 
-// The choice in 64 bits, for rows that 32 bits leave open.  Lane j returns the j-th expert (-1: none).
+// What a warp puts its candidates into, in ascending order of experts, and the best of them in order.
+constexpr int CANDIDATES = 32;
+struct Candidates { uint32_t key[CANDIDATES], expert[CANDIDATES], best[CANDIDATES]; float logit[CANDIDATES]; double score[CANDIDATES]; };
+
+// Choice scores in 64 bits, -inf of what may not be chosen; top: the row's largest logit.  The whole warp.
 template <int V, int DT>
-__device__ __noinline__ int choose_in_64_bits(const Args &p, int64_t t) {
-    const int lane = threadIdx.x & 31;
-    const Mine m = mine_of(p, lane);
-    float l[V];
-    double c[V];
-    float top = -CUDART_INF_F;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        l[i] = i < m.count ? clean(one_logit<DT>(p.logits, t * p.ldl + m.first + i)) : -CUDART_INF_F;
-        top = fmaxf(top, l[i]);
-    }
-    top = unordered(__reduce_max_sync(~0u, ordered(top)));
+__device__ __forceinline__ void scores_in_64_bits(const Args &p, int64_t t, float top, float (&l)[V], double (&c)[V]) {
+    const Mine m = mine_of(p, threadIdx.x & 31);
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
+        l[i] = i < m.count ? clean(one_logit<DT>(p.logits, t * p.ldl + m.first + i)) : -CUDART_INF_F;
         c[i] = l[i] == -CUDART_INF_F ? 0.0 : p.sigmoid ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - (double)top);
         sum += c[i];
     }
     sum = warp_sum(sum);
-    double first = -CUDART_INF, second = -CUDART_INF;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         if (!p.sigmoid) c[i] /= sum;
         if (p.bias && i < m.count) c[i] += (double)p.bias[m.first + i];
         if (!(l[i] > -CUDART_INF_F && c[i] > -CUDART_INF)) c[i] = -CUDART_INF;
-        second = max(second, min(first, c[i]));
-        first = max(first, c[i]);
     }
-    bool stays = true;
-    if (p.groups > 1) {
-        bool open;
-        stays = group_stays<double>(p, lane, group_total<double>(p, first, second), 0.0, open);
-    }
+}
+// The choice in 64 bits among all experts of the groups that stay, for rows with more equals than there is room for.  Lane j returns the j-th
+// expert (-1: none).
+template <int V, int DT>
+__device__ __noinline__ int choose_in_64_bits(const Args &p, int64_t t, float top, bool stays) {
+    const int lane = threadIdx.x & 31;
+    const Mine m = mine_of(p, lane);
+    float l[V];
+    double c[V];
+    scores_in_64_bits<V, DT>(p, t, top, l, c);
     uint32_t left = 0;   // experts that may still be taken
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -164,42 +150,142 @@ __device__ __noinline__ int choose_in_64_bits(const Args &p, int64_t t) {
     }
     return chosen;
 }
+// The candidates' choice scores in 64 bits, s.score, and their logits, s.logit; top: the row's largest logit.  The whole warp, a candidate to a lane.
+template <int V, int DT>
+__device__ __forceinline__ void score_candidates(const Args &p, int64_t t, float top, int all, Candidates &s) {
+    const int lane = threadIdx.x & 31;
+    const float l = lane < all ? clean(one_logit<DT>(p.logits, t * p.ldl + s.expert[lane])) : 0.0f;
+    double c;
+    if (p.sigmoid) {
+        c = 1.0 / (1.0 + exp(-(double)l));
+    } else {
+        const Mine m = mine_of(p, lane);
+        double sum = 0.0;
+        for (int i = 0; i < m.count; ++i) {
+            const float v = clean(one_logit<DT>(p.logits, t * p.ldl + m.first + i));
+            if (v > -CUDART_INF_F) sum += exp((double)v - (double)top);
+        }
+        c = exp((double)l - (double)top) / warp_sum(sum);
+    }
+    if (lane < all) {
+        s.score[lane] = p.bias ? c + (double)p.bias[s.expert[lane]] : c;
+        s.logit[lane] = l;
+    }
+    __syncwarp();
+}
+// Their order in 64 bits, s.best, for rows whose choice among them 32 bits leave open.
+template <int V, int DT>
+__device__ __noinline__ void settle_in_64_bits(const Args &p, int64_t t, float top, int all, Candidates &s) {
+    const int lane = threadIdx.x & 31;
+    score_candidates<V, DT>(p, t, top, all, s);
+    const double c = lane < all ? s.score[lane] : 0.0;
+    const float l = lane < all ? s.logit[lane] : 0.0f;
+    int ahead = 0;
+    for (int j = 0; j < all; ++j) {
+        const double cj = s.score[j];
+        const float lj = s.logit[j];
+        ahead += cj > c || (cj == c && (lj > l || (lj == l && j < lane)));
+    }
+    if (lane < all) s.best[ahead] = lane;
+    __syncwarp();
+}
+// Whether a lane's group is among the `kept` best, from the totals of lanes g < groups in 64 bits.
+__device__ __forceinline__ bool own_group_stays(const Args &p, double total) {
+    const int lane = threadIdx.x & 31;
+    int ahead = 0;
+    for (int g = 0; g < p.groups; ++g) {
+        const double o = __shfl_sync(~0u, total, g);
+        ahead += o > total || (o == total && g < lane);
+    }
+    return __ballot_sync(~0u, lane < p.groups && total > -CUDART_INF && ahead < p.kept) >> (lane >> p.lg_lanes) & 1;
+}
+// The same for rows whose groups 32 bits leave open: the candidates hold all that may be among the best two of a group.
+template <int V, int DT>
+__device__ __noinline__ bool group_stays_by_candidates(const Args &p, int64_t t, float top, int all, Candidates &s) {
+    const int lane = threadIdx.x & 31;
+    score_candidates<V, DT>(p, t, top, all, s);
+    double first = -CUDART_INF, second = -CUDART_INF;
+    for (int j = 0; j < all; ++j)
+        if ((int)s.expert[j] / p.per == lane) {
+            second = max(second, min(first, s.score[j]));
+            first = max(first, s.score[j]);
+        }
+    __syncwarp();
+    return own_group_stays(p, p.best == 2 && second > -CUDART_INF ? first + second : first);
+}
+// Or all of them, where there are too many.
+template <int V, int DT>
+__device__ __noinline__ bool group_stays_in_64_bits(const Args &p, int64_t t, float top) {
+    float l[V];
+    double c[V], first = -CUDART_INF, second = -CUDART_INF;
+    scores_in_64_bits<V, DT>(p, t, top, l, c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        second = max(second, min(first, c[i]));
+        first = max(first, c[i]);
+    }
+    best_two_of_group<double>(p, first, second);
+    const double total = p.best == 2 && second > -CUDART_INF ? first + second : first;
+    return own_group_stays(p, __shfl_sync(~0u, total, ((threadIdx.x & 31) << p.lg_lanes) & 31));
+}
+
+__device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float reciprocal_approx(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 // The choice of one token by one warp: lane j returns the j-th expert (-1: none) and its weight.
 //
 // Without a bias experts are in the order of their logits, which is exact.  Else choice scores are formed in 32 bits; where two that
-// follow one another among the best `top` + 1 are closer than both may be off, the row is decided in 64 bits.  How far off, in 2^-24:
-// a sigmoid, of itself: expf 4, the sum 1, the division 1.  A softmax: l - max rounds by z = max - l of e^-z, at most 0.37 of the whole, expf
-// 4, the sum of E terms V + 5 <= 37 and the mean of their z <= ln E = 6.2 and expf's 4, the division 1: 53.  The bias adds |c| / 2.
+// follow one another among the best `top` + 1 are closer than both may be off, the row is decided in 64 bits.  How far off, in u = 2^-24, with
+// ex2.approx 4, rcp.approx 2 and log2(e) and its product 2 of the exponent: a sigmoid, s = 1 / (1 + e): of s (1 - s) 2 |l| + 4, which is 1.5 at most,
+// and 3 for the sum and the reciprocal: 4.5.  A softmax, z = max - l: 3 z of e^-z, 1.1 at most, and, of itself, 4, the sum of E terms V + 5 <= 37
+// with 3 times the mean of z <= ln E = 6.2 and 4, the reciprocal and the product 3: 68.  The bias adds |c| / 2 to each.
+//
+// The best: the (top + 1)-th largest of the lanes' largest is not above the (top + 1)-th largest of all, so what reaches it are candidates; hardly
+// more than that many, since few lanes have two.  Each finds its place by counting those in front of it.  Many equals, or a large
+// `top`, leave more candidates than there is room for: then the largest is taken out time and again.  8192 tokens to 8 of 256: 36 us with the latter alone.
+// The logits of one lane as they are stored.  WIDE: `each` is V, and the rows allow wide loads.
 template <int V, int DT, bool WIDE>
-__device__ __forceinline__ int choose(const Args &p, int64_t t, const float *bias, float &weight) {
-    const int lane = threadIdx.x & 31;
-    const Mine m = mine_of(p, lane);
-    float l[V];
-    if (WIDE) {   // `each` is V, and the rows allow it
-        constexpr int BYTES = V * (DT == DT_F32 ? 4 : 2), WORDS = BYTES / 4;
-        uint32_t w[WORDS];
+struct Raw {
+    static constexpr int BYTES = V * (DT == DT_F32 ? 4 : 2), WORDS = WIDE ? BYTES / 4 : V;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const Args &p, int64_t t, const Mine &m) {
         const uint8_t *src = reinterpret_cast<const uint8_t *>(p.logits) + (t * p.ldl + m.first) * (DT == DT_F32 ? 4 : 2);
-        if (m.count) {
-            if (BYTES >= 16) {
+        constexpr uint32_t NONE = DT == DT_F32 ? 0xFF800000u : DT == DT_BF16 ? 0xFF80FF80u : 0xFC00FC00u;   // -inf
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = NONE;
+        if constexpr (WIDE) {
+            if (!m.count) return;
+            if constexpr (BYTES >= 16) {
 #pragma unroll
                 for (int i = 0; i < WORDS; i += 4) {
                     const uint4 q = load16(src + 4 * i);
-                    w[i] = q.x; w[(i + 1) % WORDS] = q.y; w[(i + 2) % WORDS] = q.z; w[(i + 3) % WORDS] = q.w;
+                    w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
                 }
-            } else if (BYTES == 8) {
+            } else if constexpr (BYTES == 8) {
                 const uint2 q = *reinterpret_cast<const uint2 *>(src);
-                w[0] = q.x; w[1 % WORDS] = q.y;
+                w[0] = q.x; w[1] = q.y;
             } else {
                 w[0] = *reinterpret_cast<const uint32_t *>(src);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < m.count) w[i] = DT == DT_F32 ? reinterpret_cast<const uint32_t *>(src)[i] : (uint32_t)reinterpret_cast<const uint16_t *>(src)[i];
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) l[i] = m.count ? clean(DT == DT_F32 ? __uint_as_float(w[i % WORDS]) : value_of<DT == DT_F32 ? DT_BF16 : DT>(w, DT == DT_F32 ? 0 : i)) : -CUDART_INF_F;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) l[i] = i < m.count ? clean(one_logit<DT>(p.logits, t * p.ldl + m.first + i)) : -CUDART_INF_F;
     }
+    __device__ __forceinline__ float logit(int i) const {
+        if constexpr (DT == DT_F32) return clean(__uint_as_float(w[i]));
+        else return clean(WIDE ? value_of<DT>(w, i) : value_of<DT>(&w[i % WORDS], 0));
+    }
+};
+
+template <int V, int DT, bool WIDE>
+__device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT, WIDE> &raw, const Mine &m, const float *bias, Candidates &s, float &weight) {
+    const int lane = threadIdx.x & 31;
+    constexpr float U = 5.9604645e-8f, LOG2E = 1.44269504f;
+    float l[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) l[i] = raw.logit(i);
     float top = l[0];
 #pragma unroll
     for (int i = 1; i < V; ++i) top = fmaxf(top, l[i]);
@@ -207,79 +293,161 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const float *bia
     weight = 0.0f;
     if (top == -CUDART_INF_F) return -1;
 
-    const bool scores = p.bias || p.groups > 1, whole = !p.sigmoid && (scores || !p.renormalise);
-    float sum = 1.0f;
+    const bool scores = bias || p.groups > 1;
+    float sum = 1.0f, rest = 0.0f;   // rest: how far two choice scores may be off, but for the part that grows with them
     uint32_t key[V];
-    bool stays = true, open = false;
-    float rest = 0.0f;   // how far two choice scores may be off, but for the part that grows with them
-    if (scores || whole) {
-        float s[V];
+    bool stays = true;
+    if (scores || (!p.sigmoid && !p.renormalise)) {
+        float c[V];
         if (p.sigmoid) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[i] = __fdiv_rn(1.0f, 1.0f + expf(-l[i]));
-            rest = 16.0f * 5.9604645e-8f;
+            for (int i = 0; i < V; ++i) c[i] = reciprocal_approx(1.0f + exp2_approx(-LOG2E * l[i]));
+            rest = 16.0f * U;
         } else {
             sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) { s[i] = expf(l[i] - top); sum += s[i]; }
+            for (int i = 0; i < V; ++i) { c[i] = exp2_approx(LOG2E * (l[i] - top)); sum += c[i]; }
             sum = warp_sum(sum);
+            const float part = reciprocal_approx(sum);
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[i] = __fdiv_rn(s[i], sum);
-            rest = 128.0f * 5.9604645e-8f;
+            for (int i = 0; i < V; ++i) c[i] *= part;
+            rest = 160.0f * U;
         }
         if (scores) {
             float first = -CUDART_INF_F, second = -CUDART_INF_F;
+            if (bias) {   // has V values behind the last
+                const float *mine = bias + m.first;
+                if constexpr (WIDE && V % 4 == 0) {
+#pragma unroll
+                    for (int i = 0; i < V; i += 4) {
+                        const float4 b = *reinterpret_cast<const float4 *>(mine + i);
+                        c[i] += b.x; c[i + 1] += b.y; c[i + 2] += b.z; c[i + 3] += b.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) c[i] += mine[i];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                if (bias && i < m.count) s[i] += bias[m.first + i];
-                if (!(l[i] > -CUDART_INF_F && s[i] > -CUDART_INF_F)) s[i] = -CUDART_INF_F;
-                second = fmaxf(second, fminf(first, s[i]));
-                first = fmaxf(first, s[i]);
+                c[i] = l[i] > -CUDART_INF_F ? c[i] : -CUDART_INF_F;
+                second = fmaxf(second, fminf(first, c[i]));
+                first = fmaxf(first, c[i]);
             }
             if (p.groups > 1) {
-                const float total = group_total<float>(p, first, second);
-                // each of four choice scores is off by |c| / 2 more, their sums by as much again: 8 |c| in units of 2^-24
                 const float a = fabsf(first), b = fabsf(second);
-                const float large = unordered(__reduce_max_sync(~0u, ordered(fmaxf(a < CUDART_INF_F ? a : 0.0f, b < CUDART_INF_F ? b : 0.0f))));
-                stays = group_stays<float>(p, lane, total, 2.0f * rest + 4.7683716e-7f * large, open);
+                const float large = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(fmaxf(a < CUDART_INF_F ? a : 0.0f, b < CUDART_INF_F ? b : 0.0f))));
+                best_two_of_group<float>(p, first, second);
+                const float total = p.best == 2 && second > -CUDART_INF_F ? first + second : first;
+                uint32_t left = lane < p.groups << p.lg_lanes && total > -CUDART_INF_F ? ordered(total) : 0u, least = 0;
+                stays = false;
+                for (int g = 0; g < p.kept; ++g) {   // the best of those that are left; of equals the first
+                    const uint32_t k = __reduce_max_sync(~0u, left);
+                    if (k == 0) break;
+                    least = k;
+                    const int from = __ffs(__ballot_sync(~0u, left == k)) - 1;
+                    if ((uint32_t)(lane - from) < 1u << p.lg_lanes) { stays = true; left = 0; }
+                }
+                // Each of four choice scores is off by |c| / 2 more, their sums by as much again: 8 |c|.  What stays has to be that far above what does not.
+                const uint32_t most = __reduce_max_sync(~0u, left);
+                if (most != 0 && !(unordered(least) - unordered(most) > 2.0f * rest + 8.0f * U * large)) {
+                    const float near = (p.best == 2 && second > -CUDART_INF_F ? second : first) - rest - 4.0f * U * large;
+                    int count = 0;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) count += c[i] > -CUDART_INF_F && c[i] >= near;
+                    int at = sum_up(count);
+                    const int all = __shfl_sync(~0u, at, 31);
+                    if (all <= CANDIDATES) {
+                        at -= count;
+#pragma unroll
+                        for (int i = 0; i < V; ++i) if (c[i] > -CUDART_INF_F && c[i] >= near) s.expert[at++] = m.first + i;
+                        __syncwarp();
+                        stays = group_stays_by_candidates<V, DT>(p, t, top, all, s);
+                    } else {
+                        stays = group_stays_in_64_bits<V, DT>(p, t, top);
+                    }
+                }
             }
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = stays && (!scores || s[i] > -CUDART_INF_F) ? ordered(bias ? s[i] + 0.0f : l[i]) : 0u;
+        for (int i = 0; i < V; ++i) key[i] = stays && c[i] > -CUDART_INF_F && l[i] > -CUDART_INF_F ? ordered(bias ? c[i] + 0.0f : l[i]) : 0u;
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = ordered(l[i]);
+        for (int i = 0; i < V; ++i) key[i] = l[i] > -CUDART_INF_F ? ordered(l[i]) : 0u;
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i) if (l[i] == -CUDART_INF_F) key[i] = 0u;
 
-    int chosen = -1;
+    const int rounds = bias ? min(p.top + 1, 32) : p.top;   // one more, to see how far it is from the last
+    int chosen = -1, count = 0;
     uint32_t got = 0, best = 0;   // lane j: the key of the j-th; the best key that this lane still has
     float logit = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) best = max(best, key[i]);
-    const int rounds = p.bias ? min(p.top + 1, 32) : p.top;   // one more, to see how far it is from the last
-    for (int j = 0; j < rounds; ++j) {
-        const uint32_t k = __reduce_max_sync(~0u, best);
-        if (k == 0) break;
-        const int from = __ffs(__ballot_sync(~0u, best == k)) - 1;
-        int at = 0;
-        float lv = 0.0f;
+    uint32_t limit = 0;
+    {
+        uint32_t left = best;
+#pragma unroll 4
+        for (int j = 0; j < rounds; ++j) {
+            limit = __reduce_max_sync(~0u, left);
+            if (left == limit) left = 0;
+        }
+        limit = max(limit, 1u);   // fewer lanes than that have any
+        if (bias && limit > 1u) {   // and what may belong in front of the last
+            const float least = unordered(limit);
+            limit = max(ordered(least - 2.0f * rest - 8.0f * U * fabsf(least)), 1u);
+        }
+    }
 #pragma unroll
-        for (int i = V - 1; i >= 0; --i) if (key[i] == k) { at = i; lv = l[i]; }
-        const int e = __shfl_sync(~0u, m.first + at, from);
-        lv = __shfl_sync(~0u, lv, from);
-        if (lane == j) { chosen = e; got = k; logit = lv; }
-        if (lane == from) {
-            best = 0;
+    for (int i = 0; i < V; ++i) count += key[i] >= limit;
+    int at = sum_up(count);
+    const int all = __shfl_sync(~0u, at, 31);
+    if (all <= CANDIDATES) {
+        at -= count;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (i == at) key[i] = 0;
-                best = max(best, key[i]);
+        for (int i = 0; i < V; ++i)
+            if (key[i] >= limit) {
+                s.key[at] = key[i];
+                s.expert[at] = m.first + i;
+                ++at;
+            }
+        if (lane < 3 && all + lane < CANDIDATES) s.key[all + lane] = 0;
+        __syncwarp();
+        const uint32_t mine = lane < all ? s.key[lane] : 0u;
+        int ahead = __popc(__match_any_sync(~0u, mine) & ((1u << lane) - 1u));   // of equals those in front: lower experts
+        for (int j = 0; j < all; j += 4) {   // what lies behind the last is not larger
+            const uint4 k = *reinterpret_cast<const uint4 *>(&s.key[j]);
+            ahead += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
+        }
+        if (lane < all) s.best[ahead] = lane;
+        __syncwarp();
+        if (lane < min(all, rounds)) {
+            const uint32_t from = s.best[lane];
+            chosen = s.expert[from]; got = s.key[from];
+            logit = bias ? clean(one_logit<DT>(p.logits, t * p.ldl + chosen)) : unordered(got);
+        }
+    } else {
+        for (int j = 0; j < rounds; ++j) {
+            const uint32_t k = __reduce_max_sync(~0u, best);
+            if (k == 0) break;
+            const int from = __ffs(__ballot_sync(~0u, best == k)) - 1;
+            int which = 0;
+            float lv = 0.0f;
+#pragma unroll
+            for (int i = V - 1; i >= 0; --i) if (key[i] == k) { which = i; lv = l[i]; }
+            const int e = __shfl_sync(~0u, m.first + which, from);
+            lv = __shfl_sync(~0u, lv, from);
+            if (lane == j) { chosen = e; got = k; logit = lv; }
+            if (lane == from) {
+                best = 0;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if (i == which) key[i] = 0;
+                    best = max(best, key[i]);
+                }
             }
         }
     }
-    if (p.bias) {
+    bool open = false;
+    if (bias) {
         // equal logits with equal biases are equal, and the lower index is first
         const int next = __shfl_down_sync(~0u, chosen, 1);
         const uint32_t after = __shfl_down_sync(~0u, got, 1);
@@ -287,15 +455,20 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const float *bia
         if (lane + 1 < rounds && chosen >= 0 && next >= 0) {
             const float a = unordered(got), b = unordered(after);
             const bool equal = logit == l1 && bias[chosen] == bias[next];
-            open |= !equal && !(a - b > rest + 2.3841858e-7f * fmaxf(fabsf(a), fabsf(b)));
+            open |= !equal && !(a - b > rest + 4.0f * U * fmaxf(fabsf(a), fabsf(b)));
         }
-        // all of 32 were wanted: what follows the last is in nobody's hands
-        if (rounds == p.top) open |= __reduce_max_sync(~0u, best) != 0;
+        if (rounds == p.top) open |= all > p.top;   // of 32 wanted ones the last has nobody behind it to be compared with
     }
     if (__any_sync(~0u, open)) {
-        chosen = choose_in_64_bits<V, DT>(p, t);
-        if (chosen >= 0) logit = clean(one_logit<DT>(p.logits, t * p.ldl + chosen));
+        if (all <= CANDIDATES) {
+            settle_in_64_bits<V, DT>(p, t, top, all, s);
+            if (lane < min(all, p.top)) { chosen = s.expert[s.best[lane]]; logit = s.logit[s.best[lane]]; }
+        } else {
+            chosen = choose_in_64_bits<V, DT>(p, t, top, stays);
+            if (chosen >= 0) logit = clean(one_logit<DT>(p.logits, t * p.ldl + chosen));
+        }
     }
+    __syncwarp();   // the candidates may be replaced
     const bool there = lane < p.top && chosen >= 0;
     if (!there) chosen = -1;
     // weights: over the sum of the chosen they do not depend on a common factor, so the largest logit is taken out where scores would vanish
@@ -304,14 +477,14 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const float *bia
         float w = 0.0f;
         if (p.sigmoid) {
             large = fminf(large, 0.0f);
-            if (there) w = logit < 0.0f ? __fdiv_rn(expf(logit - large), 1.0f + expf(logit)) : __fdiv_rn(expf(-large), 1.0f + expf(-logit));
+            if (there) w = __fdividef(logit < 0.0f ? expf(logit - large) : 1.0f, 1.0f + expf(-fabsf(logit)));   // large is 0 where a logit is not negative
         } else if (there) {
             w = expf(logit - large);
         }
         const float all = warp_sum(w);
-        if (there) weight = __fdiv_rn(w, all) * p.scale;
+        if (there) weight = __fdividef(w, all) * p.scale;
     } else if (there) {
-        weight = (p.sigmoid ? __fdiv_rn(1.0f, 1.0f + expf(-logit)) : __fdiv_rn(expf(logit - top), sum)) * p.scale;
+        weight = (p.sigmoid ? __fdividef(logit < 0.0f ? expf(logit) : 1.0f, 1.0f + expf(-fabsf(logit))) : __fdividef(expf(logit - top), sum)) * p.scale;
     }
     return chosen;
 }
@@ -321,48 +494,49 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const float *bia
 // tells a route's place among those of its expert: the routes of tokens in front, in this chunk by counting bits, before it by a running
 // count.  Nothing depends on the order in which warps come.  The places among all blocks' routes are added by place_kernel, or, where one block has
 // all tokens, at once.
-constexpr int CHUNK = 64, THREADS = 512;
-static_assert(CHUNK % 32 == 0, "words of bits");
+constexpr int CHUNK = 128, PLACED = 2;   // PLACED: blocks of tokens whose routes one block of place_kernel places
+constexpr int threads_for(int V) { return V <= 4 ? 1024 : V == 8 ? 768 : 512; }   // at least as many as there are experts
+static_assert(CHUNK % 32 == 0 && MAX_EXPERTS <= 512, "words of bits; a thread for each expert");
 
-// first route of each expert (E + 1 values), from their counts; the first warp of the block, all of it
-__device__ __forceinline__ void scan_counts(const int *counts, int E, int *first) {
-    const int lane = threadIdx.x & 31;
-    int before = 0;
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int n = e0 + lane < E ? counts[e0 + lane] : 0;
-        int s = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(~0u, s, o);
-            if (lane >= o) s += u;
-        }
-        if (e0 + lane < E) first[e0 + lane] = before + s - n;
-        before += __shfl_sync(~0u, s, 31);
-    }
-    if (lane == 0) first[E] = before;
+// Thread e's `count` routes: how many the experts in front have.  The whole block, at least E threads of it; all: of all experts; `sums`: 16 words of shared memory.
+__device__ __forceinline__ int in_front(int count, int E, int *sums, int &all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (E + 31) >> 5;
+    const int s = sum_up(count);
+    if (lane == 31 && warp < warps) sums[warp] = s;
+    __syncthreads();
+    const int of = lane < warps ? sums[lane] : 0;
+    all = __reduce_add_sync(~0u, of);
+    return s - count + __reduce_add_sync(~0u, lane < warp ? of : 0);
 }
+static_assert(MAX_EXPERTS <= 16 * 32, "sums of the warps");
 
 template <int V, int DT, bool WIDE>
-__global__ void __launch_bounds__(THREADS) route_kernel(const Args p) {
-    extern __shared__ int s_mem[];
-    constexpr int W = CHUNK / 32;
-    uint32_t *s_bits = reinterpret_cast<uint32_t *>(s_mem);          // [E][W]
-    int *s_run = s_mem + p.E * W, *s_first = s_run + p.E;            // [E], [E + 1]
-    float *s_bias = reinterpret_cast<float *>(s_first + p.E + 1);    // [E]
-    int16_t *s_chosen = reinterpret_cast<int16_t *>(s_bias + p.E);   // [CHUNK][top]
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = THREADS / 32;
+__global__ void __launch_bounds__(threads_for(V)) route_kernel(const Args p) {
+    extern __shared__ __align__(16) int s_mem[];
+    __shared__ int s_sums[16];
+    constexpr int W = CHUNK / 32, THREADS = threads_for(V), WARPS = THREADS / 32;
+    Candidates *s_candidates = reinterpret_cast<Candidates *>(s_mem);   // [WARPS]
+    uint32_t *s_bits = reinterpret_cast<uint32_t *>(s_candidates + WARPS);   // [E][W]
+    float *s_bias = reinterpret_cast<float *>(s_bits + p.E * W);     // [E + V], 16-byte aligned
+    int *s_run = reinterpret_cast<int *>(s_bias + p.E + V);          // [E]
+    int16_t *s_chosen = reinterpret_cast<int16_t *>(s_run + p.E);    // [CHUNK][top]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int from = blockIdx.x * p.per_block, to = min(p.T, from + p.per_block);
+    const Mine m = mine_of(p, lane);
     for (int i = threadIdx.x; i < p.E * W; i += THREADS) s_bits[i] = 0;
     for (int i = threadIdx.x; i < p.E; i += THREADS) s_run[i] = 0;
     tc::wait_for_previous_kernel();
-    if (p.bias) for (int i = threadIdx.x; i < p.E; i += THREADS) s_bias[i] = p.bias[i];
+    if (p.bias)
+        for (int i = threadIdx.x; i < p.E; i += THREADS) s_bias[i] = fmaxf(p.bias[i], -CUDART_INF_F);   // NaN excludes as -inf does
     __syncthreads();
     for (int t0 = from; t0 < to; t0 += CHUNK) {
         const int n = min(CHUNK, to - t0);
-        for (int i = warp; i < n; i += warps) {
-            const int64_t t = t0 + i;
+        for (int i = warp; i < n; i += WARPS) {
+            const int t = t0 + i;
+            Raw<V, DT, WIDE> raw;
+            raw.load(p, t, m);
             float weight;
-            const int e = choose<V, DT, WIDE>(p, t, p.bias ? s_bias : nullptr, weight);
+            const int e = choose<V, DT, WIDE>(p, t, raw, m, p.bias ? s_bias : nullptr, s_candidates[warp], weight);
             if (lane < p.top) {
                 p.expert[t * p.top + lane] = e;
                 p.weight[t * p.top + lane] = weight;
@@ -371,77 +545,92 @@ __global__ void __launch_bounds__(THREADS) route_kernel(const Args p) {
             }
         }
         __syncthreads();
+        // where one block has all tokens, s_run becomes the first routes of the experts
+        const int own = threadIdx.x;
+        int mine = 0, last = 0;
+        if (own < p.E) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) mine += __popc(s_bits[own * W + w]);
+        }
+        if (gridDim.x == 1) {
+            const int first = in_front(mine, p.E, s_sums, last);
+            if (own < p.E) p.offset[own] = s_run[own] = first;
+            if (own == 0) p.offset[p.E] = last;
+            __syncthreads();
+        }
         for (int i = threadIdx.x; i < n * p.top; i += THREADS) {
             const int tl = i / p.top, e = s_chosen[i];
             int at = -1;
             if (e >= 0) {
                 at = s_run[e] + __popc(s_bits[e * W + (tl >> 5)] & ((1u << (tl & 31)) - 1u));
-                for (int w = 0; w < tl >> 5; ++w) at += __popc(s_bits[e * W + w]);
-            }
-            p.row[(int64_t)t0 * p.top + i] = at;   // among this block's routes of the expert
-        }
-        __syncthreads();
-        for (int e = threadIdx.x; e < p.E; e += THREADS) {
-            int c = 0;
 #pragma unroll
-            for (int w = 0; w < W; ++w) { c += __popc(s_bits[e * W + w]); s_bits[e * W + w] = 0; }
-            s_run[e] += c;
+                for (int w = 0; w + 1 < W; ++w) at += w < tl >> 5 ? __popc(s_bits[e * W + w]) : 0;
+                if (gridDim.x == 1) p.token[at] = t0 + tl;
+            }
+            p.row[t0 * p.top + i] = at;   // among this block's routes of the expert, or among all
+            if (gridDim.x == 1 && i >= last) p.token[i] = -1;
+        }
+        if (gridDim.x == 1) return;
+        __syncthreads();
+        if (own < p.E) {
+            s_run[own] += mine;
+#pragma unroll
+            for (int w = 0; w < W; ++w) s_bits[own * W + w] = 0;
         }
         __syncthreads();
     }
-    if (gridDim.x > 1) {
-        for (int e = threadIdx.x; e < p.E; e += THREADS) p.counts[(int64_t)blockIdx.x * p.E + e] = s_run[e];
-        return;
+    for (int e = threadIdx.x; e < p.E; e += THREADS) p.counts[(int64_t)blockIdx.x * p.pitch + e] = s_run[e];
+}
+
+// The places of PLACED blocks' routes among all: those of experts in front, of the expert's in blocks in front, of the expert's in this block.
+constexpr int SLICES = 16;
+__global__ void __launch_bounds__(1024) place_kernel(const Args p, int blocks) {
+    extern __shared__ __align__(16) int s_mem[];
+    __shared__ int s_sums[16];
+    // four experts to a thread, the blocks shared among `slices` of them
+    const int quads = p.pitch / 4, slices = min(SLICES, 1024 / quads), quad = threadIdx.x % quads, slice = threadIdx.x / quads;
+    int *s_all = s_mem, *s_before = s_all + slices * p.pitch, *s_base = s_before + slices * p.pitch;   // [slices][pitch] twice, [PLACED][pitch]
+    tc::wait_for_previous_kernel();
+    const int b0 = blockIdx.x * PLACED, own = min(PLACED, blocks - b0);
+    const int of_block = p.per_block * p.top, from = b0 * of_block, to = min(p.T * p.top, from + own * of_block);   // routes: 2^30 at most, and blocks of 148 or more parts of them
+    int i = from + threadIdx.x;
+    int e = i < to ? p.expert[i] : -1, in = i < to ? p.row[i] : 0;   // on their way while the counts are added
+    int mine[PLACED];
+#pragma unroll
+    for (int g = 0; g < PLACED; ++g) mine[g] = g + 1 < own && (int)threadIdx.x < p.E ? p.counts[(int64_t)(b0 + g) * p.pitch + threadIdx.x] : 0;
+    if (slice < slices) {
+        int4 all = make_int4(0, 0, 0, 0), before = all;
+#pragma unroll 10
+        for (int b = slice; b < blocks; b += slices) {
+            const int4 c = *reinterpret_cast<const int4 *>(p.counts + (int64_t)b * p.pitch + quad * 4);
+            all.x += c.x; all.y += c.y; all.z += c.z; all.w += c.w;
+            if (b < b0) { before.x += c.x; before.y += c.y; before.z += c.z; before.w += c.w; }
+        }
+        *reinterpret_cast<int4 *>(s_all + slice * p.pitch + quad * 4) = all;
+        *reinterpret_cast<int4 *>(s_before + slice * p.pitch + quad * 4) = before;
     }
-    if (warp == 0) scan_counts(s_run, p.E, s_first);
     __syncthreads();
-    for (int e = threadIdx.x; e <= p.E; e += THREADS) p.offset[e] = s_first[e];
-    const int R = p.T * p.top, last = s_first[p.E];
-    for (int i = threadIdx.x; i < R; i += THREADS) {
-        const int e = p.expert[i];   // of this block's own writes
+    int all = 0, base = 0, last;
+    if ((int)threadIdx.x < p.E)
+        for (int k = 0; k < slices; ++k) { all += s_all[k * p.pitch + threadIdx.x]; base += s_before[k * p.pitch + threadIdx.x]; }
+    const int first = in_front(all, p.E, s_sums, last);
+    base += first;
+    if ((int)threadIdx.x < p.E) {
+        if (blockIdx.x == 0) p.offset[threadIdx.x] = first;
+#pragma unroll
+        for (int g = 0; g < PLACED; ++g) { s_base[g * p.pitch + threadIdx.x] = base; base += mine[g]; }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.offset[p.E] = last;
+    __syncthreads();
+    while (i < to) {
         if (e >= 0) {
-            const int at = s_first[e] + p.row[i];
+            const int at = s_base[(PLACED == 2 ? i - from >= of_block : (i - from) / of_block) * p.pitch + e] + in;
             p.row[i] = at;
             p.token[at] = i / p.top;
         }
         if (i >= last) p.token[i] = -1;
-    }
-}
-
-__global__ void __launch_bounds__(THREADS) place_kernel(const Args p) {
-    extern __shared__ int s_mem[];
-    int *s_all = s_mem, *s_before = s_all + p.E, *s_first = s_before + p.E;   // [E], [E], [E + 1]
-    for (int i = threadIdx.x; i < 2 * p.E; i += THREADS) s_mem[i] = 0;
-    tc::wait_for_previous_kernel();
-    __syncthreads();
-    // parts of the blocks by `slices` teams of threads, an expert to a thread
-    const int width = (p.E + 31) / 32 * 32, slices = max(1, THREADS / width), blocks = gridDim.x;
-    for (int e = threadIdx.x % width, s = threadIdx.x / width; s < slices && e < p.E; e += width) {
-        const int b0 = (int)((int64_t)blocks * s / slices), b1 = (int)((int64_t)blocks * (s + 1) / slices);
-        int all = 0, before = 0;
-#pragma unroll 8
-        for (int b = b0; b < b1; ++b) {
-            const int c = p.counts[(int64_t)b * p.E + e];
-            all += c;
-            before += b < (int)blockIdx.x ? c : 0;
-        }
-        atomicAdd(&s_all[e], all);
-        atomicAdd(&s_before[e], before);
-    }
-    __syncthreads();
-    if (threadIdx.x < 32) scan_counts(s_all, p.E, s_first);
-    __syncthreads();
-    if (blockIdx.x == 0) for (int e = threadIdx.x; e <= p.E; e += THREADS) p.offset[e] = s_first[e];
-    const int64_t from = (int64_t)blockIdx.x * p.per_block * p.top, to = min((int64_t)p.T * p.top, from + (int64_t)p.per_block * p.top);
-    const int last = s_first[p.E];
-    for (int64_t i = from + threadIdx.x; i < to; i += THREADS) {
-        const int e = p.expert[i];
-        if (e >= 0) {
-            const int at = s_first[e] + s_before[e] + p.row[i];
-            p.row[i] = at;
-            p.token[at] = (int)(i / p.top);
-        }
-        if (i >= last) p.token[i] = -1;
+        i += 1024;
+        if (i < to) { e = p.expert[i]; in = p.row[i]; }
     }
 }
 
@@ -501,15 +690,19 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, in
 
 using namespace route;
 
-// Tokens of a block, and blocks: all SMs have some; one block has all where there are few.
+// Blocks of tokens.  One block has all where there are few, and its launch is the only one: a round of its warps takes 4 us more the fuller it is, the
+// second launch 3 (256 experts in groups, us alone / in two launches: 16 tokens 7 / 8, 32: 9.6 / 8, 64: 14.2 / 8).  Else as many blocks as SMs, of four tokens or more.
+constexpr int ALONE = 16;
+static_assert(ALONE <= CHUNK, "one chunk");
 static int blocks_of(int64_t T) {
-    if (T <= CHUNK) return 1;
-    const int64_t b = (T + 31) / 32, most = sm_count();
+    if (T <= ALONE) return 1;
+    const int64_t b = (T + 3) / 4, most = sm_count();
     return (int)(b < most ? b : most);
 }
+static int pitch_of(int64_t E) { return (int)((E + 3) / 4 * 4); }
 size_t route_count_bytes(int64_t T, int64_t E) {
-    const int64_t most = (T + 31) / 32 < 148 ? (T + 31) / 32 : sm_count() > 148 ? sm_count() : 148;
-    return (size_t)(most * E) * sizeof(int32_t);
+    const int64_t most = (T + 3) / 4 < 148 ? (T + 3) / 4 : sm_count() > 148 ? sm_count() : 148;
+    return (size_t)(most * pitch_of(E)) * sizeof(int32_t);
 }
 
 cudaError_t launch_route(const RouteCall &c, cudaStream_t st) {
@@ -517,17 +710,19 @@ cudaError_t launch_route(const RouteCall &c, cudaStream_t st) {
     p.logits = c.logits; p.ldl = c.ldl; p.bias = c.bias;
     p.T = (int)c.T; p.E = c.E; p.groups = c.groups; p.per = c.E / c.groups; p.kept = c.kept; p.best = c.best; p.top = c.top;
     p.sigmoid = c.sigmoid; p.renormalise = c.renormalise; p.scale = c.scale;
-    p.expert = c.expert; p.row = c.row; p.token = c.token; p.offset = c.offset; p.weight = c.weight; p.counts = c.counts;
-    p.lanes = 32;
-    while (p.lanes > 1 && p.lanes * c.groups > 32) p.lanes >>= 1;
-    p.each = (p.per + p.lanes - 1) / p.lanes;
+    p.expert = c.expert; p.row = c.row; p.token = c.token; p.offset = c.offset; p.weight = c.weight; p.counts = c.counts; p.pitch = pitch_of(c.E);
+    p.lg_lanes = 5;
+    while (p.lg_lanes > 0 && c.groups << p.lg_lanes > 32) --p.lg_lanes;
+    const int lanes = 1 << p.lg_lanes;
+    p.each = (p.per + lanes - 1) / lanes;
     const int blocks = blocks_of(c.T);
     p.per_block = (int)((c.T + blocks - 1) / blocks);
     const int V = p.each <= 2 ? 2 : p.each <= 4 ? 4 : p.each <= 8 ? 8 : p.each <= 16 ? 16 : 32;
     const int size = c.dtype == DT_F32 ? 4 : 2, bytes = V * size, unit = bytes < 16 ? bytes : 16;
-    const bool wide = V <= 8 && p.each == V && p.per == p.lanes * V && reinterpret_cast<uintptr_t>(c.logits) % unit == 0 && c.ldl * size % unit == 0;
-    const size_t smem = ((size_t)c.E * (CHUNK / 32 + 3) + 1) * 4 + (size_t)CHUNK * c.top * 2;
-    auto go = [&](auto kern) { return launch_overlapped(kern, dim3(blocks), (unsigned)THREADS, smem, st, 1, true, p); };
+    const bool wide = V <= 8 && p.each == V && p.per == lanes * V && reinterpret_cast<uintptr_t>(c.logits) % unit == 0 && c.ldl * size % unit == 0;
+    const unsigned threads = (unsigned)threads_for(V);
+    const size_t smem = threads / 32 * sizeof(Candidates) + ((size_t)c.E * (CHUNK / 32 + 2) + V) * 4 + (size_t)CHUNK * c.top * 2;
+    auto go = [&](auto kern) { return launch_overlapped(kern, dim3(blocks), threads, smem, st, 1, true, p); };
     auto with = [&](auto v, auto dt) {
         constexpr int VV = decltype(v)::value, DT = decltype(dt)::value;
         return wide ? go(route_kernel<VV, DT, VV <= 8>) : go(route_kernel<VV, DT, false>);
@@ -545,7 +740,7 @@ cudaError_t launch_route(const RouteCall &c, cudaStream_t st) {
         default: e = of(std::integral_constant<int, 32>{}); break;
     }
     if (e != cudaSuccess || blocks == 1) return e;
-    return launch_overlapped(place_kernel, dim3(blocks), (unsigned)THREADS, (size_t)(3 * c.E + 1) * 4, st, 1, true, p);
+    return launch_overlapped(place_kernel, dim3((blocks + PLACED - 1) / PLACED), 1024u, (size_t)(2 * std::min(SLICES, 4096 / p.pitch) + PLACED) * p.pitch * 4, st, 1, true, p, blocks);
 }
 
 cudaError_t launch_combine(const uint16_t *routes, int64_t ldr, int64_t R, const float *weight, const int32_t *row, int64_t T, int top, int64_t N, const uint16_t *add,

@@ -9,7 +9,7 @@ import torch
 from . import binding
 from .binding import CubicQuantError, _check, _stream
 from .fp4 import _DTYPE, _at, _check_offset, _check_rows, _here, _need
-from .route import Routes, _check_routes, _matrix
+from .route import Routes, _matrix
 
 _L = None
 
@@ -273,12 +273,9 @@ def cq_i8_moe(gate_up: I8Tensor, down: I8Tensor, x: torch.Tensor, routes: Routes
     T, K, ld, x_at, dtype = _check_rows(x)
     if dtype == 2 or K != H:
         raise CubicQuantError(f"x is [T, {H}] in bfloat16 or float16")
-    if routes.row.dim() != 2:
-        raise CubicQuantError("routes are those of cq_route")
-    top = routes.row.shape[1]
-    _check_routes(routes, T, top)
-    if routes.offset.numel() != E + 1:
-        raise CubicQuantError(f"routes go to {E} experts")
+    top = routes.top
+    if routes.tokens != T or routes.experts != E:
+        raise CubicQuantError(f"routes are those of {T} tokens to {E} experts")
     if out is None:
         out = torch.empty((T, H), dtype=x.dtype, device=x.device)
     ldy, lda = _matrix(out, "out", T, H, x.dtype), 0 if add is None else _matrix(add, "add", T, H, x.dtype)
@@ -286,7 +283,9 @@ def cq_i8_moe(gate_up: I8Tensor, down: I8Tensor, x: torch.Tensor, routes: Routes
         workspace = cq_i8_moe_workspace(gate_up, down, T, top)
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise CubicQuantError("workspace is a contiguous uint8 tensor")
-    stream = _here(x, gate_up.layout, gate_up.scale, down.layout, down.scale, routes.token, routes.offset, routes.row, routes.weight, add, workspace, out)
+    stream = _here(x, gate_up.layout, gate_up.scale, down.layout, down.scale, add, workspace, out)
+    if routes._device != x.get_device():
+        raise CubicQuantError(f"tensors on {x.device} and {routes.row.device}")
     if T:
         status = (_L or _lib()).cq_i8_moe(gate_up.layout.data_ptr(), gate_up.scale.data_ptr(), down.layout.data_ptr(), down.scale.data_ptr(), E, x_at, ld, T, top,
                                           routes.token.data_ptr(), routes.offset.data_ptr(), routes.row.data_ptr(), routes.weight.data_ptr(), _at(add), lda, out.data_ptr(), ldy, dtype,

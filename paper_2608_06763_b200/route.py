@@ -27,15 +27,30 @@ def _lib():
     return _L
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class Routes:
     """Where tokens go: `expert` and `weight` [T, top], and the map of the routes grouped by expert: `token` [T top], `offset` [E + 1], `row`
-    [T, top], the row of each choice.  -1: no choice, no route.  All int32 on the device but `weight`, fp32."""
+    [T, top], the row of each choice.  -1: no choice, no route.  All int32 but `weight`, fp32; contiguous, on one device.  Looked over once, when it is made."""
     expert: torch.Tensor
     weight: torch.Tensor
     token: torch.Tensor
     offset: torch.Tensor
     row: torch.Tensor
+
+    def __post_init__(self):
+        ints = (self.expert, self.token, self.offset, self.row)
+        if not all(isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.is_contiguous() for t in ints):
+            raise CubicQuantError("routes are contiguous int32 tensors")
+        if not isinstance(self.weight, torch.Tensor) or self.weight.dtype != torch.float32 or not self.weight.is_contiguous():
+            raise CubicQuantError("the weights of routes are a contiguous fp32 tensor")
+        if self.expert.dim() != 2 or self.weight.shape != self.expert.shape or self.row.shape != self.expert.shape or self.token.shape != (self.expert.numel(),):
+            raise CubicQuantError("routes are expert, weight and row [T, top] and token [T top]")
+        if self.offset.dim() != 1 or self.offset.numel() < 2:
+            raise CubicQuantError("the offsets of routes are a value more than there are experts")
+        if any(t.device != self.weight.device for t in ints):
+            raise CubicQuantError("routes are on one device")
+        for name, value in (("tokens", self.expert.shape[0]), ("top", self.expert.shape[1]), ("experts", self.offset.numel() - 1), ("_device", self.weight.get_device())):
+            object.__setattr__(self, name, value)
 
 
 def cq_routes_empty(T: int, E: int, top: int, device=None) -> Routes:
@@ -49,16 +64,6 @@ def cq_route_workspace(T: int, E: int, device=None) -> torch.Tensor:
     n = _lib().cq_route_workspace_bytes(max(T, 1), E)
     _need(n > 0, f"no routing of {T} tokens to {E} experts")
     return torch.empty(n, dtype=torch.uint8, device=device or "cuda")
-
-
-def _check_routes(r: Routes, T: int, top: int):
-    for t, shape in ((r.expert, (T, top)), (r.row, (T, top)), (r.token, (T * top,))):
-        if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
-            raise CubicQuantError(f"routes of {T} tokens to {top} experts: contiguous int32 tensors")
-    if r.weight.dtype != torch.float32 or r.weight.shape != (T, top) or not r.weight.is_contiguous():
-        raise CubicQuantError("the weights of routes are a contiguous fp32 tensor")
-    if r.offset.dtype != torch.int32 or r.offset.dim() != 1 or not r.offset.is_contiguous():
-        raise CubicQuantError("the offsets of routes are a contiguous int32 tensor")
 
 
 def cq_route(logits: torch.Tensor, top: int, score: int = CQ_SOFTMAX, bias: torch.Tensor | None = None, groups: int = 1, groups_kept: int | None = None, group_best: int = 2,
@@ -80,15 +85,15 @@ def cq_route(logits: torch.Tensor, top: int, score: int = CQ_SOFTMAX, bias: torc
         raise CubicQuantError("top is 1 or more")
     if out is None:
         out = cq_routes_empty(T, E, top, logits.device)
-    else:
-        _check_routes(out, T, top)
-        if out.offset.numel() != E + 1:
-            raise CubicQuantError("out is of another number of experts")
+    elif out.tokens != T or out.top != top or out.experts != E:
+        raise CubicQuantError(f"out is for {out.tokens} tokens to {out.top} of {out.experts} experts")
     if workspace is None:
         workspace = cq_route_workspace(T, E, logits.device)
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise CubicQuantError("workspace is a contiguous uint8 tensor")
-    stream = _here(logits, bias, out.expert, out.weight, out.token, out.offset, out.row, workspace)
+    stream = _here(logits, bias, workspace)
+    if out._device != logits.get_device():
+        raise CubicQuantError(f"tensors on {logits.device} and {out.expert.device}")
     if not T:
         out.offset.zero_()
         return out
@@ -118,19 +123,18 @@ def cq_combine(y_routes: torch.Tensor, routes: Routes, add: torch.Tensor | None 
     code = _DTYPE.get(y_routes.dtype)
     if code is None or code == 2 or y_routes.dim() != 2:
         raise CubicQuantError("y_routes is [R, N] in bfloat16 or float16")
-    row, weight = routes.row, routes.weight
-    if row.dtype != torch.int32 or row.dim() != 2 or not row.is_contiguous() or weight.dtype != torch.float32 or weight.shape != row.shape or not weight.is_contiguous():
-        raise CubicQuantError("routes have contiguous rows (int32) and weights (fp32) of [T, top]")
     R, N = y_routes.shape
-    T, top = row.shape
-    ldr = _matrix(y_routes, "y_routes", R, N, y_routes.dtype)
+    T, top, dtype = routes.tokens, routes.top, y_routes.dtype
+    ldr = _matrix(y_routes, "y_routes", R, N, dtype)
     if out is None:
-        out = torch.empty((T, N), dtype=y_routes.dtype, device=y_routes.device)
-    ldy = _matrix(out, "out", T, N, y_routes.dtype)
-    lda = 0 if add is None else _matrix(add, "add", T, N, y_routes.dtype)
-    stream = _here(y_routes, row, weight, add, out)
+        out = torch.empty((T, N), dtype=dtype, device=y_routes.device)
+    ldy = _matrix(out, "out", T, N, dtype)
+    lda = 0 if add is None else _matrix(add, "add", T, N, dtype)
+    stream = _here(y_routes, add, out)
+    if routes._device != y_routes.get_device():
+        raise CubicQuantError(f"tensors on {y_routes.device} and {routes.row.device}")
     if T and N and R:
-        status = (_L or _lib()).cq_combine(y_routes.data_ptr(), ldr, R, weight.data_ptr(), row.data_ptr(), T, top, N, _at(add), lda, out.data_ptr(), ldy, code, stream)
+        status = (_L or _lib()).cq_combine(y_routes.data_ptr(), ldr, R, routes.weight.data_ptr(), routes.row.data_ptr(), T, top, N, _at(add), lda, out.data_ptr(), ldy, code, stream)
         if status != 0:
             _check(status, "cq_combine")
     elif T and N:   # no route at all

@@ -156,6 +156,19 @@ def test_swiglu_far_gates_subnormal_and_non_finite():
         check_codes(cq.cq_i8_swiglu_quantize(h.cuda()), *ref.quantize(as64(act)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M,I", [(6000, 32), (3000, 272), (20, 100000)])
+def test_swiglu_roundings_that_32_bits_leave_open(M, I, dtype):
+    """Short rows, whose largest value is open often, rows beyond what is kept of them, and activations about the least half."""
+    h = rows(M, 2 * I, dtype, seed=M, spread=0.5)
+    h[M // 3: M // 2] *= 1e-3 if dtype == "f16" else 1e-18
+    h[M // 2: M // 2 + 5] *= 2e-4 if dtype == "f16" else 1e-19
+    h[-1] = 0
+    v = as64(h)
+    act = torch.from_numpy(ref.gated(v[:, :I], v[:, I:])).to(DTYPE[dtype])
+    check_codes(cq.cq_i8_swiglu_quantize(h.cuda()), *ref.quantize(as64(act)))
+
+
 def product_case(M, N, K, dtype, seed=0):
     r = np.random.default_rng(seed)
     wc, wd = r.integers(-128, 128, (N, K)).astype(np.int8), (0.001 * np.exp(0.5 * r.standard_normal(N))).astype(np.float32)

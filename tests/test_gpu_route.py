@@ -256,8 +256,8 @@ def combine_case(T, N, top, R, dtype, seed, add):
 
 
 def as_routes(row, weight):
-    z = torch.zeros(1, dtype=torch.int32, device="cuda")
-    return cq.Routes(row.cuda(), weight.cuda(), z, z, row.cuda())
+    z = torch.zeros(max(2, row.numel()), dtype=torch.int32, device="cuda")
+    return cq.Routes(row.cuda(), weight.cuda(), z[:row.numel()], z[:2], row.cuda())
 
 
 def check_combine(got, y, row, weight, add):

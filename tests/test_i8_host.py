@@ -159,6 +159,14 @@ def test_python_route_refuses():
                 lambda: cq.cq_route_workspace(4, 513)):
         with pytest.raises(E):
             bad()
+    z = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    cq.Routes(z(4, 2), torch.zeros((4, 2)), z(8), z(5), z(4, 2))
+    for bad in (lambda: cq.Routes(z(4, 2).long(), torch.zeros((4, 2)), z(8), z(5), z(4, 2)), lambda: cq.Routes(z(4, 2), z(4, 2), z(8), z(5), z(4, 2)),
+                lambda: cq.Routes(z(4, 2), torch.zeros((4, 3)), z(8), z(5), z(4, 2)), lambda: cq.Routes(z(4, 2), torch.zeros((4, 2)), z(7), z(5), z(4, 2)),
+                lambda: cq.Routes(z(4, 2), torch.zeros((4, 2)), z(8), z(1), z(4, 2)), lambda: cq.Routes(z(2, 4).T, torch.zeros((4, 2)), z(8), z(5), z(4, 2)),
+                lambda: cq.Routes(z(4, 2), torch.zeros((4, 2)), z(8), [0, 8], z(4, 2)), lambda: cq.Routes(z(8), torch.zeros(8), z(8), z(5), z(8))):
+        with pytest.raises(E):
+            bad()
     y = torch.zeros((8, 16), dtype=torch.bfloat16)
     for bad in (lambda: cq.cq_combine(y.float(), r), lambda: cq.cq_combine(y[0], r), lambda: cq.cq_combine(y.T, r), lambda: cq.cq_combine(y, r, add=torch.zeros((4, 15), dtype=torch.bfloat16)),
                 lambda: cq.cq_combine(y, r, add=torch.zeros((4, 16))), lambda: cq.cq_combine(y, r, out=torch.zeros((4, 16), dtype=torch.float16)),
