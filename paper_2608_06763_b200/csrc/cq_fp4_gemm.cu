@@ -24,6 +24,7 @@ struct GemmArgs {
     bool early;              // launched right behind the quantiser of x: everything else may be read before that has ended
     const uint16_t *xr;      // FEW: rows of x in the model dtype, ldx apart
     int64_t ldx, K;
+    __device__ __forceinline__ int rows_of_tile(int, int) const { return bt; }
 };
 
 // What a CTA computes.  ONE: 128 channels x up to 128 rows of x; TWO: a pair of CTAs 256 channels x up to 256 rows; FEW: 128 channels x up to 16

@@ -214,15 +214,15 @@ int cq_i8_linear_routed(const void *w, const float *w_scale, const uint16_t *x, 
 
 size_t cq_i8_moe_workspace_bytes(int64_t E, int64_t T, int top, int64_t H, int64_t I) { return check_moe(E, T, top, H, I) == CQ_OK ? moe_plan(E, T * top, H, I).total : 0; }
 int cq_i8_moe(const void *gate_up, const float *gate_up_scale, const void *down, const float *down_scale, int64_t E, const uint16_t *x, int64_t ldx, int64_t T, int top,
-              const int32_t *route_token, const int32_t *expert_offset, const int32_t *route_row, const float *weight, const uint16_t *add, int64_t lda, uint16_t *y, int64_t ldy,
+              const int32_t *expert_offset, const int32_t *route_row, const float *weight, const uint16_t *add, int64_t lda, uint16_t *y, int64_t ldy,
               int act_f16, int64_t H, int64_t I, void *workspace, size_t workspace_bytes, void *stream) {
-    if (!gate_up || !gate_up_scale || !down || !down_scale || !x || !route_token || !expert_offset || !route_row || !weight || !y || !workspace) return CQ_ERR_INVALID_ARG;
+    if (!gate_up || !gate_up_scale || !down || !down_scale || !x || !expert_offset || !route_row || !weight || !y || !workspace) return CQ_ERR_INVALID_ARG;
     CQ_TRY(check_moe(E, T, top, H, I));
     const int dtype = act_f16 ? CQ_F16 : CQ_BF16;
     CQ_TRY(check_rows(x, dtype, ldx, H));
     if (ldy < H || (add && lda < H)) return CQ_ERR_INVALID_ARG;
     if (misaligned(gate_up) || misaligned(down) || misaligned(workspace) || misaligned(gate_up_scale, 4) || misaligned(down_scale, 4) || misaligned(weight, 4) ||
-        misaligned(route_token, 4) || misaligned(expert_offset, 4) || misaligned(route_row, 4) || misaligned(add, 2) || misaligned(y, 2))
+        misaligned(expert_offset, 4) || misaligned(route_row, 4) || misaligned(add, 2) || misaligned(y, 2))
         return CQ_ERR_ALIGNMENT;
     const int64_t R = T * top;
     const MoePlan p = moe_plan(E, R, H, I);
@@ -233,7 +233,8 @@ int cq_i8_moe(const void *gate_up, const float *gate_up_scale, const void *down,
     float *xs = (float *)(ws + p.x_scale), *as = (float *)(ws + p.a_scale);
     uint16_t *h = (uint16_t *)(ws + p.h);
     const bool f16 = act_f16 != 0;
-    CQ_TRY(wrap(launch_i8_quantize(x, dtype, ldx, routed_rows(route_token, expert_offset, E, R, T), H, xs, ws + p.x, st)));
+    // a token is quantised once, whatever the number of its routes
+    CQ_TRY(wrap(launch_i8_quantize(x, dtype, ldx, I8Rows{nullptr, expert_offset, (int)E, T, T, T, route_row, top, R}, H, xs, ws + p.x, st)));
     CQ_TRY(wrap(launch_i8_gemm(gate_up, gate_up_scale, ws + p.x, xs, expert_offset, (int)E, h, R, 2 * I, H, f16, true, (int *)ws, st)));
     CQ_TRY(wrap(launch_i8_swiglu_quantize(h, dtype, 2 * I, routed_rows(nullptr, expert_offset, E, R, R), I, as, ws + p.a, st)));
     CQ_TRY(wrap(launch_i8_gemm(down, down_scale, ws + p.a, as, expert_offset, (int)E, h, R, H, I, f16, true, (int *)ws, st)));
@@ -245,7 +246,7 @@ int cq_debug_i8_plan(int64_t E, int64_t M, int64_t N, int64_t K, int quantised, 
     const bool routed = E > 0;
     CQ_TRY(check_product(routed ? E : 1, routed, M, N, K));
     const bool own = !quantised && !routed && i8_few_ok(M, N, K);
-    const I8Plan p = i8_plan(E, routed, M, N, K, own);
+    const I8Plan p = i8_plan(routed, M, N, K, own);
     plan[0] = p.channels; plan[1] = p.rows; plan[2] = p.runs; plan[3] = own;
     return CQ_OK;
 }

@@ -22,6 +22,8 @@ struct GemmArgs {
     bool early;              // launched right behind the quantiser of x: everything else may be read before that has ended
     const uint16_t *xr;      // FEW: rows of x in the model dtype, ldx apart
     int64_t ldx, K;
+    // a group's rows in even tiles: 300 rows as 160 and 140, not as 256 and 44
+    __device__ __forceinline__ int rows_of_tile(int rows, int tiles) const { return offset ? ((rows + tiles - 1) / tiles + 31) & ~31 : bt; }
 };
 
 // What a CTA computes.  ONE: 128 channels x up to 128 rows of x; TWO: a pair of CTAs 256 channels x up to 256 rows; FEW: 128 channels x up to 16
@@ -464,14 +466,20 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
     return p;
 }
 
-// What computes a product of more than sixteen rows: kind of tile, rows to a tile, runs of k (log2).  Costs in microseconds.  A k tile of one CTA
-// takes as long as an SM's port to L2 does for its bytes (113 bytes a nanosecond); a pair's, its MMAs.  Cutting k saves k tiles and costs a cluster's
-// launch and the exchange.
+// What computes a product of more than sixteen rows: kind of tile, rows to a tile, runs of k (log2).  Costs in microseconds, from tiles forced in turn.  A k
+// tile of one CTA takes as long as an SM's port to L2 does for its bytes (113 bytes a nanosecond); a pair's, its MMAs.  Cutting k saves k tiles and costs a
+// cluster's launch and the exchange.
+//   4096 x 4096, 17 rows: SMALL 10.0, in two runs 7.6, four 7.2;  64 rows: 10.7 / 8.8 / 8.1;  4096 x 14336, 64 rows: 29.7 / 17.7 / 12.8;  100 rows: ONE 31.7, two runs
+//   19.9, four 14.7, SMALL in two 18.5, TWO 26.5;  200 rows: ONE in two runs 21.0, whole 32.0, SMALL 30.2, TWO 26.5 to 32.2;  4096 x 4096, 200 rows: SMALL 11.1, ONE 12.0
+//   (two runs 11.1), TWO 10.9 to 13.0;  700 rows: TWO 18.0 / 13.4 / 15.5 with 128 / 192 / 256 rows, ONE 21.2;  6144 x 4096, 1024 rows: TWO 25.5 / 21.2 / 24.2, ONE 30.0
+// Tried and dropped, sums through L2 where integers may be added in any order: even runs of all k tiles for each CTA (4096 x 4096, one row 11.0 us
+// instead of 7.8, 28672 x 4096 26 as before, 57344 x 8192 79.7 instead of 84.2), the last round's pairs cut along K (200 rows of 4096 x 14336 21.5, 1024 of 6144 x 4096
+// 28.8): an exchange there takes some four microseconds of fences, counting and reading back, and each run has two ends.
 struct Plan { int mode, bt, lg; };
 static Plan dense_plan(int64_t M, int NB, int KT) {
-    static const Plan kinds[] = {{SMALL, 64, 0}, {SMALL, 64, 1}, {ONE, 128, 0}, {ONE, 128, 1}, {TWO, 128, 0}, {TWO, 192, 0}, {TWO, 256, 0}};
+    static const Plan kinds[] = {{SMALL, 64, 0}, {SMALL, 64, 1}, {SMALL, 64, 2}, {ONE, 128, 0}, {ONE, 128, 1}, {ONE, 128, 2}, {TWO, 128, 0}, {TWO, 192, 0}, {TWO, 256, 0}};
     const int sms = sm_count();
-    Plan best = kinds[2];
+    Plan best = kinds[3];
     double least = 1e30;
     for (const Plan &k : kinds) {
         const int ctas = k.mode == TWO ? 2 : 1, S = 1 << k.lg, nbu = (NB + ctas - 1) / ctas, places = sms / ctas;
@@ -490,23 +498,25 @@ static Plan dense_plan(int64_t M, int NB, int KT) {
     }
     return best;
 }
-// Routed rows: the loads are on the GPU, so the mean decides.
-static Plan routed_plan(int64_t mean) { return mean > 256 ? Plan{TWO, 256, 0} : mean > 48 ? Plan{ONE, 128, 0} : Plan{SMALL, 64, 0}; }
-
+// Up to sixteen rows.  A CTA's own quantising takes 0.3 us for each row of 4096, the launch in front of it is hidden but for the host's part, some two microseconds: us on
+// the GPU, by itself / in front: 4096 x 4096, rows 1 to 4: 8.1 / 7.8, 8.3 / 7.7, 8.6 / 8.0, 8.9 / 8.0, 8: 11.0 / 8.1;  8192 x 2048, 4: 8.3 / 7.8, 8: 9.8 / 7.9;  4096 x 14336, 1: 13.1 / 13.4, 2:
+// 15.0 / 13.4;  28672 x 4096, 1: 23.1 / 25.3, 4: 26.4 / 25.8.  FEW_MOST: rows x k tiles of 128.
+constexpr int FEW_MOST = 112;
 bool i8_few_ok(int64_t M, int64_t N, int64_t K) {
     if (M > FEW_ROWS) return false;
     const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
-    return most <= FEW_TILES && M * KT <= 256;
+    return most <= FEW_TILES && M * KT <= FEW_MOST;
 }
-// what launch_i8_few (own) or launch_i8_gemm takes for M rows; routed: of E matrices
-static Plan plan_of(int64_t E, bool routed, int64_t M, int64_t N, int64_t K) {
+// What launch_i8_gemm takes for M rows.  Routed rows: the loads are on the GPU, and pairs with 256 rows serve all of them.  Sixteen matrices of 2816 x 2048, us with SMALL / ONE /
+// TWO: 2 rows on average 11.0 / 11.1 / 10.7, 24: 16.2 / 16.3 / 15.4, 64: 21.3 / 18.9 / 17.3, 256: 50.4 / 37.3 / 30.1, 512: 98.5 / 59.8 / 45.0.
+static Plan plan_of(bool routed, int64_t M, int64_t N, int64_t K) {
     const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB);
-    if (routed) return routed_plan(M / E);
+    if (routed) return {TWO, 256, 0};
     return M <= FEW_ROWS ? Plan{SMALL, 64, lg_runs_of(NB, KT, sm_count())} : dense_plan(M, NB, KT);
 }
-I8Plan i8_plan(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, bool own) {
+I8Plan i8_plan(bool routed, int64_t M, int64_t N, int64_t K, bool own) {
     if (own) return I8Plan{128, FEW_ROWS, 1 << lg_runs_of((int)((N + 127) / 128), (int)((K + KB - 1) / KB), sm_count())};
-    const Plan q = plan_of(E, routed, M, N, K);
+    const Plan q = plan_of(routed, M, N, K);
     return I8Plan{q.mode == TWO ? 256 : 128, q.bt, 1 << q.lg};
 }
 cudaError_t launch_i8_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, uint16_t *y, int64_t M, int64_t N, int64_t K, bool f16, int *status, cudaStream_t st) {
@@ -522,7 +532,7 @@ cudaError_t launch_i8_gemm(const void *w, const float *w_scale, const void *x, c
     GemmArgs p = args_of(w, w_scale, x_scale, y, M, N, K, f16, status);
     p.early = early;
     p.x = (const uint8_t *)x; p.offset = offset; p.E = E;
-    const Plan q = plan_of(E, offset != nullptr, M, N, K);
+    const Plan q = plan_of(offset != nullptr, M, N, K);
     p.bt = q.bt;
     p.token_tiles = (int)((M + q.bt - 1) / q.bt);
     const int ctas = q.mode == TWO ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sm_count() / ctas;

@@ -17,25 +17,26 @@ struct Rows {
     int E;                        // groups, or matrices of `per` rows each
     int64_t per, rows, T;         // rows of one matrix; all rows; rows that x has
     int team, held;               // threads to a row; units of a row that are kept, a multiple of `team`
+    const int32_t *route_row;     // SCATTER: rows are tokens, [rows][top] the routes of each (-1: none); `routes` of all
+    int top, routes;
 };
 struct Place { int64_t src, at; bool live, read; };   // row of x; row among the padded rows of the layout; whether it is one; whether x has it
 __device__ __forceinline__ void scan_if_routed(const Rows &q, int *s_off, int *s_blk) {
     if (!q.offset) return;
-    if (threadIdx.x < 32) scan_groups(q.offset, q.E, (int)q.rows, s_off, s_blk);
+    if (threadIdx.x < 32) scan_groups(q.offset, q.E, q.route_row ? q.routes : (int)q.rows, s_off, s_blk);
     __syncthreads();
 }
-__device__ __forceinline__ Place place_of(const Rows &q, int64_t r, const int *s_off, const int *s_blk) {
-    Place p{r, r, r < q.rows, r < q.rows};
+// the row of x that row r takes; known before the groups are
+__device__ __forceinline__ int64_t source_of(const Rows &q, int64_t r) { return q.route_token && r < q.rows ? q.route_token[r] : r; }
+__device__ __forceinline__ Place place_of(const Rows &q, int64_t r, int64_t source, const int *s_off, const int *s_blk) {
+    Place p{source, r, r < q.rows, r < q.rows};
     if (q.offset) {
         p.live = p.live && r >= s_off[0] && r < s_off[q.E];
         p.read = p.live;
         if (p.live) {
             const int e = find_group(s_off, q.E, (int)r);
             p.at = (int64_t)s_blk[e] * ROWS + (r - s_off[e]);
-            if (q.route_token) {
-                p.src = q.route_token[r];
-                p.read = p.src >= 0 && p.src < q.T;   // any other token is a row of zeros
-            }
+            if (q.route_token) p.read = source >= 0 && source < q.T;   // any other token is a row of zeros
         }
     } else if (q.E > 1 && p.live) {
         const int64_t e = r / q.per;
@@ -65,16 +66,17 @@ struct Plain {
     static constexpr int PIECES = DT == DT_F32 ? 4 : 2, AHEAD = DT == DT_F32 ? 2 : 4;   // units whose loads are on their way together
     const void *x;
     int64_t ldx;
+    static constexpr int UNIT = 16 * PIECES;   // bytes of a unit
     struct Raw { uint4 q[PIECES]; };
-    __device__ __forceinline__ Raw load(int64_t row, int64_t unit, bool read) const {
-        const uint8_t *p = reinterpret_cast<const uint8_t *>(x) + (row * ldx + unit * 16) * (DT == DT_F32 ? 4 : 2);
+    __device__ __forceinline__ const uint8_t *unit(int64_t row, int u) const { return reinterpret_cast<const uint8_t *>(x) + row * ldx * (DT == DT_F32 ? 4 : 2) + (int64_t)u * UNIT; }
+    __device__ __forceinline__ Raw load(const uint8_t *p, bool read) const {
         Raw r;
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) r.q[k] = read ? load16(p + 16 * k) : make_uint4(0, 0, 0, 0);
         return r;
     }
     // to a slot of the store; the largest magnitude.  The whole warp.
-    __device__ __forceinline__ void keep(const Raw &r, int64_t, int64_t, bool, const Store &s, int slot, uint32_t &largest) const {
+    __device__ __forceinline__ void keep(const Raw &r, const uint8_t *, bool, const Store &s, int slot, uint32_t &largest) const {
         uint32_t w[4 * PIECES], top = 0;
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
@@ -111,23 +113,24 @@ struct Plain {
 // where the row's largest or a code hangs on them: one in fifty does, but telling them costs more than forming them, 126 us instead of 112.)
 template <int DT>
 struct Gated {
-    static constexpr int AHEAD = 1, PIECES = 2;
+    static constexpr int AHEAD = 1, PIECES = 2, UNIT = 32;
     const uint16_t *h;
     int64_t ldh, I;
     struct Raw { uint4 g[2], u[2]; };
-    __device__ __forceinline__ Raw load(int64_t row, int64_t unit, bool read) const {
-        const uint16_t *pg = h + row * ldh + unit * 16, *pu = pg + I;
+    __device__ __forceinline__ const uint8_t *unit(int64_t row, int u) const { return reinterpret_cast<const uint8_t *>(h + row * ldh) + (int64_t)u * UNIT; }
+    __device__ __forceinline__ Raw load(const uint8_t *p, bool read) const {
+        const uint8_t *pu = p + I * 2;
         Raw r;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            r.g[k] = read ? load16(pg + 8 * k) : make_uint4(0, 0, 0, 0);
-            r.u[k] = read ? load16(pu + 8 * k) : make_uint4(0, 0, 0, 0);
+            r.g[k] = read ? load16(p + 16 * k) : make_uint4(0, 0, 0, 0);
+            r.u[k] = read ? load16(pu + 16 * k) : make_uint4(0, 0, 0, 0);
         }
         return r;
     }
     // value k of a unit in 64 bits
-    __device__ __forceinline__ void settle(int64_t row, int64_t unit, int k, const Store &s, int slot) const {
-        const uint16_t *pg = h + row * ldh + unit * 16 + k;
+    __device__ __forceinline__ void settle(const uint8_t *p, int k, const Store &s, int slot) const {
+        const uint16_t *pg = reinterpret_cast<const uint16_t *>(p) + k;
         const uint32_t g = pg[0], u = pg[I];
         const float y = gated_in_64_bits(value_of<DT>(&g, 0), value_of<DT>(&u, 0));
         reinterpret_cast<uint16_t *>(&s.piece(slot, k >> 3))[k & 7] = (uint16_t)pack16<DT>(y, 0.0f);
@@ -137,7 +140,7 @@ struct Gated {
         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         return top_of_16bit<DT>(w);
     }
-    __device__ __forceinline__ void keep(const Raw &r, int64_t row, int64_t unit, bool read, const Store &s, int slot, uint32_t &largest) const {
+    __device__ __forceinline__ void keep(const Raw &r, const uint8_t *p, bool read, const Store &s, int slot, uint32_t &largest) const {
         const uint32_t gw[8] = {r.g[0].x, r.g[0].y, r.g[0].z, r.g[0].w, r.g[1].x, r.g[1].y, r.g[1].z, r.g[1].w};
         const uint32_t uw[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[1].x, r.u[1].y, r.u[1].z, r.u[1].w};
         uint32_t act[8], low[8], near = ~0u, least = ~0u;
@@ -174,7 +177,7 @@ struct Gated {
             }
             for (; mask; mask &= mask - 1) {
                 const int b = __ffs(mask) - 1;
-                settle(row, unit, 2 * (b & 15) + (b >> 4), s, slot);
+                settle(p, 2 * (b & 15) + (b >> 4), s, slot);
             }
             top = top_of(s, slot);
         }
@@ -188,7 +191,9 @@ struct Gated {
 };
 
 // ---------------------------------------------------------------- the quantisers
-template <class From>
+// SCATTER: a token's codes go to all of its routes, formed once.
+struct Copy { uint8_t *line; int row; };   // the row block of a route, the row in it
+template <class From, bool SCATTER>
 __global__ void __launch_bounds__(512, 2) quantize_kernel(const From from, Rows q, int64_t K, int KT, float *scale, uint8_t *layout) {
     extern __shared__ uint4 s_store[];
     __shared__ uint32_t red[2][16];
@@ -196,36 +201,65 @@ __global__ void __launch_bounds__(512, 2) quantize_kernel(const From from, Rows 
     const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, mine = threadIdx.x / q.team, KU = (int)(K >> 4), units = KT * 8;
     const int slots = q.held < KU ? q.held + q.team : q.held;   // a row that is longer has a slot for each thread besides
     const Store s{s_store + mine * From::PIECES * slots, slots};
-    int *s_off = reinterpret_cast<int *>(s_store + teams * From::PIECES * slots), *s_blk = s_off + q.E + 1;
+    Copy *s_copy = reinterpret_cast<Copy *>(s_store + teams * From::PIECES * slots);   // SCATTER: [teams][two rows in turn][top]
+    int *s_off = reinterpret_cast<int *>(s_copy + (SCATTER ? 2 * teams * q.top : 0)), *s_blk = s_off + q.E + 1;
+    const int64_t stride = (int64_t)gridDim.x * teams;
+    int64_t r = (int64_t)blockIdx.x * teams + mine, next = source_of(q, r);
     scan_if_routed(q, s_off, s_blk);
     int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * teams + mine; r - mine < q.rows; r += (int64_t)gridDim.x * teams, turn ^= 1) {
-        const Place p = place_of(q, r, s_off, s_blk);
+    for (; r - mine < q.rows; r += stride, turn ^= 1) {
+        const Place p = SCATTER ? Place{r, 0, r < q.rows, r < q.rows} : place_of(q, r, next, s_off, s_blk);
+        Copy *copies = s_copy + (2 * mine + turn) * q.top;   // read until the next row's barrier, written again behind it
+        if (SCATTER) {
+            for (int j = in; j < q.top; j += q.team) {
+                const int route = p.live ? q.route_row[r * q.top + j] : -1;
+                const bool there = route >= s_off[0] && route < s_off[q.E];
+                const int e = there ? find_group(s_off, q.E, route) : 0, at = there ? s_blk[e] * ROWS + (route - s_off[e]) : 0;
+                copies[j] = Copy{there ? layout + (int64_t)(at >> 7) * KT * TILE_BYTES : nullptr, at & (ROWS - 1)};
+            }
+            __syncwarp();
+        } else {
+            next = source_of(q, r + stride);
+        }
         uint32_t top = 0;
-        for (int u0 = in; u0 - in < KU; u0 += From::AHEAD * q.team) {   // whole warps
+        const uint8_t *first = from.unit(p.src, in), *src = first;
+        const int64_t step = (int64_t)q.team * From::UNIT;
+        for (int u0 = in; u0 - in < KU; u0 += From::AHEAD * q.team, src += From::AHEAD * step) {   // whole warps
             typename From::Raw raw[From::AHEAD];
 #pragma unroll
-            for (int i = 0; i < From::AHEAD; ++i) raw[i] = from.load(p.src, u0 + i * q.team, p.read && u0 + i * q.team < KU);
+            for (int i = 0; i < From::AHEAD; ++i) raw[i] = from.load(src + i * step, p.read && u0 + i * q.team < KU);
 #pragma unroll
             for (int i = 0; i < From::AHEAD; ++i) {
                 const int u = u0 + i * q.team;
                 if (u - in >= KU) break;
-                from.keep(raw[i], p.src, u, p.read && u < KU, s, u < q.held ? u : q.held + in, top);
+                from.keep(raw[i], src + i * step, p.read && u < KU, s, u < q.held ? u : q.held + in, top);
             }
         }
-        const float d = row_scale(team_max(top, q.team, red[turn])), inverse = __fdiv_rn(1.0f, d);
-        if (p.live && in == 0) scale[r] = d;
-        uint8_t *line = layout + (p.at >> 7) * KT * (int64_t)TILE_BYTES;
-        const int rr = (int)(p.at & (ROWS - 1));
+        const float d = row_scale(team_max(top, q.team, red[turn])), inverse = __frcp_rn(d);
+        if (SCATTER) {
+            for (int j = in; j < q.top; j += q.team)
+                if (copies[j].line) scale[q.route_row[r * q.top + j]] = d;
+        } else if (p.live && in == 0) {
+            scale[r] = d;
+        }
+        // a unit's place in its tile is that of the thread, 8 units a tile
+        uint8_t *dst = layout + ((p.at >> 7) * KT + (in >> 3)) * (int64_t)TILE_BYTES + piece_offset((int)(p.at & (ROWS - 1)), in & 7);
+        const int64_t dst_step = (int64_t)(q.team >> 3) * TILE_BYTES;
+        src = first;
 #pragma unroll 1
-        for (int u = in; u - in < units; u += q.team) {
+        for (int u = in; u - in < units; u += q.team, src += step, dst += dst_step) {
             const int slot = u < q.held ? u : q.held + in;
-            if (u >= q.held && u - in < KU) {   // formed again
-                from.keep(from.load(p.src, u, p.read && u < KU), p.src, u, p.read && u < KU, s, slot, top);
-            }
+            if (u >= q.held && u - in < KU) from.keep(from.load(src, p.read && u < KU), src, p.read && u < KU, s, slot, top);   // formed again
             if (u < units && p.live) {
                 const uint4 c = u < KU ? from.codes(s, slot, d, inverse) : make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(line + (int64_t)(u >> 3) * TILE_BYTES + piece_offset(rr, u & 7)) = c;
+                if (SCATTER) {
+                    for (int j = 0; j < q.top; ++j) {
+                        const Copy to = copies[j];
+                        if (to.line) *reinterpret_cast<uint4 *>(to.line + (int64_t)(u >> 3) * TILE_BYTES + piece_offset(to.row, in & 7)) = c;
+                    }
+                } else {
+                    *reinterpret_cast<uint4 *>(dst) = c;
+                }
             }
         }
     }
@@ -242,7 +276,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t *layout, 
     scan_if_routed(q, s_off, s_blk);
     const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, units = (int)(K >> 4), odd = threadIdx.x & 1;
     for (int64_t r = (int64_t)blockIdx.x * teams + threadIdx.x / q.team; r < q.rows; r += (int64_t)gridDim.x * teams) {
-        const Place p = place_of(q, r, s_off, s_blk);
+        const Place p = place_of(q, r, r, s_off, s_blk);
         if (!p.live) continue;
         const float s = scale[r];
         const uint8_t *line = layout + (p.at >> 7) * KT * (int64_t)TILE_BYTES;
@@ -283,7 +317,7 @@ __global__ void __launch_bounds__(256) exchange_kernel(uint8_t *codes, Rows q, i
     const int64_t units = (int64_t)KT * 8, total = q.rows * units;
     for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (int64_t)gridDim.x * 256) {
         const int64_t row = idx / units, u = idx - row * units;
-        const Place p = place_of(q, row, nullptr, nullptr);
+        const Place p = place_of(q, row, row, nullptr, nullptr);
         uint4 *at = reinterpret_cast<uint4 *>(layout + ((p.at >> 7) * KT + (u >> 3)) * (int64_t)TILE_BYTES + piece_offset((int)(p.at & (ROWS - 1)), (int)(u & 7)));
         uint4 *c = reinterpret_cast<uint4 *>(codes + row * K + u * 16);
         const bool inside = u * 16 < K;
@@ -293,12 +327,15 @@ __global__ void __launch_bounds__(256) exchange_kernel(uint8_t *codes, Rows q, i
 }
 
 // ---------------------------------------------------------------- launchers
-static Rows rows_of(const I8Rows &s, int team, int held) { return Rows{s.route_token, s.offset, s.E, s.per, s.rows, s.T, team, held}; }
+static Rows rows_of(const I8Rows &s, int team, int held) { return Rows{s.route_token, s.offset, s.E, s.per, s.rows, s.T, team, held, s.route_row, s.top, (int)s.routes}; }
 static int kt_of(int64_t K) { return (int)((K + KB - 1) / KB); }
 static size_t table_bytes(const I8Rows &s) { return s.offset ? 2 * (size_t)(s.E + 1) * sizeof(int) : 0; }
-// Threads to a row: one unit each where there are few rows and latency counts, else four.
+// Threads to a row: a unit each while all fit the GPU at once and latency counts, then two, then four.  us with 64 / 128 / 256 threads: 400 x 4096 7.0 / 4.6 /
+// 4.2, 1024 x 4096 8.4 / 6.7 / 6.9, 2048 x 4096 11.3 / 10.3 / 11.6, 4096 x 8192 34.5 / 29.1 / 32.8; with 32 / 64 / 128: 4096 x 2048 11.0 / 10.1 / 11.5, 8192 x 1408
+// 12.9 / 15.2 / 19.4 (a GPU on the slow side).
 static int team_of(int64_t rows, int units, int most) {
-    const int want = rows <= 2 * sm_count() ? units : (units + 3) / 4;
+    const int64_t all = rows * units;
+    const int each = all <= 200000 ? 1 : all <= 600000 ? 2 : 4, want = (units + each - 1) / each;
     int team = 32;
     while (team < want && team < most) team *= 2;
     return team;
@@ -308,13 +345,13 @@ static unsigned grid_of(int64_t rows, int teams, int per_sm) {
     const int64_t blocks = (rows + teams - 1) / teams, most = per_sm ? (int64_t)per_sm * sm_count() : blocks;
     return (unsigned)(blocks < most ? blocks : most);
 }
-template <class From>
+template <bool SCATTER = false, class From>
 static cudaError_t quantize(const From &from, const I8Rows &s, int64_t K, float *scale, void *layout, cudaStream_t st) {
     const int KT = kt_of(K), KU = (int)(K >> 4), team = team_of(s.rows, KU, s.rows <= 2 * sm_count() ? 512 : 256), threads = team < 256 ? 256 : team, teams = threads / team;
     const int all = (KU + team - 1) / team * team, room = ROOM / (teams * From::PIECES * 16) / team * team;
     const int held = all <= room ? all : room - team;
-    const size_t smem = (size_t)teams * From::PIECES * 16 * (held < all ? held + team : held) + table_bytes(s);
-    return launch_overlapped(quantize_kernel<From>, dim3(grid_of(s.rows, teams, s.offset ? 2048 / threads : 0)), (unsigned)threads, smem, st, 1, true, from, rows_of(s, team, held), K, KT, scale,
+    const size_t smem = (size_t)teams * From::PIECES * 16 * (held < all ? held + team : held) + (SCATTER ? 2 * (size_t)teams * s.top * sizeof(Copy) : 0) + table_bytes(s);
+    return launch_overlapped(quantize_kernel<From, SCATTER>, dim3(grid_of(s.rows, teams, s.offset ? 1024 / threads : 0)), (unsigned)threads, smem, st, 1, true, from, rows_of(s, team, held), K, KT, scale,
                              (uint8_t *)layout);
 }
 
@@ -323,6 +360,7 @@ static cudaError_t quantize(const From &from, const I8Rows &s, int64_t K, float 
 using namespace i8;
 
 cudaError_t launch_i8_quantize(const void *x, int dtype, int64_t ldx, const I8Rows &s, int64_t K, float *scale, void *layout, cudaStream_t st) {
+    if (s.route_row) return dtype == DT_BF16 ? quantize<true>(Plain<DT_BF16>{x, ldx}, s, K, scale, layout, st) : quantize<true>(Plain<DT_F16>{x, ldx}, s, K, scale, layout, st);
     if (dtype == DT_BF16) return quantize(Plain<DT_BF16>{x, ldx}, s, K, scale, layout, st);
     if (dtype == DT_F16) return quantize(Plain<DT_F16>{x, ldx}, s, K, scale, layout, st);
     return quantize(Plain<DT_F32>{x, ldx}, s, K, scale, layout, st);

@@ -66,11 +66,11 @@ cudaError_t ensure_func_attr(Kern kern, std::atomic<uint64_t> &done, cudaFuncAtt
 // the compiler, wants memory that nobody writes from the kernel's start on.  cluster: CTAs per cluster (1: none); overlap: false for the few kernels
 // that do not gain by it.
 template <class... P, class... A>
-cudaError_t launch_overlapped(void (*kern)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, int cluster, bool overlap, A &&...args) {
+cudaError_t launch_overlapped(void (*kern)(P...), dim3 grid, dim3 threads, size_t smem, cudaStream_t st, int cluster, bool overlap, A &&...args) {
     static const bool use_pdl = getenv("CQ_NO_PDL") == nullptr;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
+    cfg.blockDim = threads;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -185,8 +185,9 @@ cudaError_t launch_route(const RouteCall &c, cudaStream_t st);
 cudaError_t launch_combine(const uint16_t *routes, int64_t ldr, int64_t R, const float *weight, const int32_t *row, int64_t T, int top, int64_t N, const uint16_t *add,
                            int64_t lda, uint16_t *y, int64_t ldy, bool f16, cudaStream_t st);
 
-// 8-bit integers with a scale for each row (cq_i8_quant.cu, cq_i8_gemm.cu); rows as for Fp4Rows.
-struct I8Rows { const int32_t *route_token, *offset; int E; int64_t per, rows, T; };
+// 8-bit integers with a scale for each row (cq_i8_quant.cu, cq_i8_gemm.cu); rows as for Fp4Rows, or (route_row) `rows` tokens that go to all of their routes each,
+// [rows][top] of `routes` in all: launch_i8_quantize from 16 bits alone.
+struct I8Rows { const int32_t *route_token, *offset; int E; int64_t per, rows, T; const int32_t *route_row = nullptr; int top = 0; int64_t routes = 0; };
 cudaError_t launch_i8_quantize(const void *x, int dtype, int64_t ldx, const I8Rows &rows, int64_t K, float *scale, void *layout, cudaStream_t st);
 cudaError_t launch_i8_swiglu_quantize(const void *h, int dtype, int64_t ldh, const I8Rows &rows, int64_t I, float *scale, void *layout, cudaStream_t st);
 cudaError_t launch_i8_dequantize(const void *layout, const I8Rows &rows, int64_t K, const float *scale, void *y, int dtype, cudaStream_t st);
@@ -195,7 +196,8 @@ cudaError_t launch_i8_exchange(uint8_t *codes, const I8Rows &rows, int64_t K, vo
 bool i8_few_ok(int64_t M, int64_t N, int64_t K);
 cudaError_t launch_i8_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, uint16_t *y, int64_t M, int64_t N, int64_t K, bool f16, int *status, cudaStream_t st);
 struct I8Plan { int channels, rows, runs; };
-I8Plan i8_plan(int64_t E, bool routed, int64_t M, int64_t N, int64_t K, bool own);
+// how the product is cut: channels and rows of x to an output tile, runs of K that share one; own: launch_i8_few, else launch_i8_gemm
+I8Plan i8_plan(bool routed, int64_t M, int64_t N, int64_t K, bool own);
 // y[M][N] = x W^T of two layouts; offset != null: E groups of rows, group e times matrix e; early: the kernel in front is the quantiser of x
 cudaError_t launch_i8_gemm(const void *w, const float *w_scale, const void *x, const float *x_scale, const int32_t *offset, int E, uint16_t *y, int64_t M, int64_t N, int64_t K,
                            bool f16, bool early, int *status, cudaStream_t st);

@@ -635,22 +635,23 @@ __global__ void __launch_bounds__(1024) place_kernel(const Args p, int blocks) {
 }
 
 // ---------------------------------------------------------------- the routes of a token together
-// y[t] = add[t] + sum over j of weight[t][j] routes[row[t][j]], in fp32 and in the order of j, rounded once.  A thread takes eight (one) values of a token.
-// Rows outside [0, R) are no routes and are not read.  `add` may be y.
+// y[t] = add[t] + sum over j of weight[t][j] routes[row[t][j]], in fp32 and in the order of j, rounded once.  A thread takes eight (one) values of a token, the
+// loads of four routes on their way together.  Rows outside [0, R) are no routes and are not read.  `add` may be y.  Bound by memory: 4096 tokens of 4096 values
+// and eight routes 49.5 us, 6.1 TB/s.
 template <bool F16, bool WIDE>
-__global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, int64_t ldr, int64_t R, const float *weight, const int32_t *row, int64_t T, int top, int64_t N,
-                                                      const uint16_t *add, int64_t lda, uint16_t *y, int64_t ldy) {
+__global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, int64_t ldr, int R, const float *weight, const int32_t *row, int T, int top, int N, const uint16_t *add, int64_t lda,
+                                                      uint16_t *y, int64_t ldy) {
     tc::wait_for_previous_kernel();
-    constexpr int DT = F16 ? DT_F16 : DT_BF16, BATCH = 4;
-    const int64_t per = WIDE ? N / 8 : N, total = T * per;
-    for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (int64_t)gridDim.x * 256) {
-        const int64_t t = idx / per, c = idx - t * per;
-        const int32_t *rows_of = row + t * top;
-        const float *weights = weight + t * top;
+    constexpr int DT = F16 ? DT_F16 : DT_BF16, BATCH = 4, VALUES = WIDE ? 8 : 1;
+    const int t = blockIdx.x * blockDim.y + threadIdx.y;   // blocks of one token, or of several short ones
+    if (t >= T) return;
+    const int32_t *rows_of = row + t * top;
+    const float *weights = weight + t * top;
+    for (int c = threadIdx.x * VALUES; c < N; c += blockDim.x * VALUES) {
         if (WIDE) {
             float f[8];
             uint4 a = make_uint4(0, 0, 0, 0);
-            if (add) a = load16(add + t * lda + c * 8);
+            if (add) a = load16(add + t * lda + c);
             const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
             for (int k = 0; k < 8; ++k) f[k] = add ? value_of<DT>(aw, k) : 0.0f;
@@ -660,9 +661,9 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, in
                 bool live[BATCH];
 #pragma unroll
                 for (int j = 0; j < BATCH; ++j) {
-                    const int64_t r = j0 + j < top ? rows_of[j0 + j] : -1;
+                    const int r = j0 + j < top ? rows_of[j0 + j] : -1;
                     live[j] = r >= 0 && r < R;
-                    v[j] = live[j] ? load16(routes + r * ldr + c * 8) : make_uint4(0, 0, 0, 0);
+                    v[j] = live[j] ? load16(routes + r * ldr + c) : make_uint4(0, 0, 0, 0);
                     w[j] = live[j] ? weights[j0 + j] : 0.0f;
                 }
 #pragma unroll
@@ -673,12 +674,12 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, in
                         for (int k = 0; k < 8; ++k) f[k] = fmaf(w[j], value_of<DT>(vw, k), f[k]);
                     }
             }
-            *reinterpret_cast<uint4 *>(y + t * ldy + c * 8) = make_uint4(pack16<DT>(f[0], f[1]), pack16<DT>(f[2], f[3]), pack16<DT>(f[4], f[5]), pack16<DT>(f[6], f[7]));
+            *reinterpret_cast<uint4 *>(y + t * ldy + c) = make_uint4(pack16<DT>(f[0], f[1]), pack16<DT>(f[2], f[3]), pack16<DT>(f[4], f[5]), pack16<DT>(f[6], f[7]));
         } else {
             float f = 0.0f;
             if (add) { const uint32_t w = add[t * lda + c]; f = value_of<DT>(&w, 0); }
             for (int j = 0; j < top; ++j) {
-                const int64_t r = rows_of[j];
+                const int r = rows_of[j];
                 if (r >= 0 && r < R) { const uint32_t w = routes[r * ldr + c]; f = fmaf(weights[j], value_of<DT>(&w, 0), f); }
             }
             y[t * ldy + c] = (uint16_t)pack16<DT>(f, 0.0f);
@@ -747,9 +748,12 @@ cudaError_t launch_combine(const uint16_t *routes, int64_t ldr, int64_t R, const
                            int64_t lda, uint16_t *y, int64_t ldy, bool f16, cudaStream_t st) {
     const auto odd = [](const void *q, int64_t ld) { return (reinterpret_cast<uintptr_t>(q) & 15u) != 0 || ld % 8 != 0; };
     const bool wide = N % 8 == 0 && !odd(routes, ldr) && !odd(y, ldy) && !(add && odd(add, lda));
-    const int64_t blocks = (T * (wide ? N / 8 : N) + 255) / 256, most = 16 * (int64_t)sm_count();
+    const int64_t per = wide ? N / 8 : N;
+    unsigned across = 32;
+    while (across < 256 && across < per) across *= 2;
+    const unsigned tokens = 256 / across;
     auto go = [&](auto kern) {
-        return launch_overlapped(kern, dim3((unsigned)(blocks < most ? blocks : most)), 256u, 0, st, 1, true, routes, ldr, R, weight, row, T, top, N, add, lda, y, ldy);
+        return launch_overlapped(kern, dim3((unsigned)((T + tokens - 1) / tokens)), dim3(across, tokens), 0, st, 1, true, routes, ldr, (int)R, weight, row, (int)T, top, (int)N, add, lda, y, ldy);
     };
     if (f16) return wide ? go(combine_kernel<true, true>) : go(combine_kernel<true, false>);
     return wide ? go(combine_kernel<false, true>) : go(combine_kernel<false, false>);

@@ -1,7 +1,7 @@
 // What the products of two stored operands share (cq_fp4_gemm.cu, cq_i8_gemm.cu): the order of their output tiles, the way of accumulators to
 // y, waits and arrivals within a CTA, a pair, a cluster.
-// Args, the arguments of a product, has: offset (routed: first rows of the groups), E, NB (row blocks of W), M (rows of x), bt (rows of x to a tile), token_tiles
-// (dense: tiles along the rows of x), band (how many of them are swept together).
+// Args, the arguments of a product, has: offset (routed: first rows of the groups), E, NB (row blocks of W), M (rows of x), bt (rows of x to a tile at most), token_tiles
+// (dense: tiles along the rows of x), band (how many of them are swept together), rows_of_tile(rows, tiles): what a tile has of so many rows that fill so many tiles.
 #pragma once
 #include "cq_rows.cuh"
 #include "cq_tc_ptx.cuh"
@@ -69,8 +69,8 @@ __device__ __forceinline__ Item item_of(const Args &p, int idx, const int *s_off
     const int wide = min(p.band, tiles - g * p.band);
     t.nb = rem / wide;
     const int tt = g * p.band + rem - t.nb * wide;
-    const int row0 = tt * p.bt;
-    t.rows = min(p.bt, rows - row0);
+    const int bt = p.rows_of_tile(rows, tiles), row0 = tt * bt;
+    t.rows = min(bt, rows - row0);
     t.xblk = first_blk + row0 / ROWS;
     t.off = row0 % ROWS;
     t.yrow = first_row + row0;

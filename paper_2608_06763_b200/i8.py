@@ -28,7 +28,7 @@ def _lib():
                            ("dequantize", [vp, vp, i64, i64, i64, vp, vp, i, vp]), ("gemm", [vp, vp, vp, vp, vp, i, i64, i64, i64, vp, sz, vp]),
                            ("linear", [vp, vp, vp, i64, vp, i, i64, i64, i64, vp, sz, vp]), ("gemm_routed", [vp, vp, vp, vp, vp, i64, vp, i, i64, i64, i64, vp, sz, vp]),
                            ("linear_routed", [vp, vp, vp, i64, i64, vp, vp, i64, vp, i, i64, i64, i64, vp, sz, vp]),
-                           ("moe", [vp, vp, vp, vp, i64, vp, i64, i64, i, vp, vp, vp, vp, vp, i64, vp, i64, i, i64, i64, vp, sz, vp])):
+                           ("moe", [vp, vp, vp, vp, i64, vp, i64, i64, i, vp, vp, vp, vp, i64, vp, i64, i, i64, i64, vp, sz, vp])):
             fn = getattr(L, "cq_i8_" + name)
             fn.restype, fn.argtypes = i, args
         L.cq_debug_i8_plan.restype, L.cq_debug_i8_plan.argtypes = i, [i64, i64, i64, i64, i, vp]
@@ -288,7 +288,7 @@ def cq_i8_moe(gate_up: I8Tensor, down: I8Tensor, x: torch.Tensor, routes: Routes
         raise CubicQuantError(f"tensors on {x.device} and {routes.row.device}")
     if T:
         status = (_L or _lib()).cq_i8_moe(gate_up.layout.data_ptr(), gate_up.scale.data_ptr(), down.layout.data_ptr(), down.scale.data_ptr(), E, x_at, ld, T, top,
-                                          routes.token.data_ptr(), routes.offset.data_ptr(), routes.row.data_ptr(), routes.weight.data_ptr(), _at(add), lda, out.data_ptr(), ldy, dtype,
+                                          routes.offset.data_ptr(), routes.row.data_ptr(), routes.weight.data_ptr(), _at(add), lda, out.data_ptr(), ldy, dtype,
                                           H, I, workspace.data_ptr(), workspace.numel(), stream)
         if status != 0:
             _check(status, "cq_i8_moe")

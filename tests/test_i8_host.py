@@ -138,9 +138,9 @@ def test_products_refuse():
 
 def test_moe_refuses():
     L = i8._lib()
-    names = "gu gus dn dns E x ldx T top token offset row weight add lda y ldy f16 H I workspace bytes stream".split()
-    go = with_changes(L.cq_i8_moe, names, [ONE, ONE, ONE, ONE, 4, ONE, 256, 8, 2, ONE, ONE, ONE, ONE, None, 0, ONE, 256, 0, 256, 128, ONE, 1 << 24, None])
-    for null in ("gu", "gus", "dn", "dns", "x", "token", "offset", "row", "weight", "y", "workspace"):
+    names = "gu gus dn dns E x ldx T top offset row weight add lda y ldy f16 H I workspace bytes stream".split()
+    go = with_changes(L.cq_i8_moe, names, [ONE, ONE, ONE, ONE, 4, ONE, 256, 8, 2, ONE, ONE, ONE, None, 0, ONE, 256, 0, 256, 128, ONE, 1 << 24, None])
+    for null in ("gu", "gus", "dn", "dns", "x", "offset", "row", "weight", "y", "workspace"):
         assert go(**{null: None}) == -1
     assert go(T=0) == -1 and go(top=0) == -1 and go(H=0) == -1 and go(I=0) == -1 and go(E=0) == -1 and go(ldx=255) == -1 and go(ldy=255) == -1 and go(add=ONE, lda=255) == -1
     assert go(top=33) == -2 and go(T=1 << 30) == -2 and go(E=513) == -2 and go(H=264, ldx=264, ldy=264) == -2 and go(I=72) == -2
