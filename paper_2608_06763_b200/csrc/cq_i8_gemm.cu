@@ -54,9 +54,12 @@ template <int MODE, bool SPLIT>
 struct Shape {
     static constexpr bool PAIR = MODE == TWO;
     static constexpr int BN = MODE == TWO ? 256 : MODE == ONE ? 128 : MODE == SMALL ? 64 : FEW_ROWS, CTAS = PAIR ? 2 : 1;
-    static constexpr int A_BYTES = TILE_BYTES, B_BYTES = MODE == FEW ? 0 : BN / CTAS * 128;   // of a stage; codes of x in this CTA: half of a pair's
-    static constexpr int STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = MODE == FEW || (MODE == SMALL && !SPLIT) ? 8 : MODE == ONE && SPLIT ? 4 : 6;
+    // A stage of the ring has DEEP k tiles.  Up to 64 rows a k tile's MMAs are short, and waiting, fencing and committing for each takes longer than its copy: 240 ns,
+    // of which SMs whose weights come from L2 would need 150.
+    static constexpr int DEEP = MODE == FEW || MODE == SMALL ? 2 : 1;
+    static constexpr int B_TILE = MODE == FEW ? 0 : BN / CTAS * 128;   // codes of x in this CTA: half of a pair's
+    static constexpr int A_BYTES = DEEP * TILE_BYTES, B_BYTES = DEEP * B_TILE, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = MODE == FEW ? 4 : MODE == SMALL ? (SPLIT ? 3 : 4) : MODE == ONE && SPLIT ? 4 : 6;
     static constexpr int ACCS = 2, ACC_COLS = BN < 32 ? 32 : BN;   // accumulators: while one is read the next tile fills the other
     static constexpr int PITCH = 272;                              // bytes of a row of the staged output: 128 channels and a gap against bank conflicts
     static constexpr int X_CODES = FEW_ROWS * 128, X_BYTES = MODE == FEW ? FEW_TILES * X_CODES : 0;   // FEW: codes of a k tile; all k tiles
@@ -231,15 +234,21 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
         if (PAIR) tc::tmem_alloc_pair(s_tmem, 512);
         else { tc::tmem_alloc(s_tmem, 512); tc::tmem_relinquish(); }
     }
-    if (!p.offset && !p.early && threadIdx.x == 0 && unit < n_items) {   // the first weights on their way to L2, which sees what the kernel in front may still write
-        const int nb = min(item_of<PAIR>(p, unit, nullptr, nullptr, nullptr).nb * CTAS + half, p.NB - 1);
-        for (int kt = k0; kt < k1 && kt < k0 + ST; ++kt) tc::prefetch_l2(p.w + ((int64_t)nb * p.KT + kt) * TILE_BYTES, TILE_BYTES);
-    }
     tc::tc_fence_before();
     __syncthreads();
     if (PAIR) tc::cluster_sync();   // the partner's barriers exist before anything arrives on them
     if (SPLIT) cluster_arrive();
     tc::tc_fence_after();
+    Tiles<PAIR, GemmArgs> tiles{p, unit, SPLIT ? n_items : units, n_items, s_off, s_blk, s_item, {}};   // split: one tile
+    if (!p.offset) {   // what needs no other kernel: the first tiles' places, and the first weights on their way to L2, which sees what the kernel in front may still write
+        tiles.look(0);
+        tiles.ahead = true;
+        if (warp == 3 && !p.early && tiles.has(0)) {
+            const int nb = min(tiles.at(0).nb * CTAS + half, p.NB - 1);
+            if (lane < SH::STAGES * SH::DEEP && k0 + lane < k1) tc::prefetch_l2(p.w + ((int64_t)nb * p.KT + k0 + lane) * TILE_BYTES, TILE_BYTES);
+            __syncwarp();
+        }
+    }
     // From here on the next kernel may start: this one holds its tensor memory, which a kernel that waits for this one might else take.
     // Behind the quantiser of this call only the layout and the scales that it writes have to be waited for (by the warps that read them, and in every
     // CTA): the quantiser lets this kernel start once all kernels in front of itself have ended, those that wrote weights and offsets among them.
@@ -249,10 +258,8 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
         if (warp == 3) scan_groups(p.offset, p.E, p.M, s_off, s_blk, s_item, p.bt, PAIR ? (p.NB + 1) >> 1 : p.NB);
         __syncthreads();
     }
-    const int items = p.offset ? __reduce_max_sync(~0u, s_item[p.E]) : n_items;   // (a reduction's result is uniform)
-    const int stride = SPLIT ? items : units;   // split: one tile
+    if (p.offset) tiles.items = __reduce_max_sync(~0u, s_item[p.E]);   // (a reduction's result is uniform)
 
-    Tiles<PAIR, GemmArgs> tiles{p, unit, stride, items, s_off, s_blk, s_item, {}};
     int it = 0;   // stages filled (warps 0 and 2) so far
     if (warp == 0 || (warp == 2 && MODE != FEW)) {
         // warp 0 the weights, warp 2 its rows of codes, from one row block or two (a lane for each)
@@ -265,20 +272,26 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
             const int n = columns_of<PAIR>(t.rows), mine = n / CTAS, nb = min(t.nb * CTAS + half, p.NB - 1);   // an odd last pair reads a block twice
             const int r0 = t.off + half * mine, b0 = r0 / ROWS, in0 = r0 % ROWS, n0 = min(mine, ROWS - in0), n1 = mine - n0;
             const uint8_t *xt = p.x + ((int64_t)t.xblk * p.KT + k0) * TILE_BYTES, *src = xt;
-            uint32_t to = 0, bytes = 0, all = SH::A_BYTES;
+            // warp 0: one piece, neighbouring k tiles are neighbours in memory; warp 2: lanes 2 j and 2 j + 1 the rows of k tile j of a stage
+            const int mine_kt = warp == 0 ? 0 : lane >> 1;
+            uint32_t to = 0, bytes = 0, all = TILE_BYTES;
             if (warp == 0) {
-                if (lane == 0) { src = p.w + (((int64_t)t.e * p.NB + nb) * p.KT + k0) * TILE_BYTES; bytes = SH::A_BYTES; }
+                if (lane == 0) { src = p.w + (((int64_t)t.e * p.NB + nb) * p.KT + k0) * TILE_BYTES; bytes = TILE_BYTES; }
             } else {
                 all = (uint32_t)mine * 128;
-                if (lane == 0) { src = xt + b0 * block + in0 * 128; to = SH::A_BYTES; bytes = (uint32_t)n0 * 128; }
-                else if (lane == 1) { src = xt + (b0 + 1) * block; to = SH::A_BYTES + n0 * 128; bytes = (uint32_t)n1 * 128; }
+                if (mine_kt < SH::DEEP) {
+                    src = xt + (b0 + (lane & 1)) * block + (lane & 1 ? 0 : in0 * 128) + mine_kt * TILE_BYTES;
+                    to = SH::A_BYTES + mine_kt * SH::B_TILE + (lane & 1 ? n0 * 128 : 0);
+                    bytes = (uint32_t)(lane & 1 ? n1 : n0) * 128;
+                }
             }
-            for (int kt = k0; kt < k1; ++kt, ++it, src += TILE_BYTES) {
+            for (int kt = k0; kt < k1; kt += SH::DEEP, ++it, src += SH::DEEP * TILE_BYTES) {
+                const uint32_t count = min(SH::DEEP, k1 - kt);
                 ok = uniform_wait(&empty[s], phase, p.status, 61, dead);   // the first round passes at once
                 if (!ok) break;
-                if (lane == 0) tc::mbar_arrive_expect_tx(&full[s], all);
+                if (lane == 0) tc::mbar_arrive_expect_tx(&full[s], all * count);
                 __syncwarp();
-                if (bytes) tc::bulk_load(ring + s * SH::STAGE + to, src, bytes, &full[s]);
+                if (bytes && mine_kt < (int)count) tc::bulk_load(ring + s * SH::STAGE + to, src, warp == 0 ? bytes * count : bytes, &full[s]);
                 if (++s == ST) { s = 0; phase ^= 1; }
             }
         }
@@ -289,13 +302,12 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
         uint32_t s = 0, phase = 0;
         bool ok = MODE != FEW || uniform_wait(x_ready, 0, p.status, 67, dead);
         for (int local = 0; ok && tiles.has(local); ++local) {
-            const Item t = tiles.at(local);
-            const uint32_t n = MODE == FEW ? FEW_ROWS : __reduce_max_sync(~0u, columns_of<PAIR>(t.rows));
+            const uint32_t n = MODE == FEW ? FEW_ROWS : __reduce_max_sync(~0u, columns_of<PAIR>(tiles.at(local).rows));
             const int acc = local & (ACCS - 1);
             const uint32_t d = TMEM + acc * ACC_COLS, desc = idesc_of<PAIR>(n);
             if (half == 0 && local >= ACCS) ok = uniform_wait(&acc_empty[acc], (local / ACCS - 1) & 1, p.status, 63, dead);
             tc::tc_fence_after();
-            for (int kt = k0; kt < k1 && ok; ++kt) {
+            for (int kt = k0; kt < k1 && ok; kt += SH::DEEP) {
                 ok = uniform_wait(&full[s], phase, p.status, 64, dead);
                 if (!ok) break;
                 if (PAIR && half == 1) {
@@ -304,14 +316,16 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
                     tc::tc_fence_after();
                     const uint64_t da = tc::smem_desc_sw128(tc::smem_u32(ring) + s * SH::STAGE);
                     const uint64_t db = MODE == FEW ? tc::smem_desc_sw128(tc::smem_u32(x_codes) + (kt - k0) * SH::X_CODES) : da + SH::A_BYTES / 16;
-                    const int steps = p.steps - 4 * kt;
+                    constexpr int B_STEP = (MODE == FEW ? SH::X_CODES : SH::B_TILE) / 16;
+                    const int steps = p.steps - 4 * kt, most = 4 * (k1 - kt);
                     if (tc::elect_one()) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (j == 0 || j < steps) umma_i8<PAIR>(d, da + 2 * j, db + 2 * j, desc, j > 0 || kt > k0);
+                        for (int j = 0; j < 4 * SH::DEEP; ++j)
+                            if (j == 0 || (j < steps && (SH::DEEP == 1 || j < most)))
+                                umma_i8<PAIR>(d, da + j / 4 * (TILE_BYTES / 16) + 2 * (j % 4), db + j / 4 * B_STEP + 2 * (j % 4), desc, j > 0 || kt > k0);
                         if (PAIR) commit_to_pair(&empty[s], cluster_rank);
                         else tc::umma_commit(&empty[s]);
-                        if (kt == k1 - 1) {
+                        if (kt + SH::DEEP >= k1) {
                             if (PAIR) commit_to_pair(&acc_full[acc], cluster_rank);
                             else tc::umma_commit(&acc_full[acc]);
                         }

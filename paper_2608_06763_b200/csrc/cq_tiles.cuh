@@ -81,16 +81,19 @@ __device__ __forceinline__ Item item_of(const Args &p, int idx, const int *s_off
 template <bool PAIR, class Args>
 struct Tiles {
     const Args &p;
-    const int unit, stride, items;
+    const int unit, stride;
+    int items;
     const int *s_off, *s_blk, *s_item;
     Item mine;
+    bool ahead = false;   // `look` has been called for the first 32
     __device__ __forceinline__ bool has(int i) const { return unit + (int64_t)i * stride < items; }
+    __device__ __forceinline__ void look(int i) {
+        const int64_t idx = unit + (int64_t)(i + (int)(threadIdx.x & 31)) * stride;
+        if (idx < items) mine = item_of<PAIR>(p, (int)idx, s_off, s_blk, s_item);
+        __syncwarp();
+    }
     __device__ __forceinline__ Item at(int i) {   // i = 0, 1, 2 ..; the whole warp
-        if ((i & 31) == 0) {
-            const int64_t idx = unit + (int64_t)(i + (int)(threadIdx.x & 31)) * stride;
-            if (idx < items) mine = item_of<PAIR>(p, (int)idx, s_off, s_blk, s_item);
-            __syncwarp();
-        }
+        if ((i & 31) == 0 && !(i == 0 && ahead)) look(i);
         Item t;
         const int packed = __shfl_sync(~0u, mine.rows << 8 | mine.off, i & 31);
         t.e = __shfl_sync(~0u, mine.e, i & 31);
