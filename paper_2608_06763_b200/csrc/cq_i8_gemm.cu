@@ -5,6 +5,8 @@
 #include "cq_tc_ptx.cuh"
 #include "cq_tiles.cuh"
 
+#include <algorithm>
+
 namespace cq {
 namespace i8 {
 
@@ -54,12 +56,12 @@ template <int MODE, bool SPLIT>
 struct Shape {
     static constexpr bool PAIR = MODE == TWO;
     static constexpr int BN = MODE == TWO ? 256 : MODE == ONE ? 128 : MODE == SMALL ? 64 : FEW_ROWS, CTAS = PAIR ? 2 : 1;
-    // A stage of the ring has DEEP k tiles.  Up to 64 rows a k tile's MMAs are short, and waiting, fencing and committing for each takes longer than its copy: 240 ns,
-    // of which SMs whose weights come from L2 would need 150.
-    static constexpr int DEEP = MODE == FEW || MODE == SMALL ? 2 : 1;
+    // A stage of the ring has DEEP k tiles.  Waiting, fencing and committing for each k tile takes 240 ns, more than its MMAs or its copy from L2 (150 for 64 rows).  With two
+    // to a stage 512 rows of 4096 x 4096 take 10.5 us as ONE instead of 11.9; a pair's copies take longer than that, and a deeper ring of single tiles serves it better.
+    static constexpr int DEEP = PAIR ? 1 : 2;
     static constexpr int B_TILE = MODE == FEW ? 0 : BN / CTAS * 128;   // codes of x in this CTA: half of a pair's
     static constexpr int A_BYTES = DEEP * TILE_BYTES, B_BYTES = DEEP * B_TILE, STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = MODE == FEW ? 4 : MODE == SMALL ? (SPLIT ? 3 : 4) : MODE == ONE && SPLIT ? 4 : 6;
+    static constexpr int STAGES = PAIR ? 6 : MODE == ONE ? (SPLIT ? 2 : 3) : MODE == SMALL && SPLIT ? 3 : 4;
     static constexpr int ACCS = 2, ACC_COLS = BN < 32 ? 32 : BN;   // accumulators: while one is read the next tile fills the other
     static constexpr int PITCH = 272;                              // bytes of a row of the staged output: 128 channels and a gap against bank conflicts
     static constexpr int X_CODES = FEW_ROWS * 128, X_BYTES = MODE == FEW ? FEW_TILES * X_CODES : 0;   // FEW: codes of a k tile; all k tiles
@@ -481,14 +483,14 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
 }
 
 // What computes a product of more than sixteen rows: kind of tile, rows to a tile, runs of k (log2).  Costs in microseconds, from tiles forced in turn.  A k
-// tile of one CTA takes as long as an SM's port to L2 does for its bytes (113 bytes a nanosecond); a pair's, its MMAs.  Cutting k saves k tiles and costs a
-// cluster's launch and the exchange.
-//   4096 x 4096, 17 rows: SMALL 10.0, in two runs 7.6, four 7.2;  64 rows: 10.7 / 8.8 / 8.1;  4096 x 14336, 64 rows: 29.7 / 17.7 / 12.8;  100 rows: ONE 31.7, two runs
-//   19.9, four 14.7, SMALL in two 18.5, TWO 26.5;  200 rows: ONE in two runs 21.0, whole 32.0, SMALL 30.2, TWO 26.5 to 32.2;  4096 x 4096, 200 rows: SMALL 11.1, ONE 12.0
-//   (two runs 11.1), TWO 10.9 to 13.0;  700 rows: TWO 18.0 / 13.4 / 15.5 with 128 / 192 / 256 rows, ONE 21.2;  6144 x 4096, 1024 rows: TWO 25.5 / 21.2 / 24.2, ONE 30.0
+// tile of one CTA takes as long as an SM's port to L2 does for its bytes (145 bytes a nanosecond); a pair's, its copies at least and for many rows its MMAs.  Cutting k saves
+// k tiles and costs a cluster's launch and the exchange.
+//   4096 x 4096, 200 rows: SMALL 8.9, ONE 10.0 (two runs 10.7), TWO 10.6;  300: SMALL 14.3, ONE 10.2, TWO 11.4;  512: ONE 10.5, TWO 11.7;  700: ONE 17.3, TWO 12.8
+//   4096 x 14336, 100 rows: SMALL 22.1, in two runs 15.1, ONE 24.6 / 18.7, in four 13.9, TWO 26.2;  200: SMALL 22.4, ONE 25.7, in two runs 20.6, TWO 26.6
+//   28672 x 4096, 40 rows: SMALL 20.8, TWO 22.8;  128: SMALL 28.7, ONE 24.8, TWO 25;  6144 x 4096, 1024 rows: ONE 24.9, TWO 20.3
 // Tried and dropped, sums through L2 where integers may be added in any order: even runs of all k tiles for each CTA (4096 x 4096, one row 11.0 us
-// instead of 7.8, 28672 x 4096 26 as before, 57344 x 8192 79.7 instead of 84.2), the last round's pairs cut along K (200 rows of 4096 x 14336 21.5, 1024 of 6144 x 4096
-// 28.8): an exchange there takes some four microseconds of fences, counting and reading back, and each run has two ends.
+// where whole tiles then took 7.8, 28672 x 4096 as before, 57344 x 8192 79.7 where they took 84.2), the last round's pairs cut along K (200 rows of 4096 x 14336 21.5, 1024 of
+// 6144 x 4096 28.8): an exchange there takes some four microseconds of fences, counting and reading back, and each run has two ends.
 struct Plan { int mode, bt, lg; };
 static Plan dense_plan(int64_t M, int NB, int KT) {
     static const Plan kinds[] = {{SMALL, 64, 0}, {SMALL, 64, 1}, {SMALL, 64, 2}, {ONE, 128, 0}, {ONE, 128, 1}, {ONE, 128, 2}, {TWO, 128, 0}, {TWO, 192, 0}, {TWO, 256, 0}};
@@ -502,9 +504,9 @@ static Plan dense_plan(int64_t M, int NB, int KT) {
         if (k.lg && items * S > places) continue;   // one round, or the runs of several tiles wait for one another's places
         const double n = M < k.bt ? (double)M : (double)k.bt, rounds = (double)((items * S + places - 1) / places);
         double per_kt, tail, base;
-        if (k.mode == TWO) { per_kt = 0.15 + 0.15 * n / 256; tail = 0.5 * n / 256; base = 3.2; }
+        if (k.mode == TWO) { per_kt = std::max(0.205, 0.13 + 0.15 * n / 256); tail = 0.5 * n / 256; base = 4.4; }
         else {
-            per_kt = (16.4 + 0.128 * n) / 113.0;
+            per_kt = (16.4 + 0.128 * n) / 145.0;
             tail = 0.5; base = 2.4 + (k.lg ? (k.mode == SMALL ? 3.0 : 4.5) : 0.0);
         }
         const double cost = base + rounds * ((KT + S - 1) / S * per_kt + tail);
@@ -512,10 +514,10 @@ static Plan dense_plan(int64_t M, int NB, int KT) {
     }
     return best;
 }
-// Up to sixteen rows.  A CTA's own quantising takes 0.3 us for each row of 4096, the launch in front of it is hidden but for the host's part, some two microseconds: us on
-// the GPU, by itself / in front: 4096 x 4096, rows 1 to 4: 8.1 / 7.8, 8.3 / 7.7, 8.6 / 8.0, 8.9 / 8.0, 8: 11.0 / 8.1;  8192 x 2048, 4: 8.3 / 7.8, 8: 9.8 / 7.9;  4096 x 14336, 1: 13.1 / 13.4, 2:
-// 15.0 / 13.4;  28672 x 4096, 1: 23.1 / 25.3, 4: 26.4 / 25.8.  FEW_MOST: rows x k tiles of 128.
-constexpr int FEW_MOST = 112;
+// Up to sixteen rows.  A CTA's own quantising takes 0.25 us for each row of 4096 (a call of its own in front is hidden but for the host's part, some two microseconds): us on the
+// GPU, by itself / in front: 4096 x 4096, rows 1 to 4: 7.1 / 7.0, 7.4 / 7.1, 7.6 / 7.2, 7.8 / 7.2, 6: 9.6 / 7.3;  8192 x 2048, 4: 7.3 / 7.1, 8: 9.5 / 7.6;  4096 x 14336, 1: 10.2 / 11.2, 2: 12.2 /
+// 11.4;  28672 x 4096, 1: 21.5 / 22.4, 3: 23.4 / 22.9.  FEW_MOST: rows x k tiles of 128.
+constexpr int FEW_MOST = 128;
 bool i8_few_ok(int64_t M, int64_t N, int64_t K) {
     if (M > FEW_ROWS) return false;
     const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
