@@ -341,7 +341,7 @@ enum { CQ_SOFTMAX = 0, CQ_SIGMOID = 1 };
  *   expert_offset [E + 1]: routes of expert e are rows [expert_offset[e], expert_offset[e + 1]); the last one is the number of routes, at most R
  *   route_token [R]: the tokens of the routes, grouped by expert, ascending within each; -1 from the last offset on
  *   route_row [T][top]: the row of each choice among the routes; -1 for none
- * The outputs do not depend on timing.  One launch up to 128 tokens, two beyond.
+ * The outputs do not depend on timing.  One launch up to 16 tokens, two beyond.
  * Errors: CQ_ERR_INVALID_ARG (also: E not a multiple of groups, top beyond the experts of the kept groups), CQ_ERR_UNSUPPORTED (E > 512,
  * groups > 32, top > 32, T top > 2^30). */
 size_t cq_route_workspace_bytes(int64_t T, int64_t E);

@@ -34,7 +34,6 @@ __device__ __forceinline__ uint32_t ordered(float v) {
     const uint32_t b = __float_as_uint(v);
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 __device__ __forceinline__ uint64_t ordered(double v) {
     const uint64_t b = (uint64_t)__double_as_longlong(v);
     return b ^ ((uint64_t)((int64_t)b >> 63) | 0x8000000000000000ull);
@@ -46,6 +45,11 @@ __device__ __forceinline__ uint64_t warp_max(uint64_t v) {
         if (u > v) v = u;
     }
     return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -95,7 +99,13 @@ __device__ __forceinline__ void best_two_of_group(const Args &p, F &first, F &se
 
 // What a warp puts its candidates into, in ascending order of experts, and the best of them in order.
 constexpr int CANDIDATES = 32;
-struct Candidates { uint32_t key[CANDIDATES], expert[CANDIDATES], best[CANDIDATES]; float logit[CANDIDATES]; double score[CANDIDATES]; };
+struct Candidates { float key[CANDIDATES]; uint32_t expert[CANDIDATES], best[CANDIDATES]; float logit[CANDIDATES]; double score[CANDIDATES]; };
+// Where a value reaches the limit: it and its expert to the next place of `key` and `expert`, and a place further.
+__device__ __forceinline__ void put(uint32_t &at, float key, float limit, uint32_t expert) {
+    static_assert(CANDIDATES * 4 == 128, "from key to expert");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ge.f32 p, %1, %2;\n\t@p st.shared.f32 [%0], %1;\n\t@p st.shared.u32 [%0 + 128], %3;\n\t@p add.u32 %0, %0, 4;\n\t}"
+                 : "+r"(at) : "f"(key), "f"(limit), "r"(expert) : "memory");
+}
 
 // Choice scores in 64 bits, -inf of what may not be chosen; top: the row's largest logit.  The whole warp.
 template <int V, int DT>
@@ -242,7 +252,7 @@ __device__ __forceinline__ float reciprocal_approx(float v) { float r; asm("rcp.
 //
 // The best: the (top + 1)-th largest of the lanes' largest is not above the (top + 1)-th largest of all, so what reaches it are candidates; hardly
 // more than that many, since few lanes have two.  Each finds its place by counting those in front of it.  Many equals, or a large
-// `top`, leave more candidates than there is room for: then the largest is taken out time and again.  8192 tokens to 8 of 256: 36 us with the latter alone.
+// `top`, leave more candidates than there is room for: then the largest is taken out time and again.  8192 tokens to 8 of 256: 20 us, 36 with the latter alone.
 // The logits of one lane as they are stored.  WIDE: `each` is V, and the rows allow wide loads.
 template <int V, int DT, bool WIDE>
 struct Raw {
@@ -280,41 +290,48 @@ struct Raw {
 };
 
 template <int V, int DT, bool WIDE>
-__device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT, WIDE> &raw, const Mine &m, const float *bias, Candidates &s, float &weight) {
+__device__ __forceinline__ int choose(const Args &p, int64_t t, const Mine &m, const float *bias, Candidates &s, float &weight) {
     const int lane = threadIdx.x & 31;
-    constexpr float U = 5.9604645e-8f, LOG2E = 1.44269504f;
-    float l[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) l[i] = raw.logit(i);
-    float top = l[0];
-#pragma unroll
-    for (int i = 1; i < V; ++i) top = fmaxf(top, l[i]);
-    top = unordered(__reduce_max_sync(~0u, ordered(top)));
-    weight = 0.0f;
-    if (top == -CUDART_INF_F) return -1;
-
+    constexpr float U = 5.9604645e-8f, LOG2E = 1.44269504f, LEAST = -3.402823466e38f;
+    const float NONE = -CUDART_INF_F;   // not to be chosen; LEAST: the least of those that may be
     const bool scores = bias || p.groups > 1;
-    float sum = 1.0f, rest = 0.0f;   // rest: how far two choice scores may be off, but for the part that grows with them
-    uint32_t key[V];
-    bool stays = true;
-    if (scores || (!p.sigmoid && !p.renormalise)) {
+    float l[V], key[V], top, sum, rest;   // rest: how far two choice scores may be off, but for the part that grows with them
+    bool stays;
+    // Once; a second time where 32 bits left the groups open (whatever the first time had in registers need not outlive the call that decides).
+    for (uint32_t decided = 0;;) {   // lanes whose groups stay
+        {
+            Raw<V, DT, WIDE> raw;
+            raw.load(p, t, m);
+#pragma unroll
+            for (int i = 0; i < V; ++i) l[i] = raw.logit(i);
+        }
+        top = l[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) top = fmaxf(top, l[i]);
+        top = warp_max(top);
+        weight = 0.0f;
+        if (top == NONE) return -1;
+
+        sum = 1.0f; rest = 0.0f;
+        stays = true;
         float c[V];
-        if (p.sigmoid) {
+        if (scores || (!p.sigmoid && !p.renormalise)) {
+            if (p.sigmoid) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) c[i] = reciprocal_approx(1.0f + exp2_approx(-LOG2E * l[i]));
-            rest = 16.0f * U;
-        } else {
-            sum = 0.0f;
+                for (int i = 0; i < V; ++i) c[i] = reciprocal_approx(1.0f + exp2_approx(-LOG2E * l[i]));
+                rest = 16.0f * U;
+            } else {
+                sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) { c[i] = exp2_approx(LOG2E * (l[i] - top)); sum += c[i]; }
-            sum = warp_sum(sum);
-            const float part = reciprocal_approx(sum);
+                for (int i = 0; i < V; ++i) { c[i] = exp2_approx(LOG2E * (l[i] - top)); sum += c[i]; }
+                sum = warp_sum(sum);
+                const float part = reciprocal_approx(sum);
 #pragma unroll
-            for (int i = 0; i < V; ++i) c[i] *= part;
-            rest = 160.0f * U;
+                for (int i = 0; i < V; ++i) c[i] *= part;
+                rest = 160.0f * U;
+            }
         }
         if (scores) {
-            float first = -CUDART_INF_F, second = -CUDART_INF_F;
             if (bias) {   // has V values behind the last
                 const float *mine = bias + m.first;
                 if constexpr (WIDE && V % 4 == 0) {
@@ -329,92 +346,84 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT,
                 }
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                c[i] = l[i] > -CUDART_INF_F ? c[i] : -CUDART_INF_F;
-                second = fmaxf(second, fminf(first, c[i]));
-                first = fmaxf(first, c[i]);
-            }
-            if (p.groups > 1) {
+            for (int i = 0; i < V; ++i) c[i] = l[i] > NONE ? c[i] : NONE;
+            if (p.groups > 1 && decided) {
+                stays = decided >> lane & 1;
+            } else if (p.groups > 1) {
+                float first = NONE, second = NONE;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    second = fmaxf(second, fminf(first, c[i]));
+                    first = fmaxf(first, c[i]);
+                }
                 const float a = fabsf(first), b = fabsf(second);
-                const float large = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(fmaxf(a < CUDART_INF_F ? a : 0.0f, b < CUDART_INF_F ? b : 0.0f))));
+                const float large = warp_max(fmaxf(a < CUDART_INF_F ? a : 0.0f, b < CUDART_INF_F ? b : 0.0f));
                 best_two_of_group<float>(p, first, second);
-                const float total = p.best == 2 && second > -CUDART_INF_F ? first + second : first;
-                uint32_t left = lane < p.groups << p.lg_lanes && total > -CUDART_INF_F ? ordered(total) : 0u, least = 0;
+                const float total = p.best == 2 ? 0.5f * first + (second > NONE ? 0.5f * second : 0.0f) : first;   // halves: the sum of two lowest numbers is none
+                float left = lane < p.groups << p.lg_lanes ? total : NONE, least = NONE;
                 stays = false;
                 for (int g = 0; g < p.kept; ++g) {   // the best of those that are left; of equals the first
-                    const uint32_t k = __reduce_max_sync(~0u, left);
-                    if (k == 0) break;
+                    const float k = warp_max(left);
+                    if (k == NONE) break;
                     least = k;
                     const int from = __ffs(__ballot_sync(~0u, left == k)) - 1;
-                    if ((uint32_t)(lane - from) < 1u << p.lg_lanes) { stays = true; left = 0; }
+                    if ((uint32_t)(lane - from) < 1u << p.lg_lanes) { stays = true; left = NONE; }
                 }
-                // Each of four choice scores is off by |c| / 2 more, their sums by as much again: 8 |c|.  What stays has to be that far above what does not.
-                const uint32_t most = __reduce_max_sync(~0u, left);
-                if (most != 0 && !(unordered(least) - unordered(most) > 2.0f * rest + 8.0f * U * large)) {
-                    const float near = (p.best == 2 && second > -CUDART_INF_F ? second : first) - rest - 4.0f * U * large;
+                // Each of two choice scores, or of four halves, is off by |c| / 2 more, their sums by as much again.  What stays has to be that far above what does not.
+                const float most = warp_max(left);
+                if (most > NONE && !(least - most > rest + 4.0f * U * large)) {
+                    const float near = fmaxf((p.best == 2 && second > NONE ? second : first) - rest - 4.0f * U * large, LEAST);
                     int count = 0;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) count += c[i] > -CUDART_INF_F && c[i] >= near;
-                    int at = sum_up(count);
-                    const int all = __shfl_sync(~0u, at, 31);
+                    for (int i = 0; i < V; ++i) count += c[i] >= near;
+                    const int behind = sum_up(count), all = __shfl_sync(~0u, behind, 31);
                     if (all <= CANDIDATES) {
-                        at -= count;
+                        uint32_t at = tc::smem_u32(&s.key[behind - count]);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) if (c[i] > -CUDART_INF_F && c[i] >= near) s.expert[at++] = m.first + i;
+                        for (int i = 0; i < V; ++i) put(at, c[i], near, m.first + i);
                         __syncwarp();
                         stays = group_stays_by_candidates<V, DT>(p, t, top, all, s);
                     } else {
                         stays = group_stays_in_64_bits<V, DT>(p, t, top);
                     }
+                    decided = __ballot_sync(~0u, stays);
+                    continue;
                 }
             }
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = stays && c[i] > -CUDART_INF_F && l[i] > -CUDART_INF_F ? ordered(bias ? c[i] + 0.0f : l[i]) : 0u;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = l[i] > -CUDART_INF_F ? ordered(l[i]) : 0u;
+        for (int i = 0; i < V; ++i) key[i] = !stays ? NONE : bias ? c[i] : l[i];
+        break;
     }
 
     const int rounds = bias ? min(p.top + 1, 32) : p.top;   // one more, to see how far it is from the last
     int chosen = -1, count = 0;
-    uint32_t got = 0, best = 0;   // lane j: the key of the j-th; the best key that this lane still has
-    float logit = 0.0f;
+    float got = NONE, best = key[0], limit = NONE, logit = 0.0f;   // lane j: the key of the j-th; the best key that this lane still has
 #pragma unroll
-    for (int i = 0; i < V; ++i) best = max(best, key[i]);
-    uint32_t limit = 0;
+    for (int i = 1; i < V; ++i) best = fmaxf(best, key[i]);
     {
-        uint32_t left = best;
+        float left = best;
 #pragma unroll 4
         for (int j = 0; j < rounds; ++j) {
-            limit = __reduce_max_sync(~0u, left);
-            if (left == limit) left = 0;
+            limit = warp_max(left);
+            if (left == limit) left = NONE;
         }
-        limit = max(limit, 1u);   // fewer lanes than that have any
-        if (bias && limit > 1u) {   // and what may belong in front of the last
-            const float least = unordered(limit);
-            limit = max(ordered(least - 2.0f * rest - 8.0f * U * fabsf(least)), 1u);
-        }
+        if (bias) limit -= 2.0f * rest + 8.0f * U * fabsf(limit);   // and what may belong in front of the last
+        limit = fmaxf(limit, LEAST);   // fewer lanes than that have any
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) count += key[i] >= limit;
-    int at = sum_up(count);
-    const int all = __shfl_sync(~0u, at, 31);
+    const int behind = sum_up(count), all = __shfl_sync(~0u, behind, 31);
     if (all <= CANDIDATES) {
-        at -= count;
+        uint32_t at = tc::smem_u32(&s.key[behind - count]);
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (key[i] >= limit) {
-                s.key[at] = key[i];
-                s.expert[at] = m.first + i;
-                ++at;
-            }
-        if (lane < 3 && all + lane < CANDIDATES) s.key[all + lane] = 0;
+        for (int i = 0; i < V; ++i) put(at, key[i], limit, m.first + i);
+        if (lane < 3 && all + lane < CANDIDATES) s.key[all + lane] = NONE;
         __syncwarp();
-        const uint32_t mine = lane < all ? s.key[lane] : 0u;
-        int ahead = __popc(__match_any_sync(~0u, mine) & ((1u << lane) - 1u));   // of equals those in front: lower experts
+        const float mine = lane < all ? s.key[lane] : NONE;
+        int ahead = __popc(__match_any_sync(~0u, __float_as_uint(mine)) & ((1u << lane) - 1u));   // of equals those in front: lower experts
         for (int j = 0; j < all; j += 4) {   // what lies behind the last is not larger
-            const uint4 k = *reinterpret_cast<const uint4 *>(&s.key[j]);
+            const float4 k = *reinterpret_cast<const float4 *>(&s.key[j]);
             ahead += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
         }
         if (lane < all) s.best[ahead] = lane;
@@ -422,12 +431,12 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT,
         if (lane < min(all, rounds)) {
             const uint32_t from = s.best[lane];
             chosen = s.expert[from]; got = s.key[from];
-            logit = bias ? clean(one_logit<DT>(p.logits, t * p.ldl + chosen)) : unordered(got);
+            logit = bias ? clean(one_logit<DT>(p.logits, t * p.ldl + chosen)) : got;
         }
     } else {
         for (int j = 0; j < rounds; ++j) {
-            const uint32_t k = __reduce_max_sync(~0u, best);
-            if (k == 0) break;
+            const float k = warp_max(best);
+            if (k == NONE) break;
             const int from = __ffs(__ballot_sync(~0u, best == k)) - 1;
             int which = 0;
             float lv = 0.0f;
@@ -437,11 +446,11 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT,
             lv = __shfl_sync(~0u, lv, from);
             if (lane == j) { chosen = e; got = k; logit = lv; }
             if (lane == from) {
-                best = 0;
+                best = NONE;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    if (i == which) key[i] = 0;
-                    best = max(best, key[i]);
+                    if (i == which) key[i] = NONE;
+                    best = fmaxf(best, key[i]);
                 }
             }
         }
@@ -450,12 +459,11 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT,
     if (bias) {
         // equal logits with equal biases are equal, and the lower index is first
         const int next = __shfl_down_sync(~0u, chosen, 1);
-        const uint32_t after = __shfl_down_sync(~0u, got, 1);
+        const float after = __shfl_down_sync(~0u, got, 1);
         const float l1 = __shfl_down_sync(~0u, logit, 1);
         if (lane + 1 < rounds && chosen >= 0 && next >= 0) {
-            const float a = unordered(got), b = unordered(after);
             const bool equal = logit == l1 && bias[chosen] == bias[next];
-            open |= !equal && !(a - b > rest + 4.0f * U * fmaxf(fabsf(a), fabsf(b)));
+            open |= !equal && !(got - after > rest + 4.0f * U * fmaxf(fabsf(got), fabsf(after)));
         }
         if (rounds == p.top) open |= all > p.top;   // of 32 wanted ones the last has nobody behind it to be compared with
     }
@@ -473,7 +481,7 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT,
     if (!there) chosen = -1;
     // weights: over the sum of the chosen they do not depend on a common factor, so the largest logit is taken out where scores would vanish
     if (p.renormalise) {
-        float large = unordered(__reduce_max_sync(~0u, there ? ordered(logit) : 0u));
+        float large = warp_max(there ? logit : NONE);
         float w = 0.0f;
         if (p.sigmoid) {
             large = fminf(large, 0.0f);
@@ -495,7 +503,8 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Raw<V, DT,
 // count.  Nothing depends on the order in which warps come.  The places among all blocks' routes are added by place_kernel, or, where one block has
 // all tokens, at once.
 constexpr int CHUNK = 128, PLACED = 2;   // PLACED: blocks of tokens whose routes one block of place_kernel places
-constexpr int threads_for(int V) { return V <= 4 ? 1024 : V == 8 ? 768 : 512; }   // at least as many as there are experts
+// At least as many as there are experts.  More warps hide more of a token's 3 us, until registers get short: 256 experts, 8192 / 65536 tokens with 768 threads 21.5 / 94, 896 20.4 / 92.
+constexpr int threads_for(int V) { return V <= 4 ? 1024 : V == 8 ? 896 : 512; }
 static_assert(CHUNK % 32 == 0 && MAX_EXPERTS <= 512, "words of bits; a thread for each expert");
 
 // Thread e's `count` routes: how many the experts in front have.  The whole block, at least E threads of it; all: of all experts; `sums`: 16 words of shared memory.
@@ -533,10 +542,8 @@ __global__ void __launch_bounds__(threads_for(V)) route_kernel(const Args p) {
         const int n = min(CHUNK, to - t0);
         for (int i = warp; i < n; i += WARPS) {
             const int t = t0 + i;
-            Raw<V, DT, WIDE> raw;
-            raw.load(p, t, m);
             float weight;
-            const int e = choose<V, DT, WIDE>(p, t, raw, m, p.bias ? s_bias : nullptr, s_candidates[warp], weight);
+            const int e = choose<V, DT, WIDE>(p, t, m, p.bias ? s_bias : nullptr, s_candidates[warp], weight);
             if (lane < p.top) {
                 p.expert[t * p.top + lane] = e;
                 p.weight[t * p.top + lane] = weight;

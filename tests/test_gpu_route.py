@@ -89,6 +89,29 @@ def test_groups(T, E, top, groups, kept, best, score, with_bias):
         both(l, top, score, some_bias(E, T) if with_bias else None, groups=groups, kept=kept, best=best)
 
 
+@pytest.mark.parametrize("best", [1, 2])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_groups_of_which_one_or_none_is_left(score, best):
+    r = np.random.default_rng(3)
+    l = some_logits(400, 48, "f32", 11)
+    l[torch.from_numpy(r.random((400, 48)) < np.linspace(0.3, 1.0, 400)[:, None])] = float("-inf")
+    for bias in (None, some_bias(48, 3, 0.5)):
+        both(l, 6, score, bias, groups=12, kept=5, best=best)
+
+
+@pytest.mark.parametrize("E,top,groups,kept", [(64, 8, 1, 1), (64, 6, 8, 3), (512, 32, 1, 1), (256, 30, 8, 4)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_lowest_and_infinite_biases(score, E, top, groups, kept):
+    """The type's lowest value is a bias like any other, and so is infinity: experts with it go by their logits."""
+    l = some_logits(70, E, "f32", E + top)
+    least, most = torch.finfo(torch.float32).min, float("inf")
+    for value in (least, most):
+        for share in (0.05, 0.5, 0.97, 1.0):
+            b = some_bias(E, int(100 * share))
+            b[torch.from_numpy(np.random.default_rng(E).random(E) < share)] = value
+            both(l, top, score, b, groups=groups, kept=kept)
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_scores_closer_than_32_bits_tell(score):
     """Biases that bring all choice scores of a row within a few units of fp32: decided in 64 bits."""
