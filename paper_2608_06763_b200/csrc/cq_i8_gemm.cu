@@ -123,26 +123,37 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
     if (COPY) cluster_arrive();   // what was copied from here has been received when all have arrived
     if (!ok) return;
     uint16_t *out = p.y + (int64_t)t.yrow * p.N + ch;
-    for (int r = (tid >> (lgCW - 1)) * 4; r < t.rows; r += (512 >> lgCW) * 4) {
-        int f[2][4] = {};
-        for (int s = 0; s < 1 << lgS; ++s) {
-            const uint8_t *from = COPY && s == run ? ring + s * bytes_of_run : part + s * bytes_of_run;
+    const uint8_t *own = (COPY ? ring : part) + run * bytes_of_run;
+    const int step = (512 >> lgCW) * 4;
+    for (int r = (tid >> (lgCW - 1)) * 4; r < t.rows; r += step) {
+        const int at = (mine * pitch + r) * 4, next = pitch * 4;
+        int4 f[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int4 v = *reinterpret_cast<const int4 *>(from + ((mine + j) * pitch + r) * 4);
-                f[j][0] += v.x; f[j][1] += v.y; f[j][2] += v.z; f[j][3] += v.w;
+        for (int j = 0; j < 2; ++j) f[j] = *reinterpret_cast<const int4 *>(own + at + j * next);
+#pragma unroll
+        for (int s = 1; s < 4; ++s)
+            if (s < 1 << lgS) {
+                const uint8_t *from = part + (run ^ s) * bytes_of_run + at;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int4 v = *reinterpret_cast<const int4 *>(from + j * next);
+                    f[j].x += v.x; f[j].y += v.y; f[j].z += v.z; f[j].w += v.w;
+                }
             }
-        }
+        const float4 xs = *reinterpret_cast<const float4 *>(x_scale + r);   // of what lies behind the rows nothing is stored
+        const float x4[4] = {xs.x, xs.y, xs.z, xs.w};
+        const int lo[4] = {f[0].x, f[0].y, f[0].z, f[0].w}, hi[4] = {f[1].x, f[1].y, f[1].z, f[1].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (r + i >= t.rows) break;
-            const float xs = x_scale[r + i];
-            const uint16_t a = round_out(value_of_sum(f[0][i], w0 * xs), p.f16), b = round_out(value_of_sum(f[1][i], w1 * xs), p.f16);
-            uint16_t *at = out + (int64_t)(r + i) * p.N;
-            if (p.wide && ch < p.N) *reinterpret_cast<uint32_t *>(at) = a | (uint32_t)b << 16;   // N even: both are inside
-            else {
-                if (ch < p.N) at[0] = a;
-                if (ch + 1 < p.N) at[1] = b;
+            const uint32_t v = pack_out(lo[i], hi[i], w0 * x4[i], w1 * x4[i], p.f16);
+            uint16_t *to = out + (int64_t)(r + i) * p.N;
+            if (r + i < t.rows) {
+                if (p.wide) {   // N even: both are inside
+                    if (ch < p.N) *reinterpret_cast<uint32_t *>(to) = v;
+                } else {
+                    if (ch < p.N) to[0] = (uint16_t)v;
+                    if (ch + 1 < p.N) to[1] = (uint16_t)(v >> 16);
+                }
             }
         }
     }
