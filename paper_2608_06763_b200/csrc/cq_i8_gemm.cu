@@ -498,6 +498,7 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
 // k tiles and costs a cluster's launch and the exchange.
 //   4096 x 4096, 200 rows: SMALL 8.9, ONE 10.0 (two runs 10.7), TWO 10.6;  300: SMALL 14.3, ONE 10.2, TWO 11.4;  512: ONE 10.5, TWO 11.7;  700: ONE 17.3, TWO 12.8
 //   4096 x 14336, 100 rows: SMALL 22.1, in two runs 15.1, ONE 24.6 / 18.7, in four 13.9, TWO 26.2;  200: SMALL 22.4, ONE 25.7, in two runs 20.6, TWO 26.6
+//   11176 x 22368, 341 rows: SMALL 124, ONE 88.6, TWO 84.0 / 96.2 / 113.6 with 128 / 192 / 256 rows;  925 x 12800, 1120 rows: ONE 26.1, in two runs 19.3, TWO 26.8
 //   28672 x 4096, 40 rows: SMALL 20.8, TWO 22.8;  128: SMALL 28.7, ONE 24.8, TWO 25;  6144 x 4096, 1024 rows: ONE 24.9, TWO 20.3
 // Tried and dropped, sums through L2 where integers may be added in any order: even runs of all k tiles for each CTA (4096 x 4096, one row 11.0 us
 // where whole tiles then took 7.8, 28672 x 4096 as before, 57344 x 8192 79.7 where they took 84.2), the last round's pairs cut along K (200 rows of 4096 x 14336 21.5, 1024 of

@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paper_2608_06763_b200 as cq
+from i8_shapes import PRODUCTS, ROUTED
 from oracle import i8 as ref
 from oracle import route as ref_route
 
@@ -263,6 +264,30 @@ def test_gemm_routed(counts, dtype):
     assert np.array_equal(cq.cq_i8_dequantize(q, torch.float32).cpu().numpy(), values[token.cpu().numpy()])
 
 
+@pytest.mark.parametrize("plan,M,N,K", PRODUCTS)
+def test_every_kind_of_tile(plan, M, N, K):
+    """bfloat16 and binary16 in turn; from rows in the model dtype and from quantised ones, which have the same bits."""
+    assert tuple(cq.cq_debug_i8_plan(M, N, K).values()) == plan
+    w, x, y, y32 = product_case(M, N, K, "bf16" if M % 2 else "f16", seed=M)
+    ws = cq.cq_i8_workspace(w, M)
+    got = cq.cq_i8_gemm(w, x, workspace=ws)
+    check_product(got, y, y32)
+    out = torch.full_like(got, 7.0)
+    assert torch.equal(cq.cq_i8_gemm(w, cq.cq_i8_quantize(x), workspace=ws, out=out), got)
+    assert cq.cq_gemm_status(ws) == 0
+
+
+@pytest.mark.parametrize("counts,N,K", ROUTED)
+def test_every_kind_of_routed_tile(counts, N, K):
+    w, x, token, off, y, y32 = routed_case(counts, N, K, "bf16" if N % 2 else "f16", seed=N, T=150)
+    ws = cq.cq_i8_workspace(w, sum(counts))
+    got = cq.cq_i8_gemm_routed(w, x, token, off, workspace=ws)
+    check_product(got, y, y32)
+    q = cq.cq_i8_quantize(x, route_token=token, expert_offset=off)
+    assert torch.equal(cq.cq_i8_gemm_routed(w, q, None, off, workspace=ws, out=torch.full_like(got, 7.0)), got)
+    assert cq.cq_gemm_status(ws) == 0
+
+
 def repaired(offset, R):
     """Offsets as the calls take them: the largest so far, within [0, R]."""
     return np.maximum.accumulate(np.clip(offset, 0, R))
@@ -493,6 +518,67 @@ def test_expert_block_from_logits(T, dtype):
         yr = cq.cq_i8_gemm_routed(wd, a, None, routes.offset, out=torch.empty((T * top, H), dtype=x.dtype, device="cuda"))
         assert torch.equal(cq.cq_combine(yr, routes, add=shared), y)
         assert torch.equal(cq.cq_i8_moe(wu, wd, x, routes, add=shared), y)
+    assert cq.cq_gemm_status(ws) == 0
+
+
+@pytest.mark.parametrize("T,E,top,H,I", [(1, 1, 1, 16, 16), (5, 512, 32, 48, 80), (64, 512, 1, 144, 16), (33, 60, 4, 272, 336), (700, 3, 2, 1040, 144), (300, 2, 2, 16, 1296)])
+def test_expert_block_of_odd_sizes(T, E, top, H, I):
+    """Most matrices without rows, one matrix with all, lengths that end inside a tile, tokens with fewer choices than asked for or none."""
+    r = np.random.default_rng(T + E)
+    up = (r.integers(-127, 128, (E, 2 * I, H)).astype(np.int8), (0.002 * np.exp(0.3 * r.standard_normal((E, 2 * I)))).astype(np.float32))
+    down = (r.integers(-127, 128, (E, H, I)).astype(np.int8), (0.002 * np.exp(0.3 * r.standard_normal((E, H)))).astype(np.float32))
+    wu, wd = (cq.cq_i8_pack(torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda()) for c, s in (up, down))
+    x, l = rows(T, H, "bf16", T, 0.3), torch.from_numpy(r.standard_normal((T, E))).float()
+    if T > 1:
+        l[torch.from_numpy(r.random((T, E)) < 0.4)] = -float("inf")
+        l[T // 2] = -float("inf")
+    routes = cq.cq_route(l.cuda(), top, cq.CQ_SOFTMAX)
+    expert, _ = ref_route.choose(as64(l), top, "softmax")
+    assert np.array_equal(routes.expert.cpu().numpy(), expert)
+    y = cq.cq_i8_moe(wu, wd, x.cuda(), routes)
+    want, size = moe_oracle(as64(x), expert, as64(routes.weight), up, down, torch.bfloat16)
+    err = np.abs(as64(y) - want)
+    allowed = torch.finfo(y.dtype).eps / 2 * np.abs(want) * (1 + 2.0 ** -10) + (top + 1) * 2.0 ** -24 * size + torch.finfo(y.dtype).tiny
+    assert np.all(err <= allowed), float((err / allowed).max())
+    if T > 1:
+        assert torch.all(y[T // 2] == 0)
+
+
+def test_two_expert_blocks_at_once():
+    """Two blocks on two streams with workspaces of their own, and two captured ones that share one, replayed in turn."""
+    E, H, I, top = 8, 512, 256, 2
+    g = torch.Generator("cuda").manual_seed(9)
+    wu = cq.cq_i8_quantize(torch.randn((E, 2 * I, H), generator=g, device="cuda") * 0.05)
+    wd = cq.cq_i8_quantize(torch.randn((E, H, I), generator=g, device="cuda") * 0.05)
+    cases = []
+    for T in (3, 200, 900):
+        x = torch.randn((T, H), generator=g, device="cuda").bfloat16()
+        cases.append((x, cq.cq_route(torch.randn((T, E), generator=g, device="cuda"), top)))
+    want = [cq.cq_i8_moe(wu, wd, x, r) for x, r in cases]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in cases], []
+    for _ in range(15):
+        for st, (x, r) in zip(streams, cases):
+            with torch.cuda.stream(st):
+                got.append(cq.cq_i8_moe(wu, wd, x, r))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want[i % 3]) for i, a in enumerate(got))
+    ws = cq.cq_i8_moe_workspace(wu, wd, 900, top)
+    graphs, outs = [], []
+    for x, r in cases:
+        out = torch.empty_like(x)
+        cq.cq_i8_moe(wu, wd, x, r, workspace=ws, out=out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cq.cq_i8_moe(wu, wd, x, r, workspace=ws, out=out)
+        graphs.append(graph)
+        outs.append(out)
+    for _ in range(10):
+        for graph, out, y in zip(graphs, outs, want):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(out, y)
     assert cq.cq_gemm_status(ws) == 0
 
 

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2608_06763_b200 as cq
+from i8_shapes import PRODUCTS
 from oracle import i8 as ref
 from oracle import route as ref_route
 from paper_2608_06763_b200 import i8, route
@@ -233,3 +234,28 @@ def test_debug_plan_refuses():
     assert L.cq_debug_i8_plan(0, 4, 128, 256, 0, None) == -1 and L.cq_debug_i8_plan(-1, 4, 128, 256, 0, plan) == -1 and L.cq_debug_i8_plan(0, 0, 128, 256, 0, plan) == -1
     assert L.cq_debug_i8_plan(0, 4, 128, 264, 0, plan) == -2 and L.cq_debug_i8_plan(513, 4, 128, 256, 0, plan) == -2
     assert L.cq_debug_i8_plan(0, 1 << 30, 1 << 30, 256, 0, plan) == -2
+
+
+def _cut(M, N, K, **how):
+    return tuple(cq.cq_debug_i8_plan(M, N, K, **how).values())
+
+
+def test_every_kind_of_tile_is_among_the_tested_shapes():
+    """The shapes that the GPU tests multiply reach each way of cutting a product, and no drawn size reaches another."""
+    rng = np.random.default_rng(5)
+    for plan, M, N, K in PRODUCTS:
+        assert _cut(M, N, K) == plan, (M, N, K)
+    kinds = {(p, N % 8 == 0) for p, _, N, _ in PRODUCTS}
+    for _ in range(6000):
+        M, N, K = int(2 ** rng.uniform(0, 12.5)), int(2 ** rng.uniform(0, 16)), 16 * int(2 ** rng.uniform(0, 11))
+        p = _cut(M, N, K)
+        assert (p, N % 8 == 0) in kinds, (M, N, K, p)
+        assert _cut(M, N, K, quantised=True) == ((128, 64, p[2], False) if p[3] else p)
+    assert all(_cut(R, 512, 512, matrices=E) == (256, 256, 1, False) for E in (1, 3, 16, 512) for R in (1, 60, 800, 5000, 200000))
+
+
+def test_few_rows_are_quantised_by_the_product():
+    """At most sixteen rows whose codes fit beside the ring, and few enough that each block may quantise them."""
+    own = lambda M, N, K: cq.cq_debug_i8_plan(M, N, K)["quantises"]  # noqa: E731
+    assert own(1, 4096, 4096) and own(4, 4096, 4096) and not own(5, 4096, 4096) and own(16, 4096, 1024) and not own(17, 4096, 128)
+    assert own(1, 264, 16384) and not own(1, 264, 16400) and not own(1, 30000, 8192) and not own(2, 4096, 14336)
