@@ -39,14 +39,14 @@ __device__ __forceinline__ void settle_in_64_bits(bool ask, const uint32_t *gw, 
 __device__ __forceinline__ float ulps_away(float v, int n) { return __uint_as_float(__float_as_uint(v) + n); }   // n > 0: away from zero
 // two activations
 __device__ __forceinline__ void gated_in_32_bits(float g0, float g1, float u0, float u1, float &y0, float &y1) {
-    const Pair g = pair_of(g0, g1), major = pair_of(-1.44269502f, -1.44269502f), minor = pair_of(-1.92596303e-8f, -1.92596303e-8f);   // log2(e) = their sum, negated
-    const Pair h = mul2(g, major);
+    const Pair g = pair_of(g0, g1), major = pair_of(1.44269502f, 1.44269502f), minor = pair_of(-1.92596303e-8f, -1.92596303e-8f);   // log2(e) = major - minor
+    const Pair h = mul2(g, major);   // -h: its sign is taken off where it is used
     float h0, h1, d0, d1;
     unpair(h, h0, h1);
-    const Pair l = fma2(g, minor, fma2(g, major, pair_of(-h0, -h1)));
+    const Pair l = fma2(g, minor, fma2(g, pair_of(-1.44269502f, -1.44269502f), h));
     float e0, e1;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(h0));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(h1));
+    asm("{\n\t.reg .f32 h;\n\tneg.f32 h, %1;\n\tex2.approx.ftz.f32 %0, h;\n\t}" : "=f"(e0) : "f"(h0));
+    asm("{\n\t.reg .f32 h;\n\tneg.f32 h, %1;\n\tex2.approx.ftz.f32 %0, h;\n\t}" : "=f"(e1) : "f"(h1));
     const Pair e = pair_of(e0, e1);
     unpair(add2(fma2(e, mul2(l, pair_of(0.693147181f, 0.693147181f)), e), pair_of(1.0f, 1.0f)), d0, d1);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(d0));

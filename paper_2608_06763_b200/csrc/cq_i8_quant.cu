@@ -4,6 +4,7 @@
 #include "cq_i8.cuh"
 #include "cq_internal.h"
 #include "cq_tc_ptx.cuh"
+#include "cq_tiles.cuh"
 
 namespace cq {
 namespace i8 {
@@ -11,6 +12,7 @@ namespace i8 {
 // A row belongs to a team of threads, 32 to 512 of them, which take units of sixteen neighbouring k in turn; a block has one team or several.
 // What a thread has read (formed) stays in shared memory until the row's scale is known; of a row beyond that room the rest is formed again.
 constexpr int ROOM = 40 << 10;   // bytes of shared memory for that
+constexpr int MOST_SPREAD = 8;
 struct Rows {
     const int32_t *route_token;   // routed: the row of x that row r takes (null: r itself)
     const int32_t *offset;        // routed: first rows of the groups, on the device (null: rows are dense)
@@ -19,6 +21,7 @@ struct Rows {
     int team, held;               // threads to a row; units of a row that are kept, a multiple of `team`
     const int32_t *route_row;     // SCATTER: rows are tokens, [rows][top] the routes of each (-1: none); `routes` of all
     int top, routes;
+    int lg_spread, part;          // SPREAD: blocks to a row (log2), units of each
 };
 struct Place { int64_t src, at; bool live, read; };   // row of x; row among the padded rows of the layout; whether it is one; whether x has it
 __device__ __forceinline__ void scan_if_routed(const Rows &q, int *s_off, int *s_blk) {
@@ -108,6 +111,11 @@ struct Plain {
         }
     }
 };
+__device__ __forceinline__ float largest_of(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // silu(gate) * up of rows of h (gate | up), rounded to their type (cq_gated.cuh).  Values whose rounding 32 bits leave open are formed in 64, each
 // lane one of its own at a time: in binary16 three warps of four have one in every step, but few lanes: 4096 x 14336 take 109 us, in bfloat16 72.  (Kept with a bit that says
 // so, and formed only where the row's largest or a code hangs on them: one in fifty does, but telling them costs more than forming them, 126 us.  Noted by a warp, and up to 32
@@ -145,20 +153,25 @@ struct Gated {
         const uint32_t gw[8] = {r.g[0].x, r.g[0].y, r.g[0].z, r.g[0].w, r.g[1].x, r.g[1].y, r.g[1].z, r.g[1].w};
         const uint32_t uw[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[1].x, r.u[1].y, r.u[1].z, r.u[1].w};
         uint32_t act[8], low[8], near = ~0u, least = ~0u;
+        float gate = 0.0f, most = 0.0f;   // the largest magnitudes; NaN counts as the largest
         constexpr uint32_t LEAST = 0x0400u, ENDLESS = DT == DT_BF16 ? 0x7F80u : 0x7C00u, FAR = DT == DT_BF16 ? 0x4270u : 0x5380u;   // the least normal half, infinity, 60
 #pragma unroll
         for (int k = 0; k < 16; k += 2) {
+            const float g0 = value_of<DT>(gw, k), g1 = value_of<DT>(gw, k + 1);
             float y0, y1;
-            gated_in_32_bits(value_of<DT>(gw, k), value_of<DT>(gw, k + 1), value_of<DT>(uw, k), value_of<DT>(uw, k + 1), y0, y1);
+            gated_in_32_bits(g0, g1, value_of<DT>(uw, k), value_of<DT>(uw, k + 1), y0, y1);
+            gate = largest_of(gate, g0, g1);
+            most = largest_of(most, y0, y1);
             low[k / 2] = dropped<DT>(y0, y1);
             near = nearer<DT>(near, low[k / 2]);
             act[k / 2] = pack16<DT>(y0, y1);
             if (DT == DT_F16) least = __viaddmin_u32(__float_as_uint(y0) & 0x7FFFFFFFu, ~0u, __viaddmin_u32(__float_as_uint(y1) & 0x7FFFFFFFu, ~0u, least));   // less one: 0 is exact, and becomes the largest
         }
         constexpr uint32_t WIDE = 2 * BAND * (DT == DT_BF16 ? 1 : 8);
-        uint32_t top = top_of_16bit<DT>(act);
+        const uint32_t rounded = pack16<DT>(most, 0.0f);
+        uint32_t top = __float_as_uint(value_of<DT>(&rounded, 0)) & 0x7FFFFFFFu;
         // far gates, what is not finite, and subnormal halves, which have their borders elsewhere
-        const bool odd = read && (top_of_16bit<DT>(gw) > 0x42700000u || top >= 0x7F800000u || (DT == DT_F16 && least < 0x38800000u - 1));   // 2^-14
+        const bool odd = read && (!(gate <= 60.0f) || top >= 0x7F800000u || (DT == DT_F16 && least < 0x38800000u - 1));   // 2^-14
         const bool open = read && ((near & 0xFFFFu) <= WIDE || (near >> 16) <= WIDE);
         s.piece(slot, 0) = make_uint4(act[0], act[1], act[2], act[3]);
         s.piece(slot, 1) = make_uint4(act[4], act[5], act[6], act[7]);
@@ -194,18 +207,22 @@ struct Gated {
 // ---------------------------------------------------------------- the quantisers
 // SCATTER: a token's codes go to all of its routes, formed once.
 struct Copy { uint8_t *line; int row; };   // the row block of a route, the row in it
-template <class From, bool SCATTER>
+// SPREAD: few long rows, each by a cluster of blocks, which tell one another the largest value of their parts.
+template <class From, bool SCATTER, bool SPREAD>
 __global__ void __launch_bounds__(512, 2) quantize_kernel(const From from, Rows q, int64_t K, int KT, float *scale, uint8_t *layout) {
     extern __shared__ uint4 s_store[];
-    __shared__ uint32_t red[2][16];
+    __shared__ uint32_t red[2][16], s_parts[MOST_SPREAD];
+    if (SPREAD) cluster_arrive();
     tc::wait_for_previous_kernel();
-    const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, mine = threadIdx.x / q.team, KU = (int)(K >> 4), units = KT * 8;
+    const int in = threadIdx.x & (q.team - 1), teams = blockDim.x / q.team, mine = threadIdx.x / q.team;
+    const int lg = SPREAD ? q.lg_spread : 0, rank = blockIdx.x & ((1 << lg) - 1), base = SPREAD ? rank * q.part : 0;   // this block's first unit
+    const int KU = SPREAD ? min((int)(K >> 4) - base, q.part) : (int)(K >> 4), units = SPREAD ? min(KT * 8 - base, q.part) : KT * 8;
     const int slots = q.held < KU ? q.held + q.team : q.held;   // a row that is longer has a slot for each thread besides
     const Store s{s_store + mine * From::PIECES * slots, slots};
     Copy *s_copy = reinterpret_cast<Copy *>(s_store + teams * From::PIECES * slots);   // SCATTER: [teams][two rows in turn][top]
     int *s_off = reinterpret_cast<int *>(s_copy + (SCATTER ? 2 * teams * q.top : 0)), *s_blk = s_off + q.E + 1;
-    const int64_t stride = (int64_t)gridDim.x * teams;
-    int64_t r = (int64_t)blockIdx.x * teams + mine, next = source_of(q, r);
+    const int64_t stride = (int64_t)(gridDim.x >> lg) * teams;
+    int64_t r = (int64_t)(blockIdx.x >> lg) * teams + mine, next = source_of(q, r);
     scan_if_routed(q, s_off, s_blk);
     int turn = 0;
     for (; r - mine < q.rows; r += stride, turn ^= 1) {
@@ -223,7 +240,7 @@ __global__ void __launch_bounds__(512, 2) quantize_kernel(const From from, Rows 
             next = source_of(q, r + stride);
         }
         uint32_t top = 0;
-        const uint8_t *first = from.unit(p.src, in), *src = first;
+        const uint8_t *first = from.unit(p.src, base + in), *src = first;
         const int64_t step = (int64_t)q.team * From::UNIT;
         for (int u0 = in; u0 - in < KU; u0 += From::AHEAD * q.team, src += From::AHEAD * step) {   // whole warps
             typename From::Raw raw[From::AHEAD];
@@ -236,15 +253,24 @@ __global__ void __launch_bounds__(512, 2) quantize_kernel(const From from, Rows 
                 from.keep(raw[i], src + i * step, p.read && u < KU, s, u < q.held ? u : q.held + in, top);
             }
         }
-        const float d = row_scale(team_max(top, q.team, red[turn])), inverse = __frcp_rn(d);
+        top = team_max(top, q.team, red[turn]);
+        if (SPREAD) {   // a row to a block: once
+            cluster_wait();   // the others have started
+            if (in < 1 << lg) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(tc::map_to_rank(&s_parts[rank], in)), "r"(top) : "memory");
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+            for (int j = 0; j < 1 << lg; ++j) top = max(top, s_parts[j]);
+        }
+        const float d = row_scale(top), inverse = __frcp_rn(d);
         if (SCATTER) {
             for (int j = in; j < q.top; j += q.team)
                 if (copies[j].line) scale[q.route_row[r * q.top + j]] = d;
-        } else if (p.live && in == 0) {
+        } else if (p.live && base + in == 0) {
             scale[r] = d;
         }
         // a unit's place in its tile is that of the thread, 8 units a tile
-        uint8_t *dst = layout + ((p.at >> 7) * KT + (in >> 3)) * (int64_t)TILE_BYTES + piece_offset((int)(p.at & (ROWS - 1)), in & 7);
+        uint8_t *dst = layout + ((p.at >> 7) * KT + ((base + in) >> 3)) * (int64_t)TILE_BYTES + piece_offset((int)(p.at & (ROWS - 1)), in & 7);
         const int64_t dst_step = (int64_t)(q.team >> 3) * TILE_BYTES;
         src = first;
 #pragma unroll 1
@@ -346,14 +372,27 @@ static unsigned grid_of(int64_t rows, int teams, int per_sm) {
     const int64_t blocks = (rows + teams - 1) / teams, most = per_sm ? (int64_t)per_sm * sm_count() : blocks;
     return (unsigned)(blocks < most ? blocks : most);
 }
+// Blocks to a row (log2).  A long row takes as long as its SM takes to issue it, a cluster half a microsecond: us with 1 / 2 / 4 / 8, gated (as they are) 1 x 4096 2.7 / 3.1 / 3.1 / 3.0,
+// 1 x 8192 3.3 / 3.4 / 3.1 / 3.0, 13 x 14336 4.9 / 4.8 / 3.8 / 3.6 (4.0 / 4.0 / 3.2 / 3.0), 64 x 14336 5.3 / 4.7 / 4.6 / 4.6, 64 x 28672 12.8 / 7.7 / 6.4 / 6.3 (8.8 / 6.1 / 5.5 / 5.2), 148 x 14336 6.7 /
+// 6.4 / 8.3 / 8.3.
+static int lg_spread_of(int64_t rows, int units) {
+    int lg = 0;
+    while (units >= 512 && 2 << lg <= MOST_SPREAD && rows << (lg + 1) <= 2 * sm_count() && units >> (lg + 1) >= 112) ++lg;
+    return lg;
+}
 template <bool SCATTER = false, class From>
 static cudaError_t quantize(const From &from, const I8Rows &s, int64_t K, float *scale, void *layout, cudaStream_t st) {
-    const int KT = kt_of(K), KU = (int)(K >> 4), team = team_of(s.rows, KU, s.rows <= 2 * sm_count() ? 512 : 256), threads = team < 256 ? 256 : team, teams = threads / team;
+    const int KT = kt_of(K), lg = SCATTER ? 0 : lg_spread_of(s.rows, (int)(K >> 4)), part = ((KT + (1 << lg) - 1) >> lg) * 8;   // whole tiles
+    const int KU = lg ? part : (int)(K >> 4), team = team_of(s.rows, KU, s.rows <= 2 * sm_count() ? 512 : 256), threads = lg || team >= 256 ? team : 256, teams = threads / team;
     const int all = (KU + team - 1) / team * team, room = ROOM / (teams * From::PIECES * 16) / team * team;
     const int held = all <= room ? all : room - team;
     const size_t smem = (size_t)teams * From::PIECES * 16 * (held < all ? held + team : held) + (SCATTER ? 2 * (size_t)teams * s.top * sizeof(Copy) : 0) + table_bytes(s);
-    return launch_overlapped(quantize_kernel<From, SCATTER>, dim3(grid_of(s.rows, teams, s.offset ? 1024 / threads : 0)), (unsigned)threads, smem, st, 1, true, from, rows_of(s, team, held), K, KT, scale,
-                             (uint8_t *)layout);
+    Rows q = rows_of(s, team, held);
+    q.lg_spread = lg; q.part = part;
+    const unsigned grid = lg ? (unsigned)s.rows << lg : grid_of(s.rows, teams, s.offset ? 1024 / threads : 0);
+    auto go = [&](auto kern) { return launch_overlapped(kern, dim3(grid), (unsigned)threads, smem, st, 1 << lg, true, from, q, K, KT, scale, (uint8_t *)layout); };
+    if constexpr (SCATTER) return go(quantize_kernel<From, true, false>);
+    else return lg ? go(quantize_kernel<From, false, true>) : go(quantize_kernel<From, false, false>);
 }
 
 }  // namespace i8

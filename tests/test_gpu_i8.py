@@ -170,6 +170,25 @@ def test_swiglu_roundings_that_32_bits_leave_open(M, I, dtype):
     check_codes(cq.cq_i8_swiglu_quantize(h.cuda()), *ref.quantize(as64(act)))
 
 
+@pytest.mark.parametrize("K", [8192, 14336 + 16, 40000])
+def test_few_long_routed_rows(K):
+    """Rows that several blocks share, of groups: as the same rows by themselves, tokens out of range as zeros, rows behind the last left alone."""
+    x = rows(5, 2 * K, "bf16", K, 1.0).cuda()
+    token = torch.tensor([4, 0, 9, 4, 2, -1, 1, 3], dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 3, 3, 7], dtype=torch.int32, device="cuda")
+    live, t = 7, token.clamp(0, 4).long()
+    inside = ((token >= 0) & (token < 5))[:, None]
+    taken = torch.where(inside, x[:, :K][t], torch.zeros((), dtype=x.dtype, device="cuda")).contiguous()
+    q, one = cq.cq_i8_quantize(x[:, :K], route_token=token, expert_offset=off), cq.cq_i8_quantize(taken)
+    left = torch.full((8, K), 7.0, dtype=torch.bfloat16, device="cuda")
+    cq.cq_i8_dequantize(q, out=left)
+    assert torch.equal(left[:live], cq.cq_i8_dequantize(one)[:live]) and torch.all(left[live:] == 7.0) and torch.equal(q.scale[:live], one.scale[:live])
+    h = x[t].contiguous()
+    a, b = cq.cq_i8_swiglu_quantize(h, expert_offset=off), cq.cq_i8_swiglu_quantize(h)
+    assert torch.equal(cq.cq_i8_dequantize(a)[:live], cq.cq_i8_dequantize(b)[:live]) and torch.equal(a.scale[:live], b.scale[:live])
+    check_codes(b, *ref.quantize(torch.from_numpy(ref.gated(as64(h[:, :K]), as64(h[:, K:]))).bfloat16().double().numpy()))
+
+
 def product_case(M, N, K, dtype, seed=0):
     r = np.random.default_rng(seed)
     wc, wd = r.integers(-128, 128, (N, K)).astype(np.int8), (0.001 * np.exp(0.5 * r.standard_normal(N))).astype(np.float32)
