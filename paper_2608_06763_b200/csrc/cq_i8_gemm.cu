@@ -29,8 +29,8 @@ struct GemmArgs {
 };
 
 // What a CTA computes.  ONE: 128 channels x up to 128 rows of x; TWO: a pair of CTAs 256 channels x up to 256 rows; FEW: 128 channels x up to 16
-// rows, which it quantises itself and keeps in shared memory; SMALL: 128 channels x up to 64 rows.
-enum { ONE = 0, TWO = 1, FEW = 2, SMALL = 3 };
+// rows, which it quantises itself and keeps in shared memory; SMALL: 128 channels x up to 64 rows; WIDE: 128 channels x up to 240 rows, in several runs of k.
+enum { ONE = 0, TWO = 1, FEW = 2, SMALL = 3, WIDE = 4 };
 // rows, and k tiles of them, that fit beside the ring
 constexpr int FEW_ROWS = 16, FEW_TILES = 32;
 
@@ -55,17 +55,20 @@ __device__ __forceinline__ uint32_t pack_out(uint32_t lo, uint32_t hi, float s_l
 template <int MODE, bool SPLIT>
 struct Shape {
     static constexpr bool PAIR = MODE == TWO;
-    static constexpr int BN = MODE == TWO ? 256 : MODE == ONE ? 128 : MODE == SMALL ? 64 : FEW_ROWS, CTAS = PAIR ? 2 : 1;
+    static constexpr bool ALIAS = MODE == WIDE;   // partial sums are exchanged within the ring
+    static constexpr int BN = MODE == TWO ? 256 : MODE == WIDE ? 240 : MODE == ONE ? 128 : MODE == SMALL ? 64 : FEW_ROWS, CTAS = PAIR ? 2 : 1;
     // A stage of the ring has DEEP k tiles.  Waiting, fencing and committing for each k tile takes 240 ns, more than its MMAs or its copy from L2 (150 for 64 rows).  With two
     // to a stage 512 rows of 4096 x 4096 take 10.5 us as ONE instead of 11.9; a pair's copies take longer than that, and a deeper ring of single tiles serves it better.
-    static constexpr int DEEP = PAIR ? 1 : 2;
+    static constexpr int DEEP = PAIR || MODE == WIDE ? 1 : 2;
     static constexpr int B_TILE = MODE == FEW ? 0 : BN / CTAS * 128;   // codes of x in this CTA: half of a pair's
     static constexpr int A_BYTES = DEEP * TILE_BYTES, B_BYTES = DEEP * B_TILE, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = PAIR ? 6 : MODE == ONE ? (SPLIT ? 2 : 3) : MODE == SMALL && SPLIT ? 3 : 4;
-    static constexpr int ACCS = 2, ACC_COLS = BN < 32 ? 32 : BN;   // accumulators: while one is read the next tile fills the other
+    static constexpr int ACCS = 2, ACC_COLS = BN < 32 ? 32 : BN > 128 ? 256 : BN;   // accumulators: while one is read the next tile fills the other
     static constexpr int PITCH = 272;                              // bytes of a row of the staged output: 128 channels and a gap against bank conflicts
     static constexpr int X_CODES = FEW_ROWS * 128, X_BYTES = MODE == FEW ? FEW_TILES * X_CODES : 0;   // FEW: codes of a k tile; all k tiles
-    static constexpr int OUT_BYTES = SPLIT ? 128 * (BN + 4) * 4 : (MODE == FEW ? 32 : 64) * PITCH;   // SPLIT: partial sums [run][channel][row of x, and a gap]
+    // SPLIT: partial sums [run][channel][row of x, and a gap]; ALIAS: what those that are sent and three quarters of those that come take beyond the ring
+    static constexpr int SUMS = 128 * (BN + 4) * 4;
+    static constexpr int OUT_BYTES = ALIAS ? SUMS / 4 * 7 - STAGES * STAGE : SPLIT ? SUMS : (MODE == FEW ? 32 : 64) * PITCH;
     static constexpr int SCALE_BYTES = BN * 4, BAR_BYTES = 256 + FEW_ROWS * 4;   // scales of the rows of a tile; barriers and what FEW gathers maxima in
     static constexpr size_t smem(int E, bool routed) {
         return (size_t)STAGES * STAGE + X_BYTES + OUT_BYTES + SCALE_BYTES + BAR_BYTES + (routed ? 3 * (size_t)(E + 1) * 4 : 0);
@@ -76,7 +79,7 @@ struct Shape {
 
 // SPLIT, the eight warps that write y: this CTA's partial sums to the CTAs that add them, then its own 128 / S channels of all runs.  Sums arrive
 // counted on a barrier, so nobody waits for the whole cluster in between.  Few rows are sent from the registers; more go through the ring,
-// which nobody needs any more, and from there in one copy to each CTA.
+// which nobody needs any more, and from there in one copy to each CTA.  ALIAS: those of the others land in the ring too, once all rings are free.
 template <class SH>
 __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, int lgS, int run, int warp, int lane, uint8_t *ring, uint8_t *part, const float *x_scale, uint64_t *sums,
                                              volatile int *dead) {
@@ -87,6 +90,7 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
     if (tid == 0) tc::mbar_arrive_expect_tx(sums, COPY ? ((1u << lgS) - 1) * bytes_of_run : 128u * (uint32_t)((t.rows + 3) & ~3) * 4u);
     tc::tc_fence_after();
     __syncwarp();
+    if (SH::ALIAS) { cluster_arrive(); part = ring + 128 * pitch * 4; }   // this ring is free
     if (!COPY) cluster_wait();   // the others have started, and their barriers exist
     const uint32_t to = COPY ? tc::smem_u32(ring) + (uint32_t)c * pitch * 4 : tc::map_to_rank(part, owner) + (uint32_t)((run << lgCW) + (c & (CW - 1))) * pitch * 4;
     const uint32_t bar = COPY ? 0 : tc::map_to_rank(sums, owner);
@@ -104,10 +108,10 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
     if (COPY) {
         tc::fence_proxy_async();
         epilogue_sync();
-        cluster_wait();   // the others have started, and their barriers exist
+        cluster_wait();   // the others have started, and their barriers exist (ALIAS: their rings are free)
         if (tid < 1 << lgS && tid != run)
             asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                         ::"r"(tc::map_to_rank(part, tid) + run * bytes_of_run), "r"(tc::smem_u32(ring) + tid * bytes_of_run), "r"(bytes_of_run), "r"(tc::map_to_rank(sums, tid)) : "memory");
+                         ::"r"(tc::map_to_rank(part, tid) + (run - (run > tid)) * bytes_of_run), "r"(tc::smem_u32(ring) + tid * bytes_of_run), "r"(bytes_of_run), "r"(tc::map_to_rank(sums, tid)) : "memory");
         __syncwarp();
     } else {
         __syncwarp();
@@ -133,7 +137,8 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
 #pragma unroll
         for (int s = 1; s < 4; ++s)
             if (s < 1 << lgS) {
-                const uint8_t *from = part + (run ^ s) * bytes_of_run + at;
+                const int other = run ^ s;
+                const uint8_t *from = part + (COPY && other > run ? other - 1 : other) * bytes_of_run + at;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int4 v = *reinterpret_cast<const int4 *>(from + j * next);
@@ -250,7 +255,7 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
     tc::tc_fence_before();
     __syncthreads();
     if (PAIR) tc::cluster_sync();   // the partner's barriers exist before anything arrives on them
-    if (SPLIT) cluster_arrive();
+    if (SPLIT && !SH::ALIAS) cluster_arrive();
     tc::tc_fence_after();
     Tiles<PAIR, GemmArgs> tiles{p, unit, SPLIT ? n_items : units, n_items, s_off, s_blk, s_item, {}};   // split: one tile
     if (!p.offset) {   // what needs no other kernel: the first tiles' places, and the first weights on their way to L2, which sees what the kernel in front may still write
@@ -275,7 +280,7 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
 
     int it = 0;   // stages filled (warps 0 and 2) so far
     if (warp == 0 || (warp == 2 && MODE != FEW)) {
-        // warp 0 the weights, warp 2 its rows of codes, from one row block or two (a lane for each)
+        // warp 0 the weights, warp 2 its rows of codes, from one row block or several (a lane for each)
         const int64_t block = (int64_t)p.KT * TILE_BYTES;   // from a row block to the next
         uint32_t s = 0, phase = 1;
         bool ok = true;
@@ -283,19 +288,19 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
         for (int local = 0; ok && tiles.has(local); ++local) {
             const Item t = tiles.at(local);
             const int n = columns_of<PAIR>(t.rows), mine = n / CTAS, nb = min(t.nb * CTAS + half, p.NB - 1);   // an odd last pair reads a block twice
-            const int r0 = t.off + half * mine, b0 = r0 / ROWS, in0 = r0 % ROWS, n0 = min(mine, ROWS - in0), n1 = mine - n0;
+            const int r0 = t.off + half * mine, b0 = r0 / ROWS, in0 = r0 % ROWS;
             const uint8_t *xt = p.x + ((int64_t)t.xblk * p.KT + k0) * TILE_BYTES, *src = xt;
-            // warp 0: one piece, neighbouring k tiles are neighbours in memory; warp 2: lanes 2 j and 2 j + 1 the rows of k tile j of a stage
-            const int mine_kt = warp == 0 ? 0 : lane >> 1;
+            // warp 0: one piece, neighbouring k tiles are neighbours in memory; warp 2: lanes 4 j to 4 j + 2 the rows of k tile j of a stage, a row block each
+            const int mine_kt = warp == 0 ? 0 : lane >> 2, piece = lane & 3, lo = piece ? piece * ROWS - in0 : 0, hi = min(mine, (piece + 1) * ROWS - in0);
             uint32_t to = 0, bytes = 0, all = TILE_BYTES;
             if (warp == 0) {
                 if (lane == 0) { src = p.w + (((int64_t)t.e * p.NB + nb) * p.KT + k0) * TILE_BYTES; bytes = TILE_BYTES; }
             } else {
                 all = (uint32_t)mine * 128;
-                if (mine_kt < SH::DEEP) {
-                    src = xt + (b0 + (lane & 1)) * block + (lane & 1 ? 0 : in0 * 128) + mine_kt * TILE_BYTES;
-                    to = SH::A_BYTES + mine_kt * SH::B_TILE + (lane & 1 ? n0 * 128 : 0);
-                    bytes = (uint32_t)(lane & 1 ? n1 : n0) * 128;
+                if (mine_kt < SH::DEEP && lo < hi) {
+                    src = xt + (b0 + piece) * block + (piece ? 0 : in0 * 128) + mine_kt * TILE_BYTES;
+                    to = SH::A_BYTES + mine_kt * SH::B_TILE + lo * 128;
+                    bytes = (uint32_t)(hi - lo) * 128;
                 }
             }
             for (int kt = k0; kt < k1; kt += SH::DEEP, ++it, src += SH::DEEP * TILE_BYTES) {
@@ -384,6 +389,7 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
             const bool ok = tc::mbar_wait(&acc_full[acc], (local / ACCS) & 1, p.status, 66, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
             if (epilogue_any(!ok)) {
                 *dead = 1;
+                if (SH::ALIAS) cluster_arrive();
                 if (SPLIT) { cluster_wait(); cluster_arrive(); }
                 break;
             }
@@ -448,6 +454,7 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
 
     if (SPLIT && warp < 4) {   // the others have done so on their way
         __syncwarp();
+        if (SH::ALIAS) cluster_arrive();
         cluster_wait();
         cluster_arrive();
     }
@@ -466,10 +473,14 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
 }
 
 template <int MODE, bool SPLIT>
+static cudaError_t allow_smem() {
+    static std::atomic<uint64_t> done{0};
+    return ensure_func_attr(i8_gemm_kernel<MODE, SPLIT>, done, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<MODE, SPLIT>::smem(MAX_EXPERTS, MODE != FEW));
+}
+template <int MODE, bool SPLIT>
 static cudaError_t launch(const GemmArgs &p, int lgS, int64_t items, unsigned grid, cudaStream_t st) {
     using SH = Shape<MODE, SPLIT>;
-    static std::atomic<uint64_t> done{0};
-    const cudaError_t e = ensure_func_attr(i8_gemm_kernel<MODE, SPLIT>, done, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SH::smem(MAX_EXPERTS, MODE != FEW));
+    const cudaError_t e = allow_smem<MODE, SPLIT>();
     if (e != cudaSuccess) return e;
     return launch_overlapped(i8_gemm_kernel<MODE, SPLIT>, dim3(grid), 384u, SH::smem(p.E, p.offset != nullptr), st, SH::CTAS << (SPLIT ? lgS : 0), true, p, lgS, (int)items);
 }
@@ -478,10 +489,28 @@ static cudaError_t launch(const GemmArgs &p, int lgS, int64_t items, unsigned gr
 
 using namespace i8;
 
-// Runs of k that an output tile of few row blocks is cut into, while the GPU has places for them.
-static int lg_runs_of(int tiles, int KT, int places) {
+// Clusters of four CTAs that the GPU takes at once: fewer than a quarter of its SMs, which are not in groups of four.  One cluster more waits for all others: 4352 x 4096 with 13 rows 9.9 us
+// in four runs, 5.9 with one row block less, 6.0 in two.
+static int clusters_of_four() {
+    static std::atomic<int> cached[64];
+    constexpr int USUAL = 33;   // of 148 SMs
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { (void)cudaGetLastError(); return USUAL; }
+    if ((n = cached[dev].load(std::memory_order_relaxed)) > 0) return n;
+    cudaLaunchAttribute four{};
+    four.id = cudaLaunchAttributeClusterDimension;
+    four.val.clusterDim.x = 4; four.val.clusterDim.y = four.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(4 * sm_count()); cfg.blockDim = dim3(384); cfg.dynamicSmemBytes = Shape<SMALL, true>::smem(1, false); cfg.attrs = &four; cfg.numAttrs = 1;
+    if (allow_smem<SMALL, true>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, i8_gemm_kernel<SMALL, true>, &cfg) != cudaSuccess || n <= 0) { (void)cudaGetLastError(); return USUAL; }
+    cached[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+// Runs of k (log2) that an output tile of few row blocks is cut into, while the GPU has places for them.
+static bool has_places(int64_t tiles, int lg) { return lg == 0 || (tiles << lg <= sm_count() && (lg < 2 || tiles <= clusters_of_four())); }
+static int lg_runs_of(int tiles, int KT) {
     int lg = 0;
-    while (lg < 2 && 2 << lg <= KT && (int64_t)(2 << lg) * tiles <= places) ++lg;
+    while (lg < 2 && 2 << lg <= KT && has_places(tiles, lg + 1)) ++lg;
     return lg;
 }
 static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scale, uint16_t *y, int64_t M, int64_t N, int64_t K, bool f16, int *status) {
@@ -496,30 +525,34 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
 // What computes a product of more than sixteen rows: kind of tile, rows to a tile, runs of k (log2).  Costs in microseconds, from tiles forced in turn.  A k
 // tile of one CTA takes as long as an SM's port to L2 does for its bytes (145 bytes a nanosecond); a pair's, its copies at least and for many rows its MMAs.  Cutting k saves
 // k tiles and costs a cluster's launch and the exchange.
-//   4096 x 4096, 200 rows: SMALL 8.9, ONE 10.0 (two runs 10.7), TWO 10.6;  300: SMALL 14.3, ONE 10.2, TWO 11.4;  512: ONE 10.5, TWO 11.7;  700: ONE 17.3, TWO 12.8
-//   4096 x 14336, 100 rows: SMALL 22.1, in two runs 15.1, ONE 24.6 / 18.7, in four 13.9, TWO 26.2;  200: SMALL 22.4, ONE 25.7, in two runs 20.6, TWO 26.6
-//   11176 x 22368, 341 rows: SMALL 124, ONE 88.6, TWO 84.0 / 96.2 / 113.6 with 128 / 192 / 256 rows;  925 x 12800, 1120 rows: ONE 26.1, in two runs 19.3, TWO 26.8
+//   4096 x 4096, 200 rows: SMALL 8.9, ONE 10.0 (two runs 10.0), WIDE 11.7, TWO 10.6;  300: SMALL 14.3, ONE 10.2, TWO 11.4;  512: ONE 10.5, TWO 11.7;  700: ONE 17.3, TWO 12.8
+//   4096 x 14336, 100 rows: SMALL 22.1, in two runs 15.1, ONE 24.6 / 18.7, in four 13.9, TWO 26.2;  200: SMALL 22.6, ONE 25.5, in two runs 19.7, WIDE in two 22.2, in four 17.8, TWO 26.6
+//   8192 x 8192, 160 rows: ONE 16.9, WIDE in two runs 15.2, TWO 17.9;  4096 x 8192, 300 rows: ONE 16.6, WIDE in two 15.0, TWO 18.0;  925 x 12800, 1120 rows: ONE 26.1, in two runs 19.3, TWO 26.8
+//   440 x 2912, 22 rows: SMALL 6.5, in two runs 5.6, in four 5.0;  3031 x 1664, 55 rows: 6.5 / 6.1 / 5.9
 //   28672 x 4096, 40 rows: SMALL 20.8, TWO 22.8;  128: SMALL 28.7, ONE 24.8, TWO 25;  6144 x 4096, 1024 rows: ONE 24.9, TWO 20.3
+//   11176 x 22368, 341 rows: SMALL 124, ONE 88.6, TWO 84.0 / 96.2 / 113.6 with 128 / 192 / 256 rows
 // Tried and dropped, sums through L2 where integers may be added in any order: even runs of all k tiles for each CTA (4096 x 4096, one row 11.0 us
 // where whole tiles then took 7.8, 28672 x 4096 as before, 57344 x 8192 79.7 where they took 84.2), the last round's pairs cut along K (200 rows of 4096 x 14336 21.5, 1024 of
 // 6144 x 4096 28.8): an exchange there takes some four microseconds of fences, counting and reading back, and each run has two ends.
 struct Plan { int mode, bt, lg; };
+static int even_rows(int64_t M, int64_t tiles) { return (int)((M + tiles - 1) / tiles + 15) & ~15; }   // WIDE: rows of its tiles
 static Plan dense_plan(int64_t M, int NB, int KT) {
-    static const Plan kinds[] = {{SMALL, 64, 0}, {SMALL, 64, 1}, {SMALL, 64, 2}, {ONE, 128, 0}, {ONE, 128, 1}, {ONE, 128, 2}, {TWO, 128, 0}, {TWO, 192, 0}, {TWO, 256, 0}};
+    static const Plan kinds[] = {{SMALL, 64, 0}, {SMALL, 64, 1}, {SMALL, 64, 2}, {ONE, 128, 0}, {ONE, 128, 1}, {ONE, 128, 2}, {WIDE, 240, 1}, {WIDE, 240, 2}, {TWO, 128, 0}, {TWO, 192, 0}, {TWO, 256, 0}};
     const int sms = sm_count();
     Plan best = kinds[3];
     double least = 1e30;
     for (const Plan &k : kinds) {
         const int ctas = k.mode == TWO ? 2 : 1, S = 1 << k.lg, nbu = (NB + ctas - 1) / ctas, places = sms / ctas;
-        if (S > KT) continue;
+        if (S > KT || (k.mode == WIDE && M <= 128) || (k.mode == ONE && M <= 64)) continue;
         const int64_t tiles = (M + k.bt - 1) / k.bt, items = nbu * tiles;
-        if (k.lg && items * S > places) continue;   // one round, or the runs of several tiles wait for one another's places
-        const double n = M < k.bt ? (double)M : (double)k.bt, rounds = (double)((items * S + places - 1) / places);
+        if (!has_places(items, k.lg)) continue;   // one round, or the runs of several tiles wait for one another's places
+        const double n = k.mode == WIDE ? (double)even_rows(M, tiles) : M < k.bt ? (double)M : (double)k.bt, rounds = (double)((items * S + places - 1) / places);
         double per_kt, tail, base;
         if (k.mode == TWO) { per_kt = std::max(0.205, 0.13 + 0.15 * n / 256); tail = 0.5 * n / 256; base = 4.4; }
         else {
             per_kt = (16.4 + 0.128 * n) / 145.0;
-            tail = 0.5; base = 2.4 + (k.lg ? (k.mode == SMALL ? 3.0 : 4.5) : 0.0);
+            const double exchange = k.mode == SMALL ? (k.lg == 1 ? 0.4 + 0.017 * n : 0.6 + 0.026 * n) : k.mode == WIDE && k.lg == 2 ? 6.1 : 4.1;
+            tail = k.lg ? 0.5 : 0.0094 * n; base = 2.8 + (k.lg ? exchange : 0.0);
         }
         const double cost = base + rounds * ((KT + S - 1) / S * per_kt + tail);
         if (cost < least) { least = cost; best = k; }
@@ -532,7 +565,7 @@ static Plan dense_plan(int64_t M, int NB, int KT) {
 constexpr int FEW_MOST = 128;
 bool i8_few_ok(int64_t M, int64_t N, int64_t K) {
     if (M > FEW_ROWS) return false;
-    const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT, sm_count()), most = (KT + S - 1) / S;
+    const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB), S = 1 << lg_runs_of(NB, KT), most = (KT + S - 1) / S;
     return most <= FEW_TILES && M * KT <= FEW_MOST;
 }
 // What launch_i8_gemm takes for M rows.  Routed rows: the loads are on the GPU, and pairs with 256 rows serve all of them.  Sixteen matrices of 2816 x 2048, us with SMALL / ONE /
@@ -540,17 +573,17 @@ bool i8_few_ok(int64_t M, int64_t N, int64_t K) {
 static Plan plan_of(bool routed, int64_t M, int64_t N, int64_t K) {
     const int NB = (int)((N + 127) / 128), KT = (int)((K + KB - 1) / KB);
     if (routed) return {TWO, 256, 0};
-    return M <= FEW_ROWS ? Plan{SMALL, 64, lg_runs_of(NB, KT, sm_count())} : dense_plan(M, NB, KT);
+    return M <= FEW_ROWS ? Plan{SMALL, 64, lg_runs_of(NB, KT)} : dense_plan(M, NB, KT);
 }
 I8Plan i8_plan(bool routed, int64_t M, int64_t N, int64_t K, bool own) {
-    if (own) return I8Plan{128, FEW_ROWS, 1 << lg_runs_of((int)((N + 127) / 128), (int)((K + KB - 1) / KB), sm_count())};
+    if (own) return I8Plan{128, FEW_ROWS, 1 << lg_runs_of((int)((N + 127) / 128), (int)((K + KB - 1) / KB))};
     const Plan q = plan_of(routed, M, N, K);
     return I8Plan{q.mode == TWO ? 256 : 128, q.bt, 1 << q.lg};
 }
 cudaError_t launch_i8_few(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, uint16_t *y, int64_t M, int64_t N, int64_t K, bool f16, int *status, cudaStream_t st) {
     GemmArgs p = args_of(w, w_scale, nullptr, y, M, N, K, f16, status);
     p.xr = x; p.ldx = ldx; p.bt = FEW_ROWS; p.token_tiles = 1;
-    const int places = sm_count(), lg = lg_runs_of(p.NB, p.KT, places);
+    const int places = sm_count(), lg = lg_runs_of(p.NB, p.KT);
     const unsigned grid = (unsigned)(lg ? p.NB << lg : p.NB < places ? p.NB : places);
     return lg ? launch<FEW, true>(p, lg, p.NB, grid, st) : launch<FEW, false>(p, 0, p.NB, grid, st);
 }
@@ -561,12 +594,14 @@ cudaError_t launch_i8_gemm(const void *w, const float *w_scale, const void *x, c
     p.early = early;
     p.x = (const uint8_t *)x; p.offset = offset; p.E = E;
     const Plan q = plan_of(offset != nullptr, M, N, K);
-    p.bt = q.bt;
     p.token_tiles = (int)((M + q.bt - 1) / q.bt);
+    p.bt = q.mode == WIDE ? even_rows(M, p.token_tiles) : q.bt;
+    if (q.mode == WIDE) p.token_tiles = (int)((M + p.bt - 1) / p.bt);   // rounded up, the rows of many tiles may fit fewer
     const int ctas = q.mode == TWO ? 2 : 1, nbu = (p.NB + ctas - 1) / ctas, places = sm_count() / ctas;
     const int64_t items = (int64_t)nbu * p.token_tiles;
     const unsigned grid = (unsigned)(q.lg ? items << q.lg : offset ? places : items < places ? items : places) * ctas;
     if (q.mode == TWO) return launch<TWO, false>(p, 0, items, grid, st);
+    if (q.mode == WIDE) return launch<WIDE, true>(p, q.lg, items, grid, st);
     if (q.mode == ONE) return q.lg ? launch<ONE, true>(p, q.lg, items, grid, st) : launch<ONE, false>(p, 0, items, grid, st);
     return q.lg ? launch<SMALL, true>(p, q.lg, items, grid, st) : launch<SMALL, false>(p, 0, items, grid, st);
 }

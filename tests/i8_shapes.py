@@ -13,8 +13,11 @@ PRODUCTS = [
     ((128, 64, 1, False), 99, 337, 544), ((128, 64, 1, False), 37, 19344, 272),
     ((128, 64, 2, False), 23, 5165, 5968), ((128, 64, 2, False), 20, 5720, 5856), ((128, 64, 4, False), 33, 331, 4656), ((128, 64, 4, False), 70, 264, 6160),
     # tiles of 128 rows: the same
-    ((128, 128, 1, False), 70, 10491, 304), ((128, 128, 1, False), 123, 19672, 272),
-    ((128, 128, 2, False), 67, 6187, 7552), ((128, 128, 2, False), 69, 4752, 7312), ((128, 128, 4, False), 76, 2467, 5488), ((128, 128, 4, False), 128, 2560, 8208),
+    ((128, 128, 1, False), 70, 10491, 304), ((128, 128, 1, False), 100, 19680, 144), ((128, 128, 1, False), 100, 20001, 144),
+    ((128, 128, 2, False), 67, 6187, 7552), ((128, 128, 2, False), 69, 4752, 7312), ((128, 128, 4, False), 100, 2467, 10000), ((128, 128, 4, False), 1100, 264, 12880),
+    # tiles of up to 240 rows, in two and four runs of K; several tiles, which start within a row block and may reach into a third one
+    ((128, 240, 2, False), 150, 6517, 6064), ((128, 240, 2, False), 160, 6432, 6160), ((128, 240, 4, False), 200, 3107, 9856), ((128, 240, 4, False), 240, 2825, 10000),
+    ((128, 240, 4, False), 400, 1544, 9104), ((128, 240, 4, False), 3700, 136, 12304),
     # pairs of CTAs; 192 rows to a tile: every second tile starts at row 64 of a row block
     ((256, 128, 1, False), 790, 15137, 448), ((256, 128, 1, False), 790, 15136, 448),
     ((256, 192, 1, False), 141, 14371, 800), ((256, 192, 1, False), 130, 13168, 688), ((256, 192, 1, False), 941, 14779, 144), ((256, 192, 1, False), 1341, 10304, 272),
