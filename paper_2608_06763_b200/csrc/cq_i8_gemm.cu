@@ -77,6 +77,28 @@ struct Shape {
     static_assert(ACCS * ACC_COLS <= 512, "tensor memory");
 };
 
+// A row of up to 128 values from shared memory to anywhere, by sixteen threads: sixteen bytes each where they are aligned in global memory, of which two neighbouring pieces
+// of the row are shifted together; up to eight values before and behind singly.  4096 rows of 8191 x 2048 68.6 us with all values stored singly, 45.8 for rows of 8192.
+__device__ __forceinline__ void store_row(uint16_t *to, const uint8_t *row, int j, int chans) {
+    const int m = (int)(reinterpret_cast<uintptr_t>(to) >> 1) & 7;   // values in front of the row's first in its piece
+    const uint16_t *values = reinterpret_cast<const uint16_t *>(row);
+    const int c = 8 * j - m;   // this thread's piece: values c to c + 7
+    if (c >= 0 && c + 8 <= chans) {
+        const uint4 b = *reinterpret_cast<const uint4 *>(row + j * 16), a = m ? *reinterpret_cast<const uint4 *>(row + j * 16 - 16) : b;
+        const int by = (8 - m) & 7;   // values of a that are left out
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int k = 0; k < 6; ++k) w[k] = by & 4 ? w[k + 2] : w[k];
+#pragma unroll
+        for (int k = 0; k < 5; ++k) w[k] = by & 2 ? w[k + 1] : w[k];
+        const uint32_t odd = by & 1 ? 16u : 0u;
+        *reinterpret_cast<uint4 *>(to + c) = make_uint4(__funnelshift_r(w[0], w[1], odd), __funnelshift_r(w[1], w[2], odd), __funnelshift_r(w[2], w[3], odd), __funnelshift_r(w[3], w[4], odd));
+    } else if (c >= 0) {   // of a last block that has not all 128
+        for (int k = c; k < min(c + 8, chans); ++k) to[k] = values[k];
+    }
+    const int edge = j < 8 - m ? j : 120 + j;   // before the first whole piece, behind the last of 128
+    if (m && j < 8 && edge < chans) to[edge] = values[edge];
+}
 // SPLIT, the eight warps that write y: this CTA's partial sums to the CTAs that add them, then its own 128 / S channels of all runs.  Sums arrive
 // counted on a barrier, so nobody waits for the whole cluster in between.  Few rows are sent from the registers; more go through the ring,
 // which nobody needs any more, and from there in one copy to each CTA.  ALIAS: those of the others land in the ring too, once all rings are free.
@@ -447,8 +469,11 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
                         if (r < count && c < chans) *reinterpret_cast<uint4 *>(out + (int64_t)r * p.N + c) = *reinterpret_cast<const uint4 *>(staged + r * SH::PITCH + c * 2);
                     }
                 } else {
-                    for (int r = warp - 4; r < count; r += 8)
-                        for (int c = lane; c < chans; c += 32) out[(int64_t)r * p.N + c] = *reinterpret_cast<const uint16_t *>(staged + r * SH::PITCH + c * 2);
+#pragma unroll 1
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = i * 16 + (tid >> 4);
+                        if (r < count) store_row(out + (int64_t)r * p.N, staged + r * SH::PITCH, tid & 15, chans);
+                    }
                 }
                 epilogue_sync();   // read before it is written again, and so are the scales of the rows
             }

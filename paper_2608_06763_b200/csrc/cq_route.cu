@@ -644,54 +644,68 @@ __global__ void __launch_bounds__(1024) place_kernel(const Args p, int blocks) {
 }
 
 // ---------------------------------------------------------------- the routes of a token together
-// y[t] = add[t] + sum over j of weight[t][j] routes[row[t][j]], in fp32 and in the order of j, rounded once.  A thread takes eight (one) values of a token, the
-// loads of four routes on their way together.  Rows outside [0, R) are no routes and are not read.  `add` may be y.  Bound by memory: 4096 tokens of 4096 values
-// and eight routes 46.4 us, 6.5 TB/s; with divisions of a flat index by the row's length 49.5.
-template <bool F16, bool WIDE>
+// y[t] = add[t] + sum over j of weight[t][j] routes[row[t][j]], in fp32 and in the order of j, rounded once.  A thread takes VALUES neighbouring values of a token (as many as
+// one load brings of rows that are so aligned), UNITS times; the loads of four routes are on their way together.  Rows outside [0, R) are no routes and are not read.  `add` may be
+// y.  Bound by memory: 4096 tokens of 4096 values and eight routes 46.4 us, 6.5 TB/s (with divisions of a flat index by the row's length 49.5).
+template <int VALUES> struct Some;
+template <> struct Some<8> { using T = uint4; };
+template <> struct Some<2> { using T = uint32_t; };
+template <> struct Some<1> { using T = uint16_t; };
+constexpr int units_for(int values) { return values == 8 ? 1 : 4; }
+template <bool F16, int VALUES>
 __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, int64_t ldr, int R, const float *weight, const int32_t *row, int T, int top, int N, const uint16_t *add, int64_t lda,
                                                       uint16_t *y, int64_t ldy) {
     tc::wait_for_previous_kernel();
-    constexpr int DT = F16 ? DT_F16 : DT_BF16, BATCH = 4, VALUES = WIDE ? 8 : 1;
+    using S = typename Some<VALUES>::T;
+    constexpr int DT = F16 ? DT_F16 : DT_BF16, BATCH = 4, UNITS = units_for(VALUES);
+    const auto value = [](const S &s, int k) {
+        if constexpr (VALUES == 8) { const uint32_t w[4] = {s.x, s.y, s.z, s.w}; return value_of<DT>(w, k); }
+        else { const uint32_t w = s; return value_of<DT>(&w, k); }
+    };
     const int t = blockIdx.x * blockDim.y + threadIdx.y;   // blocks of one token, or of several short ones
     if (t >= T) return;
     const int32_t *rows_of = row + t * top;
     const float *weights = weight + t * top;
-    for (int c = threadIdx.x * VALUES; c < N; c += blockDim.x * VALUES) {
-        if (WIDE) {
-            float f[8];
-            uint4 a = make_uint4(0, 0, 0, 0);
-            if (add) a = load16(add + t * lda + c);
-            const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
+    const int apart = blockDim.x * VALUES;   // from a unit to the next
+    for (int c0 = threadIdx.x * VALUES; c0 < N; c0 += apart * UNITS) {
+        float f[UNITS][VALUES];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = add ? value_of<DT>(aw, k) : 0.0f;
-            for (int j0 = 0; j0 < top; j0 += BATCH) {
-                uint4 v[BATCH];
-                float w[BATCH];
-                bool live[BATCH];
+        for (int u = 0; u < UNITS; ++u) {
+            S a{};
+            const bool with = add && c0 + u * apart < N;
+            if (with) a = *reinterpret_cast<const S *>(add + t * lda + c0 + u * apart);
 #pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    const int r = j0 + j < top ? rows_of[j0 + j] : -1;
-                    live[j] = r >= 0 && r < R;
-                    v[j] = live[j] ? load16(routes + r * ldr + c) : make_uint4(0, 0, 0, 0);
-                    w[j] = live[j] ? weights[j0 + j] : 0.0f;
+            for (int k = 0; k < VALUES; ++k) f[u][k] = with ? value(a, k) : 0.0f;
+        }
+        for (int j0 = 0; j0 < top; j0 += BATCH) {
+            S v[BATCH][UNITS];
+            float w[BATCH];
+            bool live[BATCH];
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int r = j0 + j < top ? rows_of[j0 + j] : -1;
+                live[j] = r >= 0 && r < R;
+                const uint16_t *from = routes + r * ldr + c0;
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) v[j][u] = live[j] && c0 + u * apart < N ? *reinterpret_cast<const S *>(from + u * apart) : S{};
+                w[j] = live[j] ? weights[j0 + j] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j)
+                if (live[j]) {
+#pragma unroll
+                    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+                        for (int k = 0; k < VALUES; ++k) f[u][k] = fmaf(w[j], value(v[j][u], k), f[u][k]);
                 }
+        }
 #pragma unroll
-                for (int j = 0; j < BATCH; ++j)
-                    if (live[j]) {
-                        const uint32_t vw[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) f[k] = fmaf(w[j], value_of<DT>(vw, k), f[k]);
-                    }
-            }
-            *reinterpret_cast<uint4 *>(y + t * ldy + c) = make_uint4(pack16<DT>(f[0], f[1]), pack16<DT>(f[2], f[3]), pack16<DT>(f[4], f[5]), pack16<DT>(f[6], f[7]));
-        } else {
-            float f = 0.0f;
-            if (add) { const uint32_t w = add[t * lda + c]; f = value_of<DT>(&w, 0); }
-            for (int j = 0; j < top; ++j) {
-                const int r = rows_of[j];
-                if (r >= 0 && r < R) { const uint32_t w = routes[r * ldr + c]; f = fmaf(weights[j], value_of<DT>(&w, 0), f); }
-            }
-            y[t * ldy + c] = (uint16_t)pack16<DT>(f, 0.0f);
+        for (int u = 0; u < UNITS; ++u) {
+            if (c0 + u * apart >= N) break;
+            S out;
+            if constexpr (VALUES == 8) out = make_uint4(pack16<DT>(f[u][0], f[u][1]), pack16<DT>(f[u][2], f[u][3]), pack16<DT>(f[u][4], f[u][5]), pack16<DT>(f[u][6], f[u][7]));
+            else out = (S)pack16<DT>(f[u][0], f[u][VALUES - 1]);
+            *reinterpret_cast<S *>(y + t * ldy + c0 + u * apart) = out;
         }
     }
 }
@@ -755,17 +769,20 @@ cudaError_t launch_route(const RouteCall &c, cudaStream_t st) {
 
 cudaError_t launch_combine(const uint16_t *routes, int64_t ldr, int64_t R, const float *weight, const int32_t *row, int64_t T, int top, int64_t N, const uint16_t *add,
                            int64_t lda, uint16_t *y, int64_t ldy, bool f16, cudaStream_t st) {
-    const auto odd = [](const void *q, int64_t ld) { return (reinterpret_cast<uintptr_t>(q) & 15u) != 0 || ld % 8 != 0; };
-    const bool wide = N % 8 == 0 && !odd(routes, ldr) && !odd(y, ldy) && !(add && odd(add, lda));
-    const int64_t per = wide ? N / 8 : N;
+    const auto fits = [&](int values) {
+        const auto row = [&](const void *q, int64_t ld) { return reinterpret_cast<uintptr_t>(q) % (2 * values) == 0 && ld % values == 0; };
+        return N % values == 0 && row(routes, ldr) && row(y, ldy) && (!add || row(add, lda));
+    };
+    const int values = fits(8) ? 8 : fits(2) ? 2 : 1;
+    const int64_t per = (N / values + units_for(values) - 1) / units_for(values);
     unsigned across = 32;
     while (across < 256 && across < per) across *= 2;
     const unsigned tokens = 256 / across;
     auto go = [&](auto kern) {
         return launch_overlapped(kern, dim3((unsigned)((T + tokens - 1) / tokens)), dim3(across, tokens), 0, st, 1, true, routes, ldr, (int)R, weight, row, (int)T, top, (int)N, add, lda, y, ldy);
     };
-    if (f16) return wide ? go(combine_kernel<true, true>) : go(combine_kernel<true, false>);
-    return wide ? go(combine_kernel<false, true>) : go(combine_kernel<false, false>);
+    if (f16) return values == 8 ? go(combine_kernel<true, 8>) : values == 2 ? go(combine_kernel<true, 2>) : go(combine_kernel<true, 1>);
+    return values == 8 ? go(combine_kernel<false, 8>) : values == 2 ? go(combine_kernel<false, 2>) : go(combine_kernel<false, 1>);
 }
 
 }  // namespace cq

@@ -222,6 +222,16 @@ def test_gemm(M, N, K, dtype):
     assert cq.cq_gemm_status(ws) == 0
 
 
+@pytest.mark.parametrize("M,N", [(70, n) for n in (1, 2, 3, 5, 6, 7, 8, 9, 15, 121, 122, 123, 124, 125, 126, 127, 129, 135, 249, 250)] + [(700, 259), (700, 381), (33, 1003), (300, 1134)])
+def test_rows_of_y_of_any_length(M, N):
+    """Rows of y that start at any value of a sixteen-byte piece, last row blocks of any width; nothing behind y is touched."""
+    w, x, y, y32 = product_case(M, N, 48, "bf16", seed=N)
+    room = torch.full((M * N + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = cq.cq_i8_gemm(w, x, out=room[:M * N].view(M, N))
+    check_product(got, y, y32)
+    assert torch.all(room[M * N:] == 7.0)
+
+
 @pytest.mark.parametrize("M", [2, 40, 200])
 def test_gemm_of_the_largest_sums(M):
     """All products -128 * 127 (or that with another sign) over the longest K: the sums stay within 32 bits."""

@@ -301,6 +301,18 @@ def test_combine(T, N, top, R, add, dtype):
     check_combine(got, y, row, weight, a)
 
 
+@pytest.mark.parametrize("N", [2, 3, 6, 255, 510, 1022, 1025, 2046, 4095, 4100])
+@pytest.mark.parametrize("shift", [0, 1, 2])
+def test_combine_of_any_length_and_alignment(N, shift):
+    """One, two or eight values to a load, by the alignment of all rows; values beside the rows are left alone."""
+    T, top, R = 37, 5, 60
+    y, row, weight, add = combine_case(T, N, top, R, "bf16", N + shift, True)
+    apart = torch.full((T, N + shift), 7.0, dtype=y.dtype, device="cuda")
+    cq.cq_combine(y.cuda(), as_routes(row, weight), add=add.cuda(), out=apart[:, :N])
+    check_combine(apart[:, :N], y, row, weight, add)
+    assert torch.all(apart[:, N:] == 7.0)
+
+
 def test_combine_rows_apart_in_place_and_unread_rows():
     T, N, top, R = 40, 512, 4, 60
     y, row, weight, a = combine_case(T, N, top, R, "bf16", 1, True)
