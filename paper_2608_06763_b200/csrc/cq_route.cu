@@ -646,12 +646,23 @@ __global__ void __launch_bounds__(1024) place_kernel(const Args p, int blocks) {
 // ---------------------------------------------------------------- the routes of a token together
 // y[t] = add[t] + sum over j of weight[t][j] routes[row[t][j]], in fp32 and in the order of j, rounded once.  A thread takes VALUES neighbouring values of a token (as many as
 // one load brings of rows that are so aligned), UNITS times; the loads of four routes are on their way together.  Rows outside [0, R) are no routes and are not read.  `add` may be
-// y.  Bound by memory: 4096 tokens of 4096 values and eight routes 46.4 us, 6.5 TB/s (with divisions of a flat index by the row's length 49.5).
+// y.  Bound by memory: 4096 tokens of 4096 values and eight routes 46.4 us, 6.5 TB/s (with divisions of a flat index by the row's length 49.5); of 4094 values 53, of 4095 79.
 template <int VALUES> struct Some;
 template <> struct Some<8> { using T = uint4; };
 template <> struct Some<2> { using T = uint32_t; };
-template <> struct Some<1> { using T = uint16_t; };
-constexpr int units_for(int values) { return values == 8 ? 1 : 4; }
+template <> struct Some<1> { using T = uint32_t; };
+template <int VALUES>
+__device__ __forceinline__ typename Some<VALUES>::T load_if(bool there, const uint16_t *p) {
+    if constexpr (VALUES == 1) {   // as one predicated load: 16-bit registers would be packed in pairs, each load waited for
+        uint32_t v;
+        asm volatile("{\n\t.reg .pred p;\n\t.reg .b16 h;\n\tsetp.ne.u32 p, %2, 0;\n\tmov.b16 h, 0;\n\t@p ld.global.b16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v) : "l"(p), "r"((uint32_t)there));
+        return v;
+    } else {
+        using T = typename Some<VALUES>::T;
+        return there ? *reinterpret_cast<const T *>(p) : T{};
+    }
+}
+constexpr int units_for(int values) { return 8 / values; }
 template <bool F16, int VALUES>
 __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, int64_t ldr, int R, const float *weight, const int32_t *row, int T, int top, int N, const uint16_t *add, int64_t lda,
                                                       uint16_t *y, int64_t ldy) {
@@ -671,9 +682,8 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, in
         float f[UNITS][VALUES];
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            S a{};
             const bool with = add && c0 + u * apart < N;
-            if (with) a = *reinterpret_cast<const S *>(add + t * lda + c0 + u * apart);
+            const S a = load_if<VALUES>(with, add + t * lda + c0 + u * apart);
 #pragma unroll
             for (int k = 0; k < VALUES; ++k) f[u][k] = with ? value(a, k) : 0.0f;
         }
@@ -687,7 +697,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, in
                 live[j] = r >= 0 && r < R;
                 const uint16_t *from = routes + r * ldr + c0;
 #pragma unroll
-                for (int u = 0; u < UNITS; ++u) v[j][u] = live[j] && c0 + u * apart < N ? *reinterpret_cast<const S *>(from + u * apart) : S{};
+                for (int u = 0; u < UNITS; ++u) v[j][u] = load_if<VALUES>(live[j] && c0 + u * apart < N, from + u * apart);
                 w[j] = live[j] ? weights[j0 + j] : 0.0f;
             }
 #pragma unroll
@@ -702,10 +712,10 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, in
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             if (c0 + u * apart >= N) break;
-            S out;
-            if constexpr (VALUES == 8) out = make_uint4(pack16<DT>(f[u][0], f[u][1]), pack16<DT>(f[u][2], f[u][3]), pack16<DT>(f[u][4], f[u][5]), pack16<DT>(f[u][6], f[u][7]));
-            else out = (S)pack16<DT>(f[u][0], f[u][VALUES - 1]);
-            *reinterpret_cast<S *>(y + t * ldy + c0 + u * apart) = out;
+            uint16_t *to = y + t * ldy + c0 + u * apart;
+            if constexpr (VALUES == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(pack16<DT>(f[u][0], f[u][1]), pack16<DT>(f[u][2], f[u][3]), pack16<DT>(f[u][4], f[u][5]), pack16<DT>(f[u][6], f[u][7]));
+            else if constexpr (VALUES == 2) *reinterpret_cast<uint32_t *>(to) = pack16<DT>(f[u][0], f[u][1]);
+            else *to = (uint16_t)pack16<DT>(f[u][0], 0.0f);
         }
     }
 }
@@ -775,9 +785,8 @@ cudaError_t launch_combine(const uint16_t *routes, int64_t ldr, int64_t R, const
     };
     const int values = fits(8) ? 8 : fits(2) ? 2 : 1;
     const int64_t per = (N / values + units_for(values) - 1) / units_for(values);
-    unsigned across = 32;
-    while (across < 256 && across < per) across *= 2;
-    const unsigned tokens = 256 / across;
+    const int64_t rounds = (per + 255) / 256;   // even ones, of whole warps
+    const unsigned across = (unsigned)((per + rounds - 1) / rounds + 31) / 32 * 32, tokens = 256 / across;
     auto go = [&](auto kern) {
         return launch_overlapped(kern, dim3((unsigned)((T + tokens - 1) / tokens)), dim3(across, tokens), 0, st, 1, true, routes, ldr, (int)R, weight, row, (int)T, top, (int)N, add, lda, y, ldy);
     };
