@@ -4,6 +4,10 @@ Quantisers and exchanges: equal byte for byte (every decision is exact).  Produc
 output is that, rounded once: equal bit for bit; and within half a step of the output type and three roundings to fp32 (the sum, the scales' product, theirs) of the
 formula in 64 bits.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -15,6 +19,7 @@ from oracle import route as ref_route
 
 pytestmark = pytest.mark.gpu
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 DTYPE = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
 
 
@@ -629,3 +634,19 @@ def test_routes_lead_the_other_routed_products():
     cases = [logical_case(N, K, 4, 128, seed=70 + e) for e in range(E)]
     yc = cq.cq_gemm_routed([c.pw for c in cases], x, r.token, off)
     assert torch.isfinite(cq.cq_combine(yc.view(T * top, N), r)).all()
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """What the library asks the device once (places for clusters, room for shared memory) is asked inside a capture here."""
+    code = """
+import torch, paper_2608_06763_b200 as cq
+w = cq.cq_i8_pack(torch.ones((1024, 512), dtype=torch.int8, device="cuda"), torch.full((1024,), 0.5, device="cuda"))
+x, out, ws = torch.ones((40, 512), device="cuda").bfloat16(), torch.zeros((40, 1024), dtype=torch.bfloat16, device="cuda"), cq.cq_i8_workspace(w, 40)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    cq.cq_i8_gemm(w, x, workspace=ws, out=out)
+graph.replay()
+assert torch.all(out == 256)
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=ROOT, timeout=300)
