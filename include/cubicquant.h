@@ -397,7 +397,7 @@ int cq_i8_gemm_routed(const void *w, const float *w_scale, const void *x, const 
 int cq_i8_linear_routed(const void *w, const float *w_scale, const uint16_t *x, int64_t ldx, int64_t T, const int32_t *route_token, const int32_t *expert_offset, int64_t E, uint16_t *y,
                         int act_f16, int64_t R, int64_t N, int64_t K, void *workspace, size_t workspace_bytes, void *stream);
 
-/* The experts of a layer in one call, behind cq_route: rows of x [T][H] quantised and sent to their routes (route_row), gate | up (E matrices 2 I x H), gated activation, down (E matrices
+/* The experts of a layer in one call, behind cq_route: rows of x [T][H] quantised and sent to their routes (route_row, each row once, as cq_route makes it), gate | up (E matrices 2 I x H), gated activation, down (E matrices
  * H x I), combined into y [T][H] (add: as for cq_combine).  Equal to cq_i8_linear_routed, cq_i8_swiglu_quantize, cq_i8_gemm_routed and cq_combine one after
  * another.  workspace: cq_i8_moe_workspace_bytes() bytes, zeroed once. */
 size_t cq_i8_moe_workspace_bytes(int64_t E, int64_t T, int top, int64_t H, int64_t I);
