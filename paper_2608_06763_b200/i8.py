@@ -172,11 +172,20 @@ def cq_i8_dequantize(q: I8Tensor, dtype: torch.dtype = torch.bfloat16, out: torc
     return out
 
 
+def _workspace(n: int, device) -> torch.Tensor:
+    """n bytes, zeroed where the device reports a wait that gave up; what else is read of them is written first."""
+    if n <= 1 << 22:   # one call for the host, which is slower than the device up to there
+        return torch.zeros(n, dtype=torch.uint8, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:512].zero_()
+    return ws
+
+
 def cq_i8_workspace(w: I8Tensor, M: int) -> torch.Tensor:
-    """A zeroed workspace for products of up to M rows (routes) with w.  A program that keeps one saves each call its own, and can ask cq_gemm_status of it whether a wait
+    """A workspace for products of up to M rows (routes) with w, ready to use.  A program that keeps one saves each call its own, and can ask cq_gemm_status of it whether a wait
     on the device gave up."""
     n = _lib().cq_i8_routed_workspace_bytes(w.matrices, max(M, 1), w.K)
-    return torch.zeros(max(n, 512), dtype=torch.uint8, device=w.layout.device)
+    return _workspace(max(n, 512), w.layout.device)
 
 
 def _output(w, M, dtype, workspace, out, own_workspace):
@@ -257,10 +266,10 @@ def cq_i8_gemm_routed(w: I8Tensor, x, route_token: torch.Tensor | None, expert_o
 
 
 def cq_i8_moe_workspace(gate_up: I8Tensor, down: I8Tensor, T: int, top: int) -> torch.Tensor:
-    """A zeroed workspace for cq_i8_moe of up to T tokens with `top` routes each."""
+    """A workspace for cq_i8_moe of up to T tokens with `top` routes each, ready to use."""
     n = _lib().cq_i8_moe_workspace_bytes(down.matrices, max(T, 1), top, down.M, down.K)
     _need(n > 0, f"no experts of {down.matrices} x {down.M} x {down.K} for {T} tokens of {top} routes")
-    return torch.zeros(n, dtype=torch.uint8, device=down.layout.device)
+    return _workspace(n, down.layout.device)
 
 
 def cq_i8_moe(gate_up: I8Tensor, down: I8Tensor, x: torch.Tensor, routes: Routes, add: torch.Tensor | None = None, workspace: torch.Tensor | None = None,

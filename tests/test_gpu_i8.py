@@ -650,3 +650,20 @@ graph.replay()
 assert torch.all(out == 256)
 """
     subprocess.run([sys.executable, "-c", code], check=True, cwd=ROOT, timeout=300)
+
+
+def test_workspaces_may_hold_anything_but_for_their_front():
+    """Products and expert blocks in workspaces full of NaN patterns behind the status words."""
+    E, H, I, T, top = 5, 528, 272, 150, 2
+    g = torch.Generator("cuda").manual_seed(4)
+    wu, wd = (cq.cq_i8_quantize(torch.randn((E, n, k), generator=g, device="cuda") * 0.05) for n, k in ((2 * I, H), (H, I)))
+    one = cq.cq_i8_quantize(torch.randn((700, H), generator=g, device="cuda"))
+    x, r = torch.randn((T, H), generator=g, device="cuda").bfloat16(), cq.cq_route(torch.randn((T, E), generator=g, device="cuda"), top)
+    results = []
+    for fill in (0, 0xFF):
+        ws, wm = cq.cq_i8_workspace(one, T), cq.cq_i8_moe_workspace(wu, wd, T, top)
+        ws[512:] = fill
+        wm[512:] = fill
+        results.append((cq.cq_i8_gemm(one, x, workspace=ws), cq.cq_i8_moe(wu, wd, x, r, workspace=wm)))
+        assert cq.cq_gemm_status(ws) == 0 and cq.cq_gemm_status(wm) == 0
+    assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(*results))
