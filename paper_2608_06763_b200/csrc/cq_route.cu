@@ -398,6 +398,7 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Mine &m, c
 
     const int rounds = bias ? min(p.top + 1, 32) : p.top;   // one more, to see how far it is from the last
     int chosen = -1, count = 0;
+    bool open = false;
     float got = NONE, best = key[0], limit = NONE, logit = 0.0f;   // lane j: the key of the j-th; the best key that this lane still has
 #pragma unroll
     for (int i = 1; i < V; ++i) best = fmaxf(best, key[i]);
@@ -454,18 +455,38 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Mine &m, c
                 }
             }
         }
+        if (bias) {   // of what is left none may lie in front of the last that is chosen
+            const int last = __shfl_sync(~0u, chosen, p.top - 1);
+            const float of_last = __shfl_sync(~0u, got, p.top - 1), logit_of_last = __shfl_sync(~0u, logit, p.top - 1);
+            if (last >= 0) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    open |= key[i] > NONE && !(of_last - key[i] > rest + 4.0f * U * fmaxf(fabsf(of_last), fabsf(key[i]))) && !(l[i] == logit_of_last && bias[m.first + i] == bias[last]);
+            }
+        }
     }
-    bool open = false;
     if (bias) {
-        // equal logits with equal biases are equal, and the lower index is first
+        // Equal logits with equal biases are equal, and the lower index is first.  Where that holds of the last that is chosen and the first that is not, another one
+        // behind them, as near or nearer, may lie in front of both.
+        bool tied = false;
         const int next = __shfl_down_sync(~0u, chosen, 1);
         const float after = __shfl_down_sync(~0u, got, 1);
         const float l1 = __shfl_down_sync(~0u, logit, 1);
         if (lane + 1 < rounds && chosen >= 0 && next >= 0) {
             const bool equal = logit == l1 && bias[chosen] == bias[next];
             open |= !equal && !(got - after > rest + 4.0f * U * fmaxf(fabsf(got), fabsf(after)));
+            tied = equal && lane + 1 == p.top;
         }
-        if (rounds == p.top) open |= all > p.top;   // of 32 wanted ones the last has nobody behind it to be compared with
+        if (all <= CANDIDATES && __any_sync(~0u, tied)) {   // with more of them that has been seen to
+            const int last = __shfl_sync(~0u, chosen, p.top - 1);
+            const float of_last = __shfl_sync(~0u, got, p.top - 1), logit_of_last = __shfl_sync(~0u, logit, p.top - 1);
+            if (lane < all) {
+                const int e = s.expert[lane];
+                const float k = s.key[lane];
+                open |= !(fabsf(of_last - k) > rest + 4.0f * U * fmaxf(fabsf(of_last), fabsf(k))) &&
+                        !(clean(one_logit<DT>(p.logits, t * p.ldl + e)) == logit_of_last && bias[e] == bias[last]);
+            }
+        }
     }
     if (__any_sync(~0u, open)) {
         if (all <= CANDIDATES) {
