@@ -17,7 +17,7 @@ using namespace rows;
 
 constexpr int KB = 128;                     // k of a tile
 constexpr int TILE_BYTES = ROWS * KB;
-constexpr int64_t MOST_K = 1 << 17;         // sums of so many products of codes stay within 32 bits: 2^17 * 128 * 127 < 2^31
+constexpr int64_t MOST_K = 1 << 17;         // sums of so many products of codes have 32 bits to themselves: from -2^17 * 128 * 127 > -2^31 to 2^17 * 128 * 128 = 2^31
 
 // byte of a tile that holds piece u (sixteen k) of row r
 __host__ __device__ inline int piece_offset(int r, int u) { return r * 128 + ((u ^ (r & 7)) << 4); }

@@ -21,6 +21,7 @@ struct GemmArgs {
     int M;                   // rows of x
     int64_t N;
     bool f16, wide;          // wide: rows of y start on 16-byte boundaries
+    bool longest;            // K is MOST_K
     bool early;              // launched right behind the quantiser of x: everything else may be read before that has ended
     const uint16_t *xr;      // FEW: rows of x in the model dtype, ldx apart
     int64_t ldx, K;
@@ -47,6 +48,9 @@ template <bool PAIR>
 __device__ __forceinline__ uint32_t idesc_of(uint32_t n) { return (2u << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | ((PAIR ? 16u : 8u) << 24); }
 // a sum times both scales: one rounding for the sum (beyond 2^24), one for the scales' product, one for theirs
 __device__ __forceinline__ float value_of_sum(uint32_t sum, float s) { return (float)(int32_t)sum * s; }
+// Sums of the longest K lie in (-2^31, 2^31]: the bits of -2^31 are those of +2^31, 2^17 products of -128 and -128, and 2^31 - 1 rounds to the same float.  (For every K at
+// the conversion it cost the output of large products 1 to 6 %.)
+__device__ __forceinline__ uint32_t largest_sum(uint32_t sum) { return sum == 0x80000000u ? 0x7FFFFFFFu : sum; }
 __device__ __forceinline__ uint32_t pack_out(uint32_t lo, uint32_t hi, float s_lo, float s_hi, bool f16) {
     const float a = value_of_sum(lo, s_lo), b = value_of_sum(hi, s_hi);
     return f16 ? pack16<DT_F16>(a, b) : pack16<DT_BF16>(a, b);
@@ -153,9 +157,9 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
     const int step = (512 >> lgCW) * 4;
     for (int r = (tid >> (lgCW - 1)) * 4; r < t.rows; r += step) {
         const int at = (mine * pitch + r) * 4, next = pitch * 4;
-        int4 f[2];
+        uint4 f[2];   // modulo 2^32, as the tensor core adds
 #pragma unroll
-        for (int j = 0; j < 2; ++j) f[j] = *reinterpret_cast<const int4 *>(own + at + j * next);
+        for (int j = 0; j < 2; ++j) f[j] = *reinterpret_cast<const uint4 *>(own + at + j * next);
 #pragma unroll
         for (int s = 1; s < 4; ++s)
             if (s < 1 << lgS) {
@@ -163,13 +167,17 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
                 const uint8_t *from = part + (COPY && other > run ? other - 1 : other) * bytes_of_run + at;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int4 v = *reinterpret_cast<const int4 *>(from + j * next);
+                    const uint4 v = *reinterpret_cast<const uint4 *>(from + j * next);
                     f[j].x += v.x; f[j].y += v.y; f[j].z += v.z; f[j].w += v.w;
                 }
             }
+        if (COPY && p.longest) {   // (what quantises itself has no -128)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) f[j] = make_uint4(largest_sum(f[j].x), largest_sum(f[j].y), largest_sum(f[j].z), largest_sum(f[j].w));
+        }
         const float4 xs = *reinterpret_cast<const float4 *>(x_scale + r);   // of what lies behind the rows nothing is stored
         const float x4[4] = {xs.x, xs.y, xs.z, xs.w};
-        const int lo[4] = {f[0].x, f[0].y, f[0].z, f[0].w}, hi[4] = {f[1].x, f[1].y, f[1].z, f[1].w};
+        const uint32_t lo[4] = {f[0].x, f[0].y, f[0].z, f[0].w}, hi[4] = {f[1].x, f[1].y, f[1].z, f[1].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t v = pack_out(lo[i], hi[i], w0 * x4[i], w1 * x4[i], p.f16);
@@ -434,6 +442,10 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
                     tmem_ld_16x32(from, lo);
                     tmem_ld_16x32(from + (16u << 16), hi);
                     tc::tmem_ld_wait();
+                    if (MODE != FEW && p.longest) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) { lo[i] = largest_sum(lo[i]); hi[i] = largest_sum(hi[i]); }
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float2 xs = BN >= 32 || c0 + 8 * i < BN ? *reinterpret_cast<const float2 *>(x_scale + c0 + 8 * i + 2 * (lane & 3)) : make_float2(0.0f, 0.0f);
@@ -545,7 +557,7 @@ static GemmArgs args_of(const void *w, const float *w_scale, const float *x_scal
     GemmArgs p{};
     p.w = (const uint8_t *)w; p.w_scale = w_scale; p.x_scale = x_scale; p.y = y; p.status = status;
     p.E = 1; p.NB = (int)((N + 127) / 128); p.KT = (int)((K + KB - 1) / KB); p.steps = (int)((K + 31) / 32);
-    p.M = (int)M; p.N = N; p.K = K; p.f16 = f16; p.wide = N % 8 == 0;
+    p.M = (int)M; p.N = N; p.K = K; p.f16 = f16; p.wide = N % 8 == 0; p.longest = K == MOST_K;
     p.band = 16;
     return p;
 }
