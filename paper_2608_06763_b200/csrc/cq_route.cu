@@ -248,7 +248,8 @@ __device__ __forceinline__ float reciprocal_approx(float v) { float r; asm("rcp.
 // follow one another among the best `top` + 1 are closer than both may be off, the row is decided in 64 bits.  How far off, in u = 2^-24, with
 // ex2.approx 4, rcp.approx 2 and log2(e) and its product 2 of the exponent: a sigmoid, s = 1 / (1 + e): of s (1 - s) 2 |l| + 4, which is 1.5 at most,
 // and 3 for the sum and the reciprocal: 4.5.  A softmax, z = max - l: 3 z of e^-z, 1.1 at most, and, of itself, 4, the sum of E terms V + 5 <= 37
-// with 3 times the mean of z <= ln E = 6.2 and 4, the reciprocal and the product 3: 68.  The bias adds |c| / 2 to each.
+// with 3 times the mean of z <= ln E = 6.2 and 4, the reciprocal and the product 3: 68.  Adding the bias is off by |c| more, half a step of the sum.  Two choice scores are then
+// out of order by 9 + 2 |c| or 136 + 2 |c| at most; what is taken, 16 + 4 |c| and 160 + 4 |c|, leaves room for the rounding of the comparison itself.
 //
 // The best: the (top + 1)-th largest of the lanes' largest is not above the (top + 1)-th largest of all, so what reaches it are candidates; hardly
 // more than that many, since few lanes have two.  Each finds its place by counting those in front of it.  Many equals, or a large
@@ -369,7 +370,8 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Mine &m, c
                     const int from = __ffs(__ballot_sync(~0u, left == k)) - 1;
                     if ((uint32_t)(lane - from) < 1u << p.lg_lanes) { stays = true; left = NONE; }
                 }
-                // Each of two choice scores, or of four halves, is off by |c| / 2 more, their sums by as much again.  What stays has to be that far above what does not.
+                // Each of four halves is off by |c| / 2 (single scores by |c|), either sum by |c| again: 4 |c| for two groups, all that is taken, besides
+                // what their scores are off (`rest` leaves room there).  What stays has to be that far above what does not.
                 const float most = warp_max(left);
                 if (most > NONE && !(least - most > rest + 4.0f * U * large)) {
                     const float near = fmaxf((p.best == 2 && second > NONE ? second : first) - rest - 4.0f * U * large, LEAST);
