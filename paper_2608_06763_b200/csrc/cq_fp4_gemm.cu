@@ -108,9 +108,12 @@ struct Shape {
 // order.  Sums arrive counted on a barrier, so nobody waits for the whole cluster in between.  Few rows are sent from the registers;
 // more go through the ring, which nobody needs any more, and from there in one copy to each CTA (128 rows: 6000 cycles in pieces of
 // sixteen bytes, 2500 so).
+// gave_up: the accumulator did not come.  Such a CTA sends zeros, and waits like the others for what is sent to it: a CTA whose sums have not all
+// come may not leave, since they would land in shared memory that is no longer its own.  After a wait that ran out it waits once more; the
+// status tells that y is not valid.
 template <class SH>
 __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, int lgS, int run, int k_tiles, int warp, int lane, uint8_t *ring, uint8_t *part, uint64_t *sums,
-                                             volatile int *dead) {
+                                             volatile int *dead, bool gave_up) {
     constexpr bool COPY = SH::BN > 16;
     const int lgCW = 7 - lgS, CW = 1 << lgCW, pitch = ((t.rows + 15) & ~15) + 4;
     const int quad = warp & 3, c = quad * 32 + lane, owner = c >> lgCW, tid = threadIdx.x - 128;
@@ -133,6 +136,10 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
         } else {
             tc::tmem_ld_wait();
         }
+        if (gave_up) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0;
+        }
 #pragma unroll
         for (int i = 0; i < 32; i += 4)
             if (c0 + i < t.rows) {
@@ -153,11 +160,14 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
         cluster_arrive();
     }
     const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
-    const bool ok = tc::mbar_wait(sums, 0, p.status, 58, tc::WAIT_LIMIT_CYCLES, dead);
-    if (!ok) *dead = 1;
+    const bool ok = tc::mbar_wait(sums, 0, p.status, 58, tc::WAIT_LIMIT_CYCLES, gave_up ? nullptr : dead);
+    if (!ok) {
+        *dead = 1;
+        tc::mbar_wait(sums, 0, p.status, 58);
+    }
     __syncwarp();
     if (COPY) cluster_arrive();   // what was copied from here has been received when all have arrived
-    if (!ok) return;
+    if (!ok || gave_up) return;
     // two channels of four rows a thread
     const int mine = 2 * (tid & (CW / 2 - 1));
     const int64_t ch = (int64_t)t.nb * 128 + (run << lgCW) + mine;
@@ -403,15 +413,13 @@ __global__ void __launch_bounds__(384, 1) fp4_gemm_kernel(const GemmArgs p, int 
             const Item t = tiles.at(local);
             const int acc = local & (ACCS - 1);
             const bool ok = tc::mbar_wait(&acc_full[acc], (local / ACCS) & 1, p.status, 56, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
-            if (epilogue_any(!ok)) {
-                *dead = 1;
-                if (SPLIT) { cluster_wait(); cluster_arrive(); }
-                break;
-            }
+            const bool gave_up = epilogue_any(!ok);
+            if (gave_up) *dead = 1;
             if constexpr (SPLIT) {
-                send_and_add<SH>(p, t, lgS, run, k1 - k0, warp, lane, ring, staged, sums, dead);
+                send_and_add<SH>(p, t, lgS, run, k1 - k0, warp, lane, ring, staged, sums, dead, gave_up);
                 break;
             }
+            if (gave_up) break;
             tc::tc_fence_after();
             const float alpha = (p.w_scale ? p.w_scale[t.e] : 1.0f) * (p.x_scale ? *p.x_scale : 1.0f);
             const int nb = t.nb * CTAS + half;

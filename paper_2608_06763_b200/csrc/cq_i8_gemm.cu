@@ -106,9 +106,11 @@ __device__ __forceinline__ void store_row(uint16_t *to, const uint8_t *row, int 
 // SPLIT, the eight warps that write y: this CTA's partial sums to the CTAs that add them, then its own 128 / S channels of all runs.  Sums arrive
 // counted on a barrier, so nobody waits for the whole cluster in between.  Few rows are sent from the registers; more go through the ring,
 // which nobody needs any more, and from there in one copy to each CTA.  ALIAS: those of the others land in the ring too, once all rings are free.
+// gave_up: the accumulator did not come.  Such a CTA sends zeros, and waits like the others for what is sent to it: a CTA whose sums have not all come may not leave, since
+// they would land in shared memory that is no longer its own.  After a wait that ran out it waits once more; the status tells that y is not valid.
 template <class SH>
 __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, int lgS, int run, int warp, int lane, uint8_t *ring, uint8_t *part, const float *x_scale, uint64_t *sums,
-                                             volatile int *dead) {
+                                             volatile int *dead, bool gave_up) {
     constexpr bool COPY = SH::BN > 16;
     const int lgCW = 7 - lgS, CW = 1 << lgCW, pitch = ((t.rows + 15) & ~15) + 4;
     const int quad = warp & 3, c = quad * 32 + lane, owner = c >> lgCW, tid = threadIdx.x - 128;
@@ -124,6 +126,10 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
         uint32_t v[32];
         tc::tmem_ld32(c0 + ((uint32_t)(quad * 32) << 16), v);
         tc::tmem_ld_wait();
+        if (gave_up) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0;
+        }
 #pragma unroll
         for (int i = 0; i < 32; i += 4)
             if (c0 + i < t.rows) {
@@ -147,11 +153,14 @@ __device__ __forceinline__ void send_and_add(const GemmArgs &p, const Item &t, i
     const int mine = 2 * (tid & (CW / 2 - 1));
     const int64_t ch = (int64_t)t.nb * 128 + (run << lgCW) + mine;
     const float w0 = ch < p.N ? p.w_scale[ch] : 0.0f, w1 = ch + 1 < p.N ? p.w_scale[ch + 1] : 0.0f;
-    const bool ok = tc::mbar_wait(sums, 0, p.status, 68, tc::WAIT_LIMIT_CYCLES, dead);
-    if (!ok) *dead = 1;
+    const bool ok = tc::mbar_wait(sums, 0, p.status, 68, tc::WAIT_LIMIT_CYCLES, gave_up ? nullptr : dead);
+    if (!ok) {
+        *dead = 1;
+        tc::mbar_wait(sums, 0, p.status, 68);
+    }
     __syncwarp();
     if (COPY) cluster_arrive();   // what was copied from here has been received when all have arrived
-    if (!ok) return;
+    if (!ok || gave_up) return;
     uint16_t *out = p.y + (int64_t)t.yrow * p.N + ch;
     const uint8_t *own = (COPY ? ring : part) + run * bytes_of_run;
     const int step = (512 >> lgCW) * 4;
@@ -420,16 +429,13 @@ __global__ void __launch_bounds__(384, 1) i8_gemm_kernel(const GemmArgs p, int l
                 ws[i] = !SPLIT && ch < p.N ? p.w_scale[(int64_t)t.e * p.N + ch] : 0.0f;
             }
             const bool ok = tc::mbar_wait(&acc_full[acc], (local / ACCS) & 1, p.status, 66, tc::WAIT_LIMIT_CYCLES, (volatile int *)dead);
-            if (epilogue_any(!ok)) {
-                *dead = 1;
-                if (SH::ALIAS) cluster_arrive();
-                if (SPLIT) { cluster_wait(); cluster_arrive(); }
-                break;
-            }
+            const bool gave_up = epilogue_any(!ok);
+            if (gave_up) *dead = 1;
             if constexpr (SPLIT) {
-                send_and_add<SH>(p, t, lgS, run, warp, lane, ring, staged, x_scale, sums, dead);
+                send_and_add<SH>(p, t, lgS, run, warp, lane, ring, staged, x_scale, sums, dead, gave_up);
                 break;
             }
+            if (gave_up) break;
             tc::tc_fence_after();
             constexpr int GROUPS = (BN + 63) / 64;
             uint32_t out16[GROUPS][16];
