@@ -381,7 +381,7 @@ int cq_i8_quantize(const void *x, int dtype, int64_t ldx, int64_t E, int64_t M, 
 int cq_i8_quantize_routed(const void *x, int dtype, int64_t ldx, int64_t T, const int32_t *route_token, const int32_t *expert_offset, int64_t E, int64_t R, int64_t K, void *layout,
                           float *scale, void *stream);
 int cq_i8_swiglu_quantize(const void *h, int dtype, int64_t ldh, int64_t M, int64_t I, const int32_t *expert_offset, int64_t E, void *layout, float *scale, void *stream);
-/* code * scale, y [E M][K] (routed: [M][K], rows of no group left alone), rounded once to `dtype`. */
+/* code * scale in fp32, y [E M][K] (routed: [M][K], rows of no group left alone), rounded from there to `dtype`. */
 int cq_i8_dequantize(const void *layout, const float *scale, int64_t E, int64_t M, int64_t K, const int32_t *expert_offset, void *y, int dtype, void *stream);
 
 /* y[M][N] = x W^T; w: layout and scales of the N x K matrix, x: layout and scales of M rows.  (float)sum * (w_scale * x_scale) in fp32, rounded

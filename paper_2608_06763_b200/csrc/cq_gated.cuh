@@ -1,11 +1,12 @@
-// The gated activation silu(gate) * up, rounded to the model dtype as its exact value is.
+// The gated activation silu(gate) * up: its exact value rounded to fp32, and that to the model dtype.
 #pragma once
 #include "cq_rows.cuh"
 
 namespace cq {
 namespace rows {
 
-// act = gate up / (1 + exp(-gate)).  32 bits leave its rounding open where it lies next to a border of the model dtype.  In units of 2^-24 of
+// act = gate up / (1 + exp(-gate)).  (Of bfloat16 activations some ten in a million, of binary16 ones eight times as many, become halfway values by the first rounding, and the second
+// takes the even neighbour, wherever the exact value lay.)  32 bits leave its rounding open where it lies next to a border of the model dtype.  In units of 2^-24 of
 // the value: gate * up is exact; exp(-g) = 2^h (1 + l ln 2), h + l = -g log2(e) with the constant in two parts, ex2.approx 4 and the two products 2;
 // the sum 1, the reciprocal 2, the last product 1: ten.  Where no value lies within BAND = 12 units of the last place (each at least such a unit)
 // of a border, the roundings stand; in a unit of sixteen one does in 170 in bfloat16, in 22 in binary16.  Gates beyond 60
