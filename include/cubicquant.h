@@ -326,7 +326,9 @@ int cq_debug_fp4_plan(int fmt, int64_t E, int64_t M, int64_t N, int64_t K, int q
 
 /* ---- Routing to experts (no counterpart in the paper, which leaves it outside) ------------------------------
  * What stands in front of a routed product and behind it: the choice of experts from a router's logits, with the route map that the
- * routed products take, and the weighted sum of a token's routes. */
+ * routed products take, and the weighted sum of a token's routes.  cq_fp4_*_routed and cq_i8_*_routed take the map as it is, on the device, so a
+ * captured call follows the router; cq_gemm_routed takes its offsets on the HOST: copy expert_offset there first, and name as many tokens as there
+ * are routes (fewer than T top where rows have fewer choices). */
 enum { CQ_SOFTMAX = 0, CQ_SIGMOID = 1 };
 
 /* logits [T][E] of `dtype` (CQ_BF16, CQ_F16, CQ_F32), rows ldl elements apart, any alignment.

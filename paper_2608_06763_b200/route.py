@@ -69,7 +69,9 @@ def cq_route_workspace(T: int, E: int, device=None) -> torch.Tensor:
 def cq_route(logits: torch.Tensor, top: int, score: int = CQ_SOFTMAX, bias: torch.Tensor | None = None, groups: int = 1, groups_kept: int | None = None, group_best: int = 2,
              renormalise: bool = True, scale: float = 1.0, workspace: torch.Tensor | None = None, out: Routes | None = None) -> Routes:
     """The `top` experts of each row of logits [T, E] (bfloat16, float16, float32), their weights and the map of their routes.  bias: fp32 [E], for the choice alone.
-    groups, groups_kept, group_best: experts of the best groups alone, by the sum of a group's best one or two."""
+    groups, groups_kept, group_best: experts of the best groups alone, by the sum of a group's best one or two.
+    cq_fp4_gemm_routed, cq_i8_gemm_routed and cq_i8_moe take the map as it is; cq_gemm_routed takes offsets on the host and no tokens behind the last route:
+    offset = routes.offset.tolist(); cq_gemm_routed(experts, x, routes.token[:offset[-1]], offset)."""
     dtype = _DTYPE.get(logits.dtype)
     if dtype is None or logits.dim() != 2:
         raise CubicQuantError("logits are [T, E] in bfloat16, float16 or float32")
