@@ -525,10 +525,11 @@ __device__ __forceinline__ int choose(const Args &p, int64_t t, const Mine &m, c
 // tells a route's place among those of its expert: the routes of tokens in front, in this chunk by counting bits, before it by a running
 // count.  Nothing depends on the order in which warps come.  The places among all blocks' routes are added by place_kernel, or, where one block has
 // all tokens, at once.
-// Bound by issue slots: 980 warp instructions a token (256 experts in groups).  8192 tokens: 13 us in normal blocks, of 20.4 in all: a row that 64 bits have to settle (six of them do) holds
-// its block up by one to four, the second kernel takes four.  Their bytes would take 0.8.
+// Bound by latency: a token is 980 warp instructions (256 experts in groups), most of them in a chain of reductions, of which 28 warps hide half (55 % of the issue slots are taken).  8192
+// tokens are 56 to a block, two for each warp one after the other: 19 to 20 us, some 10 of them in normal blocks; a row that 64 bits have to settle (six of them do) holds its block up by one to four, the
+// second kernel takes four.  Their bytes would take 0.8.
 constexpr int CHUNK = 128, PLACED = 2;   // PLACED: blocks of tokens whose routes one block of place_kernel places
-// At least as many as there are experts.  More warps hide more of a token's 3 us, until registers get short: 256 experts, 8192 / 65536 tokens with 768 threads 21.5 / 94, 896 20.4 / 92.
+// At least as many as there are experts.  More warps hide more of a token's 3 us, until registers get short: 256 experts, 8192 / 65536 tokens with 768 threads 20.0 / 85, 896 19.1 / 84.
 constexpr int threads_for(int V) { return V <= 4 ? 1024 : V == 8 ? 896 : 512; }
 static_assert(CHUNK % 32 == 0 && MAX_EXPERTS <= 512, "words of bits; a thread for each expert");
 
@@ -669,7 +670,8 @@ __global__ void __launch_bounds__(1024) place_kernel(const Args p, int blocks) {
 // ---------------------------------------------------------------- the routes of a token together
 // y[t] = add[t] + sum over j of weight[t][j] routes[row[t][j]], in fp32 and in the order of j, rounded once.  A thread takes VALUES neighbouring values of a token (as many as
 // one load brings of rows that are so aligned), UNITS times; the loads of four routes are on their way together.  Rows outside [0, R) are no routes and are not read.  `add` may be
-// y.  Bound by memory: 4096 tokens of 4096 values and eight routes 46.4 us, 6.5 TB/s (with divisions of a flat index by the row's length 49.5); of 4094 values 53, of 4095 79.
+// y.  Bound by memory: 4096 tokens of 4096 values and eight routes 46.4 us, 6.5 TB/s (with divisions of a flat index by the row's length 49.5); of 4094 values 53.  Of 4095 79,
+// bound by instructions: one value to a load, 55 M warp instructions where wide loads need 25, 64 % of the issue slots taken by 24 warps to an SM (their registers).
 template <int VALUES> struct Some;
 template <> struct Some<8> { using T = uint4; };
 template <> struct Some<2> { using T = uint32_t; };
@@ -748,7 +750,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint16_t *routes, in
 using namespace route;
 
 // Blocks of tokens.  One block has all where there are few, and its launch is the only one: a round of its warps takes 4 us more the fuller it is, the
-// second launch 3 (256 experts in groups, us alone / in two launches: 16 tokens 7 / 8, 32: 9.6 / 8, 64: 14.2 / 8).  Else as many blocks as SMs, of four tokens or more.
+// second launch 3 (256 experts in groups, us alone / in two launches: 16 tokens 5.1 / 7.7, 32: 8.4 / 7.6, 64: 12.3 / 7.7).  Else as many blocks as SMs, of four tokens or more.
 constexpr int ALONE = 16;
 static_assert(ALONE <= CHUNK, "one chunk");
 static int blocks_of(int64_t T) {
